@@ -277,6 +277,79 @@ lpq_status lpq_decoder_layer(const lpq_layer *layer, const lpq_layer_cfg *cfg, c
                              int32_t n_seqs, int32_t T, int32_t pos0, const void *x, void *y, void *workspace,
                              size_t workspace_bytes, void *hip_stream);
 
+/* ---- Batches of sequences of different lengths: paged caches and packed rows ---------------------------------
+ * A server's step has n_seqs sequences, sequence s with q_s >= 0 new tokens behind the positions it has cached.  The rows of all of
+ * them are packed: rows cu_q[s] .. cu_q[s + 1] - 1 of a batch of M rows are sequence s's; rows from cu_q[n_seqs] on belong to nobody (a
+ * batch may be padded to a fixed M, as a captured graph needs it) and their outputs are left as they were.  All lengths, offsets, slots and tables are
+ * int32 DEVICE arrays: a step can be planned, appended and attended to without the host knowing a length.
+ * K and V live in a pool of pages that a layer's two buffers hold: k_pages, v_pages [n_pages][n_kv_heads][page_size][head_dim], 16-bit
+ * elements, positions of a page in order.  Entry i of a sequence's row of the block table is the page of its positions i * page_size .. ; one table serves
+ * all layers.  Page ids and slots are checked on the device: what is not in the pool is neither read nor written. */
+typedef enum { LPQ_DT_FP16 = 0, LPQ_DT_BF16 = 1 } lpq_dtype;
+
+/* Heads of a batch's rows: qkv is [M][(n_heads + 2 * n_kv_heads) * head_dim], per row q | k | v; query head h reads K/V head
+ * h / (n_heads / n_kv_heads).  dtype is that of qkv, the pages and the output. */
+typedef struct {
+    int32_t n_heads, n_kv_heads;     /* n_heads % n_kv_heads == 0                                          */
+    int32_t head_dim;                /* 64 or 128                                                          */
+    int32_t dtype;                   /* lpq_dtype                                                          */
+} lpq_attn_cfg;
+
+/* The pool's bookkeeping, on the device, caller-owned.  The free pages are entries head .. head + free - 1 (modulo n_pages) of `ring`;
+ * counters = {head, free}.  An empty pool of n pages: ring = 0 .. n - 1, counters = {0, n}. */
+typedef struct {
+    int32_t page_size;               /* 16, 32, 64, 128 or 256                                             */
+    int32_t n_pages;                 /* entries of ring; n_pages * page_size < 2^31                        */
+    int32_t max_pages;               /* entries of a sequence's row of the table; max_pages * page_size <= 2^30 */
+    int32_t *table;                  /* [n_seqs][max_pages]                                                */
+    int32_t *ring, *counters;        /* [n_pages], [2]; read by lpq_paged_plan only                        */
+} lpq_page_pool;
+
+/* What lpq_paged_plan writes, all of it: */
+typedef struct {
+    int32_t *counters;               /* [2] the pool's afterwards; may be the pool's own                   */
+    int32_t *cu_q;                   /* [n_seqs + 1] first rows (at most M)                                */
+    int32_t *kv_lens;                /* [n_seqs] cached positions afterwards; may be `past`                */
+    int32_t *slots;                  /* [M] page * page_size + offset of a row's position, -1: none        */
+    int32_t *positions;              /* [M] a row's position, 0 where it has no slot                       */
+    int32_t *info;                   /* [4] rows, pages taken, pages returned, sequences starved           */
+} lpq_page_plan;
+
+/* The plan of a step.  past[s]: positions of sequence s that are cached (its row of the table has their pages); q_lens[s]: its new tokens, or
+ * negative: it has finished.  Pages for the new tokens are taken off the ring in order of the sequences and written behind the pages a sequence
+ * has; nothing else of the table changes.  A finished sequence's pages go behind the ring's last free page (as far as the ring has
+ * room) and can be taken from the next call on; its kv_lens is 0.  A sequence is starved if its rows end behind M, its
+ * positions behind max_pages * page_size, or its and its predecessors' needs exceed the free pages: it gets no page, its rows no slots, its kv_lens stays
+ * at `past`, and the caller may plan it again later.  Negative past counts as 0, counters are taken into their range.
+ * With in-place counters and kv_lens a step is the same call every time and can be replayed from a graph.  The other outputs must not overlap the
+ * inputs.  n_seqs <= 2048.  M > 4096 uses n_seqs words of the library's workspace.
+ * Errors: NULL, SHAPE (page_size, counts, limits above), ALIGN (4 bytes), BUFSIZE, DEVICE. */
+lpq_status lpq_paged_plan(const lpq_page_pool *pool, const int32_t *past, const int32_t *q_lens, int32_t n_seqs, int32_t M,
+                          const lpq_page_plan *plan, void *hip_stream);
+
+/* K and V parts of each row of qkv to its slot of the pages.  Rows whose slot is negative or behind the pool are skipped.  Slots of a call are
+ * distinct (as a plan's are): where two rows name the same one, it ends up with either's 16-byte pieces.  Only page_size and n_pages of the pool are used.
+ * Errors: NULL, SHAPE (heads, page_size, counts; M * n_heads <= 2^27), UNSUPPORTED (dtype), ALIGN, DEVICE. */
+lpq_status lpq_paged_append(const void *qkv, const lpq_attn_cfg *cfg, const lpq_page_pool *pool, void *k_pages, void *v_pages,
+                            const int32_t *slots, int32_t M, void *hip_stream);
+
+/* Causal attention of the new tokens over the pages, after their append: token t of sequence s stands at position kv_lens[s] - q_s + t and sees
+ * positions up to its own; out = softmax(q . k / sqrt(head_dim) + slope * (key position - query position)) . v per head, heads
+ * concatenated, [M][n_heads * head_dim].  Positions whose table entry is not a page of the pool, or lies behind the table, count as masked; a row that sees
+ * nothing (or only scores of minus infinity) gives zero.  Values at masked places, infinite or NaN, do not touch the result.
+ * alibi_slopes: fp32 [n_heads] or NULL.  q_s may be 1 (decode), a chunk, a whole prompt, 0, and differ from sequence to sequence.
+ * max_q, max_kv: the largest q_s and kv_lens the caller expects; they choose kernels and splits, and larger ones than that are only slower.
+ * Partial results are kept in the library's workspace; where a reservation leaves no room the work is not split.
+ * Errors: NULL, SHAPE (as above, n_seqs in 1 .. 2048, max_q, max_kv < 1), UNSUPPORTED (dtype), ALIGN, DEVICE. */
+lpq_status lpq_paged_attention(const void *qkv, const lpq_attn_cfg *cfg, const lpq_page_pool *pool, const void *k_pages, const void *v_pages,
+                               const float *alibi_slopes, const int32_t *cu_q, const int32_t *kv_lens, int32_t n_seqs, int32_t M,
+                               int32_t max_q, int32_t max_kv, void *out, void *hip_stream);
+
+/* Causal attention of whole prompts over themselves: the same with keys and values read from the packed rows, no cache.
+ * Errors: as lpq_paged_attention. */
+lpq_status lpq_packed_attention(const void *qkv, const lpq_attn_cfg *cfg, const float *alibi_slopes, const int32_t *cu_q, int32_t n_seqs,
+                                int32_t M, int32_t max_q, void *out, void *hip_stream);
+
 /* Variance indicator of one linear operator (Sec. 4.2, Theorem 1 and Eq. 3): the estimated extra output
  * variance D_W * S_W(b)^2 * G(X) under b-bit weight quantisation, G(X) = Var[X] / 4 (deterministic rounding,
  * stochastic = 0) or (E[X]^2 + Var[X]) / 6 (stochastic = 1), E and Var over all elements of X.  A layer's

@@ -5,6 +5,7 @@ Every step of the path (quantise, pack, decode and prefill linears, stage dispat
 HIP kernels of liblpq.so; torch is used to allocate device memory and to name the stream.
 There is no CPU fallback: if the library is missing, loading raises.
 """
+import collections
 import ctypes
 import os
 
@@ -17,7 +18,8 @@ LPQ_OK = 0
 LINEARS = ("qkv", "out", "fc1", "fc2")
 EXPORTS = ("lpq_packed_sizes", "lpq_quantize_pack", "lpq_quantize_pack_rows", "lpq_load_quantize_pack",
            "lpq_qlinear_prefill", "lpq_qlinear_decode", "lpq_qlinear_fused", "lpq_stage_linears", "lpq_stage_linears_noalloc", "lpq_layernorm",
-           "lpq_kv_append", "lpq_attention", "lpq_decoder_layer_workspace", "lpq_decoder_layer", "lpq_variance_indicator",
+           "lpq_kv_append", "lpq_attention", "lpq_paged_plan", "lpq_paged_append", "lpq_paged_attention", "lpq_packed_attention",
+           "lpq_decoder_layer_workspace", "lpq_decoder_layer", "lpq_variance_indicator",
            "lpq_mem_embedding_bytes", "lpq_mem_layer_bytes", "lpq_mem_kv_bytes", "lpq_latency_fit", "lpq_latency_predict",
            "lpq_plan_objective", "lpq_plan_adabits", "lpq_plan_bitwidth_transfer",
            "lpq_workspace_policy", "lpq_workspace_reserve", "lpq_workspace_bytes", "lpq_set_decode_routing", "lpq_route_of", "lpq_layer_route_of",
@@ -59,6 +61,19 @@ class lpq_layer_state(ctypes.Structure):
                 ("alibi_slopes", ctypes.c_void_p)]
 
 
+class lpq_attn_cfg(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class lpq_page_pool(ctypes.Structure):
+    _fields_ = [("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("ring", ctypes.c_void_p), ("counters", ctypes.c_void_p)]
+
+
+class lpq_page_plan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("counters", "cu_q", "kv_lens", "slots", "positions", "info")]
+
+
 class lpq_model_shape(ctypes.Structure):
     _fields_ = [("h1", ctypes.c_int64), ("h2", ctypes.c_int64), ("vocab", ctypes.c_int64), ("d_t", ctypes.c_int64),
                 ("pos", ctypes.c_int64), ("rmsnorm", ctypes.c_int32), ("pad", ctypes.c_int32)]
@@ -72,6 +87,7 @@ class lpq_layer_route(ctypes.Structure):
     _fields_ = [("norm1", ctypes.c_int32), ("norm2", ctypes.c_int32), ("append", ctypes.c_int32)]
 
 
+LPQ_DT_FP16, LPQ_DT_BF16 = 0, 1
 LPQ_NORM_LAUNCH, LPQ_NORM_IN_LINEAR, LPQ_NORM_BEHIND_SPLITS = 0, 1, 2
 LPQ_ROUTE_EVEN_SHARE, LPQ_ROUTE_ROWS, LPQ_ROUTE_MID, LPQ_ROUTE_PREFILL = 0, 1, 2, 3
 _dp, _ip = ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)
@@ -117,6 +133,11 @@ def load_library():
         cfgp, stp = ctypes.POINTER(lpq_layer_cfg), ctypes.POINTER(lpq_layer_state)
         L.lpq_kv_append.argtypes = [vp, cfgp, stp, i32, i32, i32, vp]
         L.lpq_attention.argtypes = [vp, cfgp, stp, i32, i32, i32, vp, vp]
+        acfg, pool = ctypes.POINTER(lpq_attn_cfg), ctypes.POINTER(lpq_page_pool)
+        L.lpq_paged_plan.argtypes = [pool, vp, vp, i32, i32, ctypes.POINTER(lpq_page_plan), vp]
+        L.lpq_paged_append.argtypes = [vp, acfg, pool, vp, vp, vp, i32, vp]
+        L.lpq_paged_attention.argtypes = [vp, acfg, pool, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp]
+        L.lpq_packed_attention.argtypes = [vp, acfg, vp, vp, i32, i32, i32, vp, vp]
         L.lpq_decoder_layer_workspace.argtypes = [ctypes.POINTER(lpq_layer), cfgp, i32]
         L.lpq_decoder_layer.argtypes = [ctypes.POINTER(lpq_layer), cfgp, stp, ctypes.c_int, i32, i32, i32, vp, vp, vp, ctypes.c_size_t, vp]
         L.lpq_unpack_dequant.argtypes = [ctypes.POINTER(lpq_qweight), vp, vp]
@@ -319,6 +340,123 @@ def lpq_attention(qkv, state, n_seqs, T, pos0, out=None, stream=None):
     st = state.struct()
     _check(load_library().lpq_attention(qkv.data_ptr(), ctypes.byref(state.cfg), ctypes.byref(st), n_seqs, T, pos0, out.data_ptr(),
                                         _stream(stream)), "lpq_attention")
+    return out
+
+
+# ---- batches of sequences of different lengths: paged caches and packed rows (see include/lpq.h) -------------------
+
+PagePlan = collections.namedtuple("PagePlan", "cu_q kv_lens slots positions counters info")
+
+
+def _on(device, **tensors):
+    """Each tensor (name=(tensor, dtype, dimensions)) is contiguous, of that type, and on the current CUDA device, where the kernels run."""
+    import torch
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current CUDA device")
+    for name, (t, dtype, dims) in tensors.items():
+        if t.dtype != dtype or t.dim() != dims or t.device != device or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous %d-D %s tensor on %s" % (name, dims, dtype, device))
+
+
+def _attn_cfg(qkv, n_heads, n_kv_heads):
+    import torch
+    if qkv.dtype not in (torch.float16, torch.bfloat16) or qkv.dim() != 2:
+        raise ValueError("qkv must be 2-D, fp16 or bf16")
+    heads = n_heads + 2 * n_kv_heads
+    if n_heads < 1 or n_kv_heads < 1 or qkv.shape[1] % heads:
+        raise ValueError("qkv has %d columns, not a multiple of %d heads" % (qkv.shape[1], heads))
+    return lpq_attn_cfg(n_heads, n_kv_heads, qkv.shape[1] // heads, LPQ_DT_FP16 if qkv.dtype == torch.float16 else LPQ_DT_BF16)
+
+
+def _paged_cfg(qkv, k_pages, v_pages):
+    """(attention cfg, page size, pages): K and V pages are [n_pages][kv heads][page_size][head_dim]."""
+    _on(qkv.device, qkv=(qkv, qkv.dtype, 2), k_pages=(k_pages, qkv.dtype, 4), v_pages=(v_pages, qkv.dtype, 4))
+    n_pages, kv, page_size, d = k_pages.shape
+    if v_pages.shape != k_pages.shape:
+        raise ValueError("k_pages and v_pages must have the same shape")
+    cfg = _attn_cfg(qkv, qkv.shape[1] // max(d, 1) - 2 * kv, kv)
+    if cfg.head_dim != d:
+        raise ValueError("qkv's columns do not match the pages' heads")
+    return cfg, page_size, n_pages
+
+
+def _out_and_slopes(qkv, cfg, out, alibi_slopes):
+    import torch
+    shape = (qkv.shape[0], cfg.n_heads * cfg.head_dim)
+    if out is None:
+        out = torch.zeros(shape, dtype=qkv.dtype, device=qkv.device)          # rows that no sequence has stay as they are: zero
+    else:
+        _on(qkv.device, out=(out, qkv.dtype, 2))
+        if tuple(out.shape) != shape:
+            raise ValueError("out must be [%d][%d]" % shape)
+    if alibi_slopes is not None:
+        _on(qkv.device, alibi_slopes=(alibi_slopes, torch.float32, 1))
+        if alibi_slopes.shape[0] != cfg.n_heads:
+            raise ValueError("alibi_slopes must have a value per head")
+    return out, alibi_slopes.data_ptr() if alibi_slopes is not None else None
+
+
+def lpq_paged_plan(past, q_lens, table, ring, counters, page_size, M, plan=None, stream=None):
+    """Where a step's M rows go: past, q_lens int32 [n_seqs]; table int32 [n_seqs][max_pages], ring int32 [n_pages] and counters int32 {head, free} are the
+    pool's, the first two updated in place.  plan: the outputs (PagePlan or a tuple in its order), of which kv_lens may be `past` and counters the pool's
+    own; None allocates them.  -> PagePlan."""
+    import torch
+    i32, n = torch.int32, past.shape[0]
+    if plan is None:
+        plan = PagePlan(*(torch.empty(m, dtype=i32, device=past.device) for m in (n + 1, n, M, M, 2, 4)))
+    plan = PagePlan(*plan)
+    _on(past.device, past=(past, i32, 1), q_lens=(q_lens, i32, 1), table=(table, i32, 2), ring=(ring, i32, 1), counters=(counters, i32, 1),
+        cu_q=(plan.cu_q, i32, 1), kv_lens=(plan.kv_lens, i32, 1), slots=(plan.slots, i32, 1), positions=(plan.positions, i32, 1),
+        new_counters=(plan.counters, i32, 1), info=(plan.info, i32, 1))
+    sizes = (q_lens.shape[0], table.shape[0], counters.shape[0], *(t.shape[0] for t in plan))
+    if sizes != (n, n, 2, n + 1, n, M, M, 2, 4):
+        raise ValueError("sizes of the plan's tensors do not match %d sequences and %d rows" % (n, M))
+    p = lpq_page_pool(page_size, ring.shape[0], table.shape[1], table.data_ptr(), ring.data_ptr(), counters.data_ptr())
+    o = lpq_page_plan(plan.counters.data_ptr(), plan.cu_q.data_ptr(), plan.kv_lens.data_ptr(), plan.slots.data_ptr(), plan.positions.data_ptr(), plan.info.data_ptr())
+    _check(load_library().lpq_paged_plan(ctypes.byref(p), past.data_ptr(), q_lens.data_ptr(), n, M, ctypes.byref(o), _stream(stream)), "lpq_paged_plan")
+    return plan
+
+
+def lpq_paged_append(qkv, k_pages, v_pages, slots, stream=None):
+    """K and V of the rows of qkv ([M][(heads + 2 kv heads) * d], fp16 or bf16) into their slots of the pages ([n_pages][kv heads][page_size][d])."""
+    import torch
+    cfg, page_size, n_pages = _paged_cfg(qkv, k_pages, v_pages)
+    _on(qkv.device, slots=(slots, torch.int32, 1))
+    if slots.shape[0] != qkv.shape[0]:
+        raise ValueError("slots must have a value per row")
+    p = lpq_page_pool(page_size, n_pages, 0, None, None, None)
+    _check(load_library().lpq_paged_append(qkv.data_ptr(), ctypes.byref(cfg), ctypes.byref(p), k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr(),
+                                           qkv.shape[0], _stream(stream)), "lpq_paged_append")
+
+
+def lpq_paged_attention(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None, max_kv=None, alibi_slopes=None, out=None, stream=None):
+    """Causal attention of the packed rows over the pages of their sequences: table int32 [n_seqs][max_pages], cu_q int32 [n_seqs + 1], kv_lens int32
+    [n_seqs] (new tokens included).  max_q, max_kv: the most to expect (None: the batch, the table).  -> out [M][heads * d]."""
+    import torch
+    i32 = torch.int32
+    cfg, page_size, n_pages = _paged_cfg(qkv, k_pages, v_pages)
+    _on(qkv.device, table=(table, i32, 2), cu_q=(cu_q, i32, 1), kv_lens=(kv_lens, i32, 1))
+    n, M = kv_lens.shape[0], qkv.shape[0]
+    if cu_q.shape[0] != n + 1 or table.shape[0] != n:
+        raise ValueError("table, cu_q and kv_lens do not have the same number of sequences")
+    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes)
+    p = lpq_page_pool(page_size, n_pages, table.shape[1], table.data_ptr(), None, None)
+    _check(load_library().lpq_paged_attention(qkv.data_ptr(), ctypes.byref(cfg), ctypes.byref(p), k_pages.data_ptr(), v_pages.data_ptr(), slopes, cu_q.data_ptr(),
+                                              kv_lens.data_ptr(), n, M, M if max_q is None else int(max_q),
+                                              table.shape[1] * page_size if max_kv is None else int(max_kv), out.data_ptr(), _stream(stream)),
+           "lpq_paged_attention")
+    return out
+
+
+def lpq_packed_attention(qkv, cu_q, n_heads, n_kv_heads, max_q=None, alibi_slopes=None, out=None, stream=None):
+    """Causal attention of whole prompts, packed in the rows of qkv, over themselves; cu_q int32 [n_seqs + 1].  -> out [M][heads * d]."""
+    import torch
+    cfg = _attn_cfg(qkv, n_heads, n_kv_heads)
+    _on(qkv.device, qkv=(qkv, qkv.dtype, 2), cu_q=(cu_q, torch.int32, 1))
+    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes)
+    M = qkv.shape[0]
+    _check(load_library().lpq_packed_attention(qkv.data_ptr(), ctypes.byref(cfg), slopes, cu_q.data_ptr(), cu_q.shape[0] - 1, M,
+                                               M if max_q is None else int(max_q), out.data_ptr(), _stream(stream)), "lpq_packed_attention")
     return out
 
 

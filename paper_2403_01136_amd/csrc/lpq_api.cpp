@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "lpq_common.h"
+#include "lpq_paged_index.h"
 
 namespace lpq {
 
@@ -825,6 +826,58 @@ lpq_status run_attention(const void* qkv, const lpq_layer_cfg* cfg, const lpq_la
                                    range, splits, out, part, stream) == hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
 }
 
+bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+// ---- paged caches and packed batches
+int page_shift_of(int page_size)         // -1: not a page size
+{
+    for (int s = 4; s <= 8; ++s)
+        if (page_size == 1 << s) return s;
+    return -1;
+}
+
+lpq_status check_heads(const lpq_attn_cfg* c, int32_t M)
+{
+    if (c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads != 0 || (c->head_dim != 64 && c->head_dim != 128)) return LPQ_ERR_SHAPE;
+    if (c->n_heads > 65536 || M < 1 || (int64_t)M * c->n_heads > (int64_t)1 << 27) return LPQ_ERR_SHAPE;
+    if (c->dtype != LPQ_DT_FP16 && c->dtype != LPQ_DT_BF16) return LPQ_ERR_UNSUPPORTED;
+    return LPQ_OK;
+}
+
+lpq_status check_pool(const lpq_page_pool* p)
+{
+    const int shift = page_shift_of(p->page_size);
+    if (shift < 0 || p->n_pages < 1 || (int64_t)p->n_pages << shift > INT32_MAX) return LPQ_ERR_SHAPE;
+    return LPQ_OK;
+}
+
+lpq_status check_table(const lpq_page_pool* p, int32_t n_seqs)
+{
+    if (p->max_pages < 1 || (int64_t)p->max_pages << page_shift_of(p->page_size) > (int64_t)1 << 30) return LPQ_ERR_SHAPE;
+    if (n_seqs < 1 || n_seqs > PAGED_MAX_SEQS) return LPQ_ERR_SHAPE;
+    return LPQ_OK;
+}
+
+// kp null: packed rows
+lpq_status run_batch_attention(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* kp, const void* vp, const float* slopes,
+                               const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M, int32_t max_q, int32_t max_kv, void* out,
+                               hipStream_t stream)
+{
+    int cus = 0;
+    const lpq_status cst = device_cus(&cus);
+    if (cst != LPQ_OK) return cst;
+    AttentionPlan plan = attention_plan(*cfg, kp != nullptr, n_seqs, M, max_q, max_kv, cus);
+    float* part = nullptr;
+    const size_t floats = std::max(plan.stream_floats, plan.tile_floats);
+    if (floats) {
+        const lpq_status s = workspace(false, floats * sizeof(float), &part);
+        if (s == LPQ_ERR_BUFSIZE) plan.splits = 1, plan.stream_floats = plan.tile_floats = 0;      // no room for parts: nothing is split
+        else if (s != LPQ_OK) return s;
+    }
+    return launch_batch_attention(plan, *cfg, qkv, kp, vp, pool ? pool->table : nullptr, pool ? page_shift_of(pool->page_size) : 4, pool ? pool->n_pages : 0,
+                                  pool ? pool->max_pages : 0, cu_q, kv_lens, slopes, n_seqs, M, out, part, stream) == hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
+}
+
 }  // namespace
 }  // namespace lpq
 
@@ -917,6 +970,68 @@ lpq_status lpq_attention(const void* qkv, const lpq_layer_cfg* cfg, const lpq_la
     if (s != LPQ_OK) return s;
     if (misaligned(qkv) || misaligned(out)) return LPQ_ERR_ALIGN;
     return run_attention(qkv, cfg, st, n_seqs, T, pos0, false, out, static_cast<hipStream_t>(hip_stream));
+}
+
+lpq_status lpq_paged_plan(const lpq_page_pool* pool, const int32_t* past, const int32_t* q_lens, int32_t n_seqs, int32_t M, const lpq_page_plan* plan,
+                          void* hip_stream)
+{
+    if (!pool || !past || !q_lens || !plan || !pool->table || !pool->ring || !pool->counters || !plan->counters || !plan->cu_q || !plan->kv_lens ||
+        !plan->slots || !plan->positions || !plan->info)
+        return LPQ_ERR_NULL;
+    lpq_status s = check_pool(pool);
+    if (s == LPQ_OK) s = check_table(pool, n_seqs);
+    if (s != LPQ_OK) return s;
+    if (M < 1 || M > 1 << 27) return LPQ_ERR_SHAPE;
+    for (const void* p : {(const void*)past, (const void*)q_lens, (const void*)pool->table, (const void*)pool->ring, (const void*)pool->counters,
+                          (const void*)plan->counters, (const void*)plan->cu_q, (const void*)plan->kv_lens, (const void*)plan->slots,
+                          (const void*)plan->positions, (const void*)plan->info})
+        if (misaligned4(p)) return LPQ_ERR_ALIGN;
+    float* ws = nullptr;
+    const size_t need = paged_plan_workspace_bytes(n_seqs, M);
+    if (need && (s = workspace(false, need, &ws)) != LPQ_OK) return s;
+    return launch_paged_plan(*pool, page_shift_of(pool->page_size), past, q_lens, n_seqs, M, *plan, ws, static_cast<hipStream_t>(hip_stream)) == hipSuccess
+               ? LPQ_OK : LPQ_ERR_DEVICE;
+}
+
+lpq_status lpq_paged_append(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, void* k_pages, void* v_pages, const int32_t* slots,
+                            int32_t M, void* hip_stream)
+{
+    if (!qkv || !cfg || !pool || !k_pages || !v_pages || !slots) return LPQ_ERR_NULL;
+    lpq_status s = check_heads(cfg, M);
+    if (s == LPQ_OK) s = check_pool(pool);
+    if (s != LPQ_OK) return s;
+    if (misaligned(qkv) || misaligned(k_pages) || misaligned(v_pages) || misaligned4(slots)) return LPQ_ERR_ALIGN;
+    return launch_paged_append(qkv, *cfg, page_shift_of(pool->page_size), pool->n_pages, k_pages, v_pages, slots, M, static_cast<hipStream_t>(hip_stream)) ==
+                   hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
+}
+
+lpq_status lpq_paged_attention(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* k_pages, const void* v_pages,
+                               const float* alibi_slopes, const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M, int32_t max_q,
+                               int32_t max_kv, void* out, void* hip_stream)
+{
+    if (!qkv || !cfg || !pool || !pool->table || !k_pages || !v_pages || !cu_q || !kv_lens || !out) return LPQ_ERR_NULL;
+    lpq_status s = check_heads(cfg, M);
+    if (s == LPQ_OK) s = check_pool(pool);
+    if (s == LPQ_OK) s = check_table(pool, n_seqs);
+    if (s != LPQ_OK) return s;
+    if (max_q < 1 || max_kv < 1) return LPQ_ERR_SHAPE;
+    if (misaligned(qkv) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out) || misaligned4(alibi_slopes) || misaligned4(cu_q) ||
+        misaligned4(kv_lens) || misaligned4(pool->table))
+        return LPQ_ERR_ALIGN;
+    return run_batch_attention(qkv, cfg, pool, k_pages, v_pages, alibi_slopes, cu_q, kv_lens, n_seqs, M, max_q, max_kv, out,
+                               static_cast<hipStream_t>(hip_stream));
+}
+
+lpq_status lpq_packed_attention(const void* qkv, const lpq_attn_cfg* cfg, const float* alibi_slopes, const int32_t* cu_q, int32_t n_seqs, int32_t M,
+                                int32_t max_q, void* out, void* hip_stream)
+{
+    if (!qkv || !cfg || !cu_q || !out) return LPQ_ERR_NULL;
+    const lpq_status s = check_heads(cfg, M);
+    if (s != LPQ_OK) return s;
+    if (n_seqs < 1 || n_seqs > PAGED_MAX_SEQS || max_q < 1) return LPQ_ERR_SHAPE;
+    if (misaligned(qkv) || misaligned(out) || misaligned4(alibi_slopes) || misaligned4(cu_q)) return LPQ_ERR_ALIGN;
+    return run_batch_attention(qkv, cfg, nullptr, nullptr, nullptr, alibi_slopes, cu_q, nullptr, n_seqs, M, max_q, std::min(max_q, M), out,
+                               static_cast<hipStream_t>(hip_stream));
 }
 
 size_t lpq_decoder_layer_workspace(const lpq_layer* layer, const lpq_layer_cfg* cfg, int32_t M)

@@ -205,5 +205,21 @@ hipError_t launch_attention_decode(const void* qkv, void* kc, void* vtc, const f
                                    int range, int splits, void* out, float* part, hipStream_t s);
 hipError_t launch_attention_prefill(const void* qkv, const void* kc, const void* vtc, const float* slopes, int n_seqs, int T, int pos0, int H, int d,
                                     int S, void* out, hipStream_t s);
+// paged caches and packed batches (lpq_paged.hip, lpq_paged_attention.hip); shift: log2 of the page size
+size_t paged_plan_workspace_bytes(int n_seqs, int M);
+hipError_t launch_paged_plan(const lpq_page_pool& pool, int shift, const int32_t* past, const int32_t* q_lens, int n_seqs, int M, const lpq_page_plan& out,
+                             void* ws, hipStream_t s);
+hipError_t launch_paged_append(const void* qkv, const lpq_attn_cfg& c, int shift, int n_pages, void* k_pages, void* v_pages, const int32_t* slots, int M,
+                               hipStream_t s);
+struct AttentionPlan {
+    int stream_tiles, workers;           // streaming kernel: column tiles of 16 rows (0: not launched), workgroups
+    bool tile;                           // tile kernel launched
+    int tiles, splits;                   // its virtual row tiles and K splits
+    size_t stream_floats, tile_floats;   // partial results of either (0: whole row tiles only)
+};
+AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int M, int max_q, int max_kv, int cus);
+hipError_t launch_batch_attention(const AttentionPlan& p, const lpq_attn_cfg& c, const void* qkv, const void* kp, const void* vp, const int32_t* table,
+                                  int shift, int n_pages, int max_pages, const int32_t* cu_q, const int32_t* kv_lens, const float* slopes, int n_seqs, int M,
+                                  void* out, float* part, hipStream_t s);
 
 }  // namespace lpq

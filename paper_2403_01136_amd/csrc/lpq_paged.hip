@@ -1,0 +1,247 @@
+// Paged caches: the plan of a step (block tables, slots and positions from the requests' lengths) and the append of its K and V to the
+// pages.  Both are bound by latency in a decode step; the append of long prompts is a copy at the memory's rate.
+#include <algorithm>
+
+#include "lpq_common.h"
+#include "lpq_device.h"
+#include "lpq_paged_index.h"
+
+namespace lpq {
+
+namespace {
+
+// ---- the plan ---------------------------------------------------------------------------------
+// With q = max(q_lens, 0), n = past + q, page size P and a table of W entries per sequence:
+//   offsets    cu[s] = sum of q before s, at most M
+//   owned      min(ceil(past / P), W);  need = ceil(n / P) - owned if q > 0
+//   starved    rows end behind M, n > W P, or need > 0 and the sum of the needs up to s exceeds the free pages
+// One workgroup: all of it hangs on three prefix sums over the sequences, which are a handful of numbers per thread; what is left is
+// a search (in LDS) per new page, returned page and row.  The lengths and the pool's counters may be updated in place: every thread has read what
+// it needs of them ahead of the first barrier.
+constexpr int PLAN_THREADS = 1024;
+constexpr uint32_t SUM_CAP = 1u << 30;                 // sums stop here: above any number of rows or pages that can be served
+
+__device__ __forceinline__ uint32_t capped_add(uint32_t a, uint32_t b) { return min(a + b, SUM_CAP); }
+
+// Exclusive prefix sums of v0 (sequence 2 t) and v1 (2 t + 1) over the workgroup, and the total.  part: a word per wave.
+struct Scan { uint32_t before, total; };
+__device__ __forceinline__ Scan block_scan(uint32_t v, uint32_t* part)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (blockDim.x + 63) >> 6;
+    uint32_t sum = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = (uint32_t)__shfl_up((int)sum, d);
+        if (lane >= d) sum = capped_add(sum, o);
+    }
+    const uint32_t prev = (uint32_t)__shfl_up((int)sum, 1);
+    Scan r{lane ? prev : 0u, 0u};
+    if (waves == 1) {
+        r.total = (uint32_t)__shfl((int)sum, 63);
+        return r;
+    }
+    if (lane == 63) part[wave] = sum;
+    __syncthreads();
+    uint32_t base = 0;
+    for (int w = 0; w < waves; ++w) {
+        const uint32_t p = part[w];
+        if (w < wave) base = capped_add(base, p);
+        r.total = capped_add(r.total, p);
+    }
+    r.before = capped_add(base, r.before);
+    return r;
+}
+
+// The last sequence whose prefix sum is at most i (prefix[0] is 0): of several with the same sum, the one that has elements.
+__device__ __forceinline__ int last_at_most(const uint32_t* prefix, int n, uint32_t i)
+{
+    int lo = 0, hi = n;                                // prefix[lo] <= i < prefix[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (prefix[mid] <= i) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ int ring_at(uint32_t at, int n_pages) { return at >= (uint32_t)n_pages ? (int)(at - n_pages) : (int)at; }
+
+struct PlanArgs {
+    const int32_t *past, *q_lens, *counters;
+    int32_t *table, *ring, *counters_out, *cu_q, *kv_lens, *slots, *positions, *info;
+    int32_t* base;                                     // [n] cached positions of a served sequence, -1 of a starved one; null: this launch does the rows
+    int32_t n, M, shift, n_pages, width;
+};
+
+__device__ __forceinline__ void write_row(const PlanArgs& a, int r, int page, int pos)
+{
+    const int id = page_checked(page, a.n_pages);
+    a.slots[r] = id < 0 ? -1 : (id << a.shift) + (pos & ((1 << a.shift) - 1));
+    a.positions[r] = pos;
+}
+__device__ __forceinline__ void write_no_row(const PlanArgs& a, int r)
+{
+    a.slots[r] = -1;
+    a.positions[r] = 0;
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void paged_plan_kernel(PlanArgs a)
+{
+    __shared__ uint32_t cu[PAGED_MAX_SEQS], need_before[PAGED_MAX_SEQS], back_before[PAGED_MAX_SEQS];
+    __shared__ int32_t base[PAGED_MAX_SEQS];
+    __shared__ uint32_t part[3][PLAN_THREADS / 64];
+    __shared__ uint32_t taken_s, starved_s;
+    const int tid = threadIdx.x, n = a.n, P = 1 << a.shift;
+    const int64_t room = (int64_t)a.width << a.shift;
+    if (tid == 0) taken_s = 0, starved_s = 0;
+    int head = a.counters[0], free_pages = a.counters[1];
+    free_pages = clamp_int(free_pages, 0, a.n_pages);
+    head = head < 0 ? 0 : head % a.n_pages;
+    int past[2], q[2], owned[2];
+    bool done[2];
+    uint32_t rows[2], back[2], need[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int s = 2 * tid + i;
+        past[i] = s < n ? max(a.past[s], 0) : 0;
+        const int ql = s < n ? a.q_lens[s] : 0;
+        done[i] = ql < 0;
+        q[i] = max(ql, 0);
+        owned[i] = (int)min<int64_t>(((int64_t)past[i] + P - 1) >> a.shift, a.width);
+        rows[i] = min((uint32_t)q[i], SUM_CAP);
+        back[i] = done[i] ? (uint32_t)owned[i] : 0u;
+    }
+    const Scan sr = block_scan(capped_add(rows[0], rows[1]), part[0]), sb = block_scan(capped_add(back[0], back[1]), part[1]);
+    bool late[2];
+    uint32_t before = sr.before;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int s = 2 * tid + i;
+        if (s < n) {
+            cu[s] = before;
+            back_before[s] = i ? capped_add(sb.before, back[0]) : sb.before;
+            a.cu_q[s] = (int)min(before, (uint32_t)a.M);
+        }
+        before = capped_add(before, rows[i]);
+        const int64_t total = (int64_t)past[i] + q[i];
+        late[i] = q[i] > 0 && (before > (uint32_t)a.M || total > room);
+        need[i] = q[i] > 0 && !late[i] ? (uint32_t)(((total + P - 1) >> a.shift) - owned[i]) : 0u;
+    }
+    const Scan sn = block_scan(capped_add(need[0], need[1]), part[2]);      // a barrier, if there is more than a wave: taken_s is zero
+    uint32_t sum = sn.before;
+    uint32_t n_starved = 0, most = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int s = 2 * tid + i;
+        if (s >= n) break;
+        need_before[s] = sum;
+        sum = capped_add(sum, need[i]);
+        const bool starved = late[i] || (need[i] > 0 && sum > (uint32_t)free_pages);
+        if (need[i] > 0 && !starved) most = sum;
+        n_starved += starved;
+        base[s] = starved ? -1 : past[i];
+        if (a.base) a.base[s] = base[s];
+        a.kv_lens[s] = done[i] ? 0 : starved ? past[i] : past[i] + q[i];
+    }
+    if (most) atomicMax(&taken_s, most);
+    if (n_starved) atomicAdd(&starved_s, n_starved);
+    __syncthreads();
+    const int taken = (int)taken_s, returned = (int)min(sb.total, (uint32_t)(a.n_pages - free_pages)), total_rows = (int)min(sr.total, (uint32_t)a.M);
+    if (tid == 0) {
+        a.cu_q[n] = total_rows;
+        a.counters_out[0] = ring_at((uint32_t)head + (uint32_t)taken, a.n_pages);
+        a.counters_out[1] = free_pages - taken + returned;
+        a.info[0] = total_rows;
+        a.info[1] = taken;
+        a.info[2] = returned;
+        a.info[3] = (int)starved_s;
+    }
+    for (int i = tid; i < taken; i += blockDim.x) {
+        const int s = last_at_most(need_before, n, (uint32_t)i);
+        const int e = ((base[s] + P - 1) >> a.shift) + (i - (int)need_before[s]);
+        a.table[(size_t)s * a.width + e] = a.ring[ring_at((uint32_t)head + (uint32_t)i, a.n_pages)];
+    }
+    // behind the free pages: no entry that is read here, as no more are returned than the ring has room for
+    for (int i = tid; i < returned; i += blockDim.x) {
+        const int s = last_at_most(back_before, n, (uint32_t)i);
+        const uint32_t at = (uint32_t)head + (uint32_t)free_pages;
+        a.ring[ring_at((uint32_t)ring_at(at, a.n_pages) + (uint32_t)i, a.n_pages)] = a.table[(size_t)s * a.width + (i - (int)back_before[s])];
+    }
+    if (a.base) return;
+    for (int r = tid; r < a.M; r += blockDim.x) {
+        const int s = r < total_rows ? last_at_most(cu, n, (uint32_t)r) : -1;
+        if (s < 0 || base[s] < 0) { write_no_row(a, r); continue; }
+        const int pos = base[s] + r - (int)cu[s], e = pos >> a.shift, held = (base[s] + P - 1) >> a.shift;
+        // a new page's entry may not be in the table yet: from the ring
+        write_row(a, r, e < held ? a.table[(size_t)s * a.width + e] : a.ring[ring_at((uint32_t)head + need_before[s] + (uint32_t)(e - held), a.n_pages)], pos);
+    }
+}
+
+// The rows of a long batch, behind the kernel above: the table is complete.
+constexpr int PLAN_ROWS_PER_WG = 1024;
+__global__ __launch_bounds__(256) void paged_plan_rows_kernel(PlanArgs a)
+{
+    __shared__ uint32_t cu[PAGED_MAX_SEQS];
+    __shared__ int32_t base[PAGED_MAX_SEQS];
+    for (int s = threadIdx.x; s < a.n; s += 256) cu[s] = (uint32_t)a.cu_q[s], base[s] = a.base[s];
+    const int total = a.cu_q[a.n];
+    __syncthreads();
+    const int end = min(a.M, (int)(blockIdx.x + 1) * PLAN_ROWS_PER_WG);
+    for (int r = (int)blockIdx.x * PLAN_ROWS_PER_WG + (int)threadIdx.x; r < end; r += 256) {
+        const int s = r < total ? last_at_most(cu, a.n, (uint32_t)r) : -1;
+        if (s < 0 || base[s] < 0) { write_no_row(a, r); continue; }
+        const int pos = base[s] + r - (int)cu[s];
+        write_row(a, r, a.table[(size_t)s * a.width + (pos >> a.shift)], pos);
+    }
+}
+
+// ---- the append: each row's K and V parts to its slot, 16 bytes a thread at a time ----------------
+// Rows without a slot are skipped.
+template <int D>
+__global__ __launch_bounds__(256) void paged_append_kernel(const uint16_t* __restrict__ qkv, uint16_t* __restrict__ kp, uint16_t* __restrict__ vp,
+                                                           const int32_t* __restrict__ slots, int M, int H, int KV, int shift, int n_pages)
+{
+    constexpr int CH = D / 8;                          // 16-byte chunks of a head
+    const int per_row = KV * CH, cols = (H + 2 * KV) * D;
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x, row = i / (uint32_t)per_row;      // below 2^31: the host's bound on M
+    if (row >= (uint32_t)M) return;
+    const int c = (int)(i - row * (uint32_t)per_row), h = c / CH;
+    const uint16_t* src = qkv + (size_t)row * cols + H * D + 8 * c;
+    const u32x4 k = *reinterpret_cast<const u32x4*>(src), v = *reinterpret_cast<const u32x4*>(src + KV * D);
+    const int slot = slot_checked(slots[row], n_pages, shift);
+    if (slot < 0) return;
+    const size_t at = (size_t)page_element(slot >> shift, h, KV, shift, D) + (size_t)(slot & ((1 << shift) - 1)) * D + 8 * (c % CH);
+    *reinterpret_cast<u32x4*>(kp + at) = k;
+    *reinterpret_cast<u32x4*>(vp + at) = v;
+}
+
+}  // namespace
+
+constexpr int PLAN_ONE_LAUNCH_ROWS = 4096;
+
+size_t paged_plan_workspace_bytes(int n_seqs, int M) { return M > PLAN_ONE_LAUNCH_ROWS ? (size_t)n_seqs * sizeof(int32_t) : 0; }
+
+hipError_t launch_paged_plan(const lpq_page_pool& pool, int shift, const int32_t* past, const int32_t* q_lens, int n_seqs, int M, const lpq_page_plan& out,
+                             void* ws, hipStream_t s)
+{
+    const PlanArgs a{past, q_lens, pool.counters, pool.table, pool.ring, out.counters, out.cu_q, out.kv_lens, out.slots, out.positions, out.info,
+                     static_cast<int32_t*>(ws), n_seqs, M, shift, pool.n_pages, pool.max_pages};
+    // threads for the sequences (two each) and, up to eight waves, for the rows
+    const int want = std::max((n_seqs + 1) / 2, std::min(ws ? 0 : M, 512));
+    paged_plan_kernel<<<1, std::min(PLAN_THREADS, (want + 63) / 64 * 64), 0, s>>>(a);
+    if (ws) paged_plan_rows_kernel<<<(unsigned)((M + PLAN_ROWS_PER_WG - 1) / PLAN_ROWS_PER_WG), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_append(const void* qkv, const lpq_attn_cfg& c, int shift, int n_pages, void* k_pages, void* v_pages, const int32_t* slots, int M,
+                               hipStream_t s)
+{
+    const uint16_t* q = static_cast<const uint16_t*>(qkv);
+    uint16_t *k = static_cast<uint16_t*>(k_pages), *v = static_cast<uint16_t*>(v_pages);
+    const int64_t chunks = (int64_t)M * c.n_kv_heads * (c.head_dim / 8);
+    const unsigned grid = (unsigned)((chunks + 255) / 256);
+    if (c.head_dim == 128) paged_append_kernel<128><<<grid, 256, 0, s>>>(q, k, v, slots, M, c.n_heads, c.n_kv_heads, shift, n_pages);
+    else                   paged_append_kernel<64><<<grid, 256, 0, s>>>(q, k, v, slots, M, c.n_heads, c.n_kv_heads, shift, n_pages);
+    return hipGetLastError();
+}
+
+}  // namespace lpq

@@ -1,0 +1,987 @@
+// Causal attention of new tokens of many sequences at once, over paged caches or over the packed rows themselves, with any number of query
+// heads per K/V head:
+//     out[row] = sum_j w_j v_j / sum_j w_j,   w_j = exp(q . k_j / sqrt(D) + slope (j - p)),   j <= p, p the row's position
+// and zero where no key is visible.  The rows of a sequence and K/V head are its new tokens times the head's `group` query heads, row = token * group +
+// g: all of them read the same keys, so a tile of rows is one product whatever the layout, and the diagonal of a group is narrow.
+//
+// Two kernels.  The streaming kernel (few rows per sequence: decode) reads the pages once, straight into registers, as fast as the memory gives them.
+// The tile kernel (prompts and chunks) shares tiles of keys through LDS between 128 rows and is bound by the matrix and vector units.
+// Both keep a running maximum and sum per row in fp32 and take exponents to base 2; weights are rounded to the inputs' type for the matrix units
+// (the sum is of the unrounded ones).
+//
+// Keys that no row may see (behind the sequence's end, pages that are not in the pool) are read from page 0 or a stale page, their scores are replaced and
+// their values set to zero.  A later token's value row stays in the products at weight zero, and is finite; where it is not, the sums that it has
+// spoilt are formed again by row_walk, over the visible keys and no others.
+#include <algorithm>
+#include <type_traits>
+
+#include "lpq_common.h"
+#include "lpq_device.h"
+#include "lpq_lanes.h"
+#include "lpq_paged_index.h"
+
+namespace lpq {
+
+namespace {
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int DT> struct Elem;
+template <> struct Elem<LPQ_DT_FP16> {
+    typedef _Float16 t;
+    typedef h8 v8;
+    static __device__ __forceinline__ f16x mfma32(v8 a, v8 b, f16x c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f4 mfma16(v8 a, v8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { const h2 p = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, p); }
+};
+template <> struct Elem<LPQ_DT_BF16> {
+    typedef __bf16 t;
+    typedef bf8 v8;
+    static __device__ __forceinline__ f16x mfma32(v8 a, v8 b, f16x c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f4 mfma16(v8 a, v8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { const bf2 p = {(__bf16)a, (__bf16)b}; return __builtin_bit_cast(uint32_t, p); }
+};
+
+// What a launch is about.  Pointers are to 16-bit elements.
+struct AttnArgs {
+    const uint16_t* qkv;                 // [M][(heads + 2 kv_heads) * D]
+    const uint16_t *kp, *vp;             // pages; null: keys are the rows themselves
+    const int32_t *table, *cu_q, *kv_lens;
+    const float* slopes;
+    uint16_t* out;                       // [M][heads * D]
+    float* part;                         // partial results, or null: nothing is split
+    int32_t n_seqs, M, heads, kv_heads, group, shift, n_pages, max_pages;
+    int32_t rows_from, rows_to;          // sequences with rows_from <= rows < rows_to are this launch's
+    int32_t workers, splits, tiles;      // streaming: workgroups; tile kernel: K splits, virtual row tiles
+};
+
+// A sequence as a kernel sees it.
+struct Seq {
+    int s, first, len, rows;             // rows of the batch [first, first + len); rows = len * group
+    int pos0, ctx;                       // position of its first new token; keys that exist
+};
+__device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s)
+{
+    const RowSpan r = row_span(a.cu_q[s], a.cu_q[s + 1], a.M);
+    Seq q;
+    q.s = s;
+    q.first = r.first;
+    q.len = r.end - r.first;
+    q.rows = q.len * a.group;
+    const int kv = a.kv_lens ? a.kv_lens[s] : q.len;
+    q.pos0 = token_position(kv, q.len, 0);
+    q.ctx = a.kv_lens ? keys_of(kv, a.max_pages, a.shift) : q.len;
+    return q;
+}
+__device__ __forceinline__ bool takes(const AttnArgs& a, int rows) { return rows > 0 && rows >= a.rows_from && rows < a.rows_to; }
+
+__device__ __forceinline__ int page_of_group(const AttnArgs& a, int s, int g)
+{
+    const int e = page_entry(g, a.shift, a.max_pages);
+    return e < 0 ? -1 : page_checked(a.table[(size_t)s * a.max_pages + e], a.n_pages);
+}
+
+// One row by one wave, on the vector units, over the visible keys of [k0, k1) and no others: lanes along the keys for the scores, along the features for
+// the sums.  For rows whose sums came out not finite (see above); the same scaling, exponents and rounding of the weights.
+template <int DT, int D>
+__device__ __forceinline__ void row_walk(const AttnArgs& a, const Seq& q, int h, const uint16_t* qp, int p, float slope, int k0, int k1,
+                                         float& m, float& l, float (&acc)[D / 64])
+{
+    typedef typename Elem<DT>::t T;
+    typedef typename Elem<DT>::v8 V8;
+    const int lane = threadIdx.x & 63, cols = (a.heads + 2 * a.kv_heads) * D;
+    const float c = LOG2E / sqrtf((float)D);
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) acc[i] = 0.0f;
+    k1 = min(k1, min(p + 1, q.ctx));
+    auto key_row = [&](int j, bool v) -> const uint16_t* {                       // null: not there
+        if (!a.kp) return a.qkv + (size_t)(q.first + j) * cols + (a.heads + (v ? a.kv_heads : 0) + h) * D;
+        const int page = page_of_group(a, q.s, j >> 4);
+        if (page < 0) return nullptr;
+        return (v ? a.vp : a.kp) + page_element(page, h, a.kv_heads, a.shift, D) + (size_t)(j & ((1 << a.shift) - 1)) * D;
+    };
+#pragma unroll 1
+    for (int j0 = k0; j0 < k1; j0 += 64) {
+        const int j = j0 + lane;
+        const uint16_t* kr = j < k1 ? key_row(j, false) : nullptr;
+        float sc = -INFINITY;
+        if (kr) {
+            float d = 0.0f;
+#pragma unroll 1
+            for (int f = 0; f < D; f += 8) {
+                const V8 x = *reinterpret_cast<const V8*>(qp + f), k = *reinterpret_cast<const V8*>(kr + f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d += (float)x[e] * (float)k[e];
+            }
+            sc = __builtin_fmaf(d, c, slope * (float)(j - p));
+        }
+        const float mn = fmaxf(m, group_reduce<64>(sc, OpMax())), ms = mn == -INFINITY ? 0.0f : mn;
+        const float alpha = __builtin_amdgcn_exp2f(m - ms), w = kr ? __builtin_amdgcn_exp2f(sc - ms) : 0.0f;
+        m = mn;
+        l = l * alpha + w;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) acc[i] *= alpha;
+        const int n = min(64, k1 - j0);
+#pragma unroll 1
+        for (int u = 0; u < n; ++u) {
+            const uint16_t* vr = key_row(j0 + u, true);
+            const float wu = (float)(T)__shfl(w, u);
+            if (!vr) continue;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) acc[i] = __builtin_fmaf(wu, (float)__builtin_bit_cast(T, vr[64 * i + lane]), acc[i]);
+        }
+    }
+    l = group_reduce<64>(l, OpAdd());
+}
+
+// ---- streaming kernel ---------------------------------------------------------------------------
+// Bound by the memory: 4 D bytes per key and K/V head.  A persistent launch; the units of 128 keys of all (sequence, head, row tile) are one list, cut into
+// equal shares, so contexts of any lengths fill the chip evenly.  A wave takes every fourth 32 keys of its workgroup's range, keeps the
+// next 32 under way in registers (16 KB per wave at D = 128) and meets the other waves only where a row tile ends.
+//
+// Products on 16x16x32 matrix instructions, columns = rows of the problem (16 per column tile), so that scores land where the weights are wanted:
+//   S^T = K . Q^T    A = K: lane (i = lane % 16, q = lane / 16) holds key i, features 32 step + 8 q + 0..7, loaded as they lie;
+//                    register r of the result: key 4 q + r, column i.
+//   O^T = V^T . P^T  over 32 keys: lane quarter q contracts over keys {4 q + 0..3, 16 + 4 q + 0..3}: its own scores of the two key tiles, so
+//                    the weights go from result to operand in place.  V is read in whole rows (lane i: features F i .. F i + F - 1, F = D / 16, of the quarter's
+//                    eight keys); V^T operand e, features F i + e, is one v_perm per register, no LDS.  Register r of result e: feature F (4 q + r) + e.
+// A range's cut row tiles leave (unnormalised sums, maximum, sum) in two slots per workgroup, added up by stream_combine_kernel in the order of the keys.
+template <int DT, int D, int NT> struct StreamSmem {
+    float o[4][STREAM_ROWS][D + 4];      // one column tile at a time
+    float m[4][STREAM_ROWS * NT], l[4][STREAM_ROWS * NT];
+    uint64_t scan[4];
+    int64_t begin;                       // the worker's first unit's sequence: units before it
+    int seq;
+    uint32_t again;
+};
+
+__device__ __forceinline__ int64_t seq_units(const AttnArgs& a, int s, int tile_rows)
+{
+    if (s >= a.n_seqs) return 0;
+    const Seq q = load_seq(a, s);
+    return takes(a, q.rows) ? (int64_t)a.kv_heads * stream_row_tiles(q.rows, tile_rows) * stream_key_blocks(q.ctx) : 0;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t shfl64(int64_t v, int from)
+{
+    const int lo = __shfl((int)(uint32_t)v, from), hi = __shfl((int)(v >> 32), from);
+    return (int64_t)(uint32_t)lo | (int64_t)hi << 32;
+}
+__device__ __forceinline__ int64_t scan64(int64_t v)                              // inclusive, over the wave
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t o = shfl64(v, lane - d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+// Total of the launch's units, by a workgroup of 256; scan: a word per wave.
+__device__ __forceinline__ int64_t units_total(const AttnArgs& a, int tile_rows, uint64_t* scan)
+{
+    int64_t v = 0;
+    for (int s = threadIdx.x; s < a.n_seqs; s += 256) v += seq_units(a, s, tile_rows);
+    v = shfl64(scan64(v), 63);
+    if ((threadIdx.x & 63) == 0) scan[threadIdx.x >> 6] = (uint64_t)v;
+    __syncthreads();
+    const int64_t total = (int64_t)(scan[0] + scan[1] + scan[2] + scan[3]);
+    __syncthreads();
+    return uniform64(total);
+}
+// The sequence that has unit u, and the units before it, into *seq and *begin (LDS).
+__device__ __forceinline__ void units_find(const AttnArgs& a, int tile_rows, int64_t u, uint64_t* scan, int* seq, int64_t* begin)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t carry = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 256) {
+        const int64_t mine = seq_units(a, s0 + (int)threadIdx.x, tile_rows), sum = scan64(mine);
+        if (lane == 63) scan[wave] = (uint64_t)sum;
+        __syncthreads();
+        int64_t before = carry + sum - mine;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) before += (int64_t)scan[w];
+            carry += (int64_t)scan[w];
+        }
+        if (u >= before && u < before + mine) *seq = s0 + (int)threadIdx.x, *begin = before;
+        __syncthreads();
+    }
+}
+
+// A row tile of a sequence and head, and the units that it has.
+struct Segment {
+    Seq q;
+    int h, rt, blocks;
+    int64_t first;                       // its first unit
+};
+__device__ __forceinline__ Segment segment_of(const AttnArgs& a, int s, int64_t seq_begin, int64_t u, int tile_rows)
+{
+    Segment g;
+    g.q = load_seq(a, s);
+    g.blocks = stream_key_blocks(g.q.ctx);
+    const int tiles = stream_row_tiles(g.q.rows, tile_rows);
+    const int64_t at = u - seq_begin;
+    const int64_t t = at >> 31 ? at / g.blocks : (int64_t)((uint32_t)at / (uint32_t)g.blocks);
+    g.h = tiles == 1 ? (int)t : (int)(t / tiles);
+    g.rt = tiles == 1 ? 0 : (int)(t % tiles);
+    g.first = seq_begin + t * g.blocks;
+    return g;
+}
+
+template <int DT, int D, int NT, bool ALIBI>
+__global__ __launch_bounds__(256, 2) void stream_attention_kernel(AttnArgs a)
+{
+    typedef typename Elem<DT>::v8 V8;
+    constexpr int KJ = D / 32, F = D / 16, TILE_ROWS = STREAM_ROWS * NT;         // feature steps of S^T; features of a lane's V chunk
+    constexpr int SLOT = TILE_ROWS * (D + 2);
+    typedef uint32_t vchunk __attribute__((ext_vector_type(F / 2)));
+    __shared__ __attribute__((aligned(16))) StreamSmem<DT, D, NT> sm;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    const float c = LOG2E / sqrtf((float)D);
+    const int cols = (a.heads + 2 * a.kv_heads) * D;
+
+    const int64_t units = units_total(a, TILE_ROWS, sm.scan);
+    const int W = (int)min<int64_t>(a.workers, units), w = blockIdx.x;
+    if (w >= W) return;
+    int64_t u = stream_begin(units, w, W);
+    const int64_t u_end = stream_begin(units, w + 1, W), u_begin = u;
+    units_find(a, TILE_ROWS, u, sm.scan, &sm.seq, &sm.begin);
+    int s = __builtin_amdgcn_readfirstlane(sm.seq);
+    int64_t s_begin = uniform64(sm.begin), s_units = seq_units(a, s, TILE_ROWS);
+
+    while (u < u_end) {
+        while (u >= s_begin + s_units) {               // the next sequence with units: there is one, u is below the total
+            s_begin += s_units;
+            s_units = seq_units(a, ++s, TILE_ROWS);
+        }
+        const Segment g = segment_of(a, s, s_begin, u, TILE_ROWS);
+        const Seq q = g.q;
+        if (!a.part && g.first < u) {                  // nowhere to leave parts: a worker takes the row tiles that begin in its range, whole
+            u = g.first + g.blocks;
+            continue;
+        }
+        const int b0 = (int)(u - g.first), b1 = a.part ? (int)min<int64_t>(g.blocks, u_end - g.first) : g.blocks;
+        const int row0 = g.rt * TILE_ROWS, n_rows = min(TILE_ROWS, q.rows - row0);
+        const int t_first = row0 / a.group, t_last = (row0 + n_rows - 1) / a.group;
+        const int key_end = min(q.ctx, q.pos0 + t_last + 1);                     // no row sees a key from here on (may be below 1)
+        const int all_see = q.pos0 + t_first + 1;                               // every row sees the keys below
+
+        // the lane's column(s): query row, position, slope
+        V8 qf[NT][KJ];
+        int p[NT];
+        float slope[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int r = row0 + min(STREAM_ROWS * t + col, n_rows - 1), tok = r / a.group, head = g.h * a.group + r % a.group;
+            const uint16_t* qp = a.qkv + (size_t)(q.first + tok) * cols + head * D + 8 * quarter;
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) qf[t][j] = *reinterpret_cast<const V8*>(qp + 32 * j);
+            p[t] = q.pos0 + tok;
+            slope[t] = ALIBI ? a.slopes[head] * LOG2E : 0.0f;
+        }
+        float m[NT], l[NT];
+        f4 o[NT][F];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            m[t] = -INFINITY;
+            l[t] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < F; ++e) o[t][e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+        // pages: lane 2 n + i holds the page of 16-key group i of step n, counted from step n0, 32 steps at a time
+        const int steps = max(0, min(b1 - b0, (key_end - 32 * wave - STREAM_BLOCK * b0 + STREAM_BLOCK - 1) / STREAM_BLOCK));       // of this wave
+        int ids = 0;
+        auto load_ids = [&](int n0) {
+            const int n = n0 + lane / 2;
+            ids = n < steps ? page_of_group(a, q.s, (STREAM_BLOCK / 16) * (b0 + n) + 2 * wave + (lane & 1)) : -1;
+        };
+        const uint32_t koff = (uint32_t)(col * D + 8 * quarter) * 2u, voff = (uint32_t)(4 * quarter * D + F * col) * 2u;
+        V8 kf[2][2][KJ];
+        vchunk vf[2][2][4];
+        auto load = [&](int n, int x) {
+            const int key0 = STREAM_BLOCK * (b0 + n) + 32 * wave;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int id = max(__builtin_amdgcn_readlane(ids, 2 * (n & 31) + i), 0);
+                const size_t at = (size_t)page_element(id, g.h, a.kv_heads, a.shift, D) + (size_t)((key0 + 16 * i) & ((1 << a.shift) - 1)) * D;
+                const uint8_t *kb = reinterpret_cast<const uint8_t*>(a.kp + at), *vb = reinterpret_cast<const uint8_t*>(a.vp + at);
+#pragma unroll
+                for (int j = 0; j < KJ; ++j) kf[x][i][j] = __builtin_nontemporal_load(reinterpret_cast<const V8*>(kb + koff + 64 * j));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vf[x][i][r] = __builtin_nontemporal_load(reinterpret_cast<const vchunk*>(vb + voff + 2 * D * r));
+            }
+        };
+        auto compute = [&](int n, int x, uint32_t bad) {       // bad: bit i set: 16-key group i has no page
+            const int key0 = STREAM_BLOCK * (b0 + n) + 32 * wave;
+            const bool plain = bad == 0 && key0 + 32 <= min(all_see, key_end);
+            if (!plain)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if ((bad >> i & 1) || key0 + 16 * i + 4 * quarter + r >= key_end) vf[x][i][r] = vchunk{};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                f4 sc[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    sc[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < KJ; ++j) sc[i] = Elem<DT>::mfma16(kf[x][i][j], qf[t][j], sc[i]);
+                }
+                float mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int key = key0 + 16 * i + 4 * quarter + r;
+                        float v = sc[i][r] * c;
+                        if constexpr (ALIBI) v = __builtin_fmaf(slope[t], (float)(key - p[t]), v);
+                        if (!plain) v = (bad >> i & 1) || key > p[t] || key >= key_end ? -INFINITY : v;
+                        sc[i][r] = v;
+                        mx = fmaxf(mx, v);
+                    }
+                f2 z = both_rows(mx);
+                z = both_halves(fmaxf(z[0], z[1]));
+                const float mn = fmaxf(m[t], fmaxf(z[0], z[1])), ms = mn == -INFINITY ? 0.0f : mn;
+                if (__any(mn > m[t])) {
+                    const float alpha = __builtin_amdgcn_exp2f(m[t] - ms);
+                    l[t] *= alpha;
+#pragma unroll
+                    for (int e = 0; e < F; ++e) o[t][e] *= alpha;
+                    m[t] = mn;
+                }
+                u32x4 pk;
+                float ls = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; r += 2) {
+                        const float e0 = __builtin_amdgcn_exp2f(sc[i][r] - ms), e1 = __builtin_amdgcn_exp2f(sc[i][r + 1] - ms);
+                        ls += e0 + e1;
+                        pk[2 * i + r / 2] = Elem<DT>::pack(e0, e1);
+                    }
+                l[t] += ls;
+                const V8 pf = __builtin_bit_cast(V8, pk);
+#pragma unroll
+                for (int e = 0; e < F; ++e) {
+                    u32x4 vt;                          // element e of the lane's chunks of the quarter's eight keys
+                    const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; r += 2) vt[2 * i + r / 2] = __builtin_amdgcn_perm(vf[x][i][r + 1][e / 2], vf[x][i][r][e / 2], sel);
+                    o[t][e] = Elem<DT>::mfma16(__builtin_bit_cast(V8, vt), pf, o[t][e]);
+                }
+            }
+        };
+        uint64_t bad_ids = 0;
+        if (steps > 0) {
+            load_ids(0);
+            bad_ids = __ballot(ids < 0);
+            load(0, 0);
+        }
+        for (int n = 0; n < steps; n += 2) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {              // buffers by name
+                const int k = n + x;
+                if (k >= steps) break;
+                const uint32_t bad = (uint32_t)(bad_ids >> (2 * (k & 31))) & 3u;
+                if (k + 1 < steps) {
+                    if (((k + 1) & 31) == 0) {
+                        load_ids(k + 1);
+                        bad_ids = __ballot(ids < 0);
+                    }
+                    load(k + 1, x ^ 1);
+                }
+                compute(k, x, bad);
+            }
+        }
+
+        // the four waves' sums, a column tile at a time
+        const bool whole = b0 == 0 && b1 == g.blocks;
+        float* slot = a.part + (size_t)(2 * w + (g.first < u_begin ? 0 : 1)) * SLOT;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            f2 z = both_rows(l[t]);
+            z = both_halves(z[0] + z[1]);
+            if (quarter == 0) {
+                sm.m[wave][STREAM_ROWS * t + col] = m[t];
+                sm.l[wave][STREAM_ROWS * t + col] = z[0] + z[1];
+            }
+        }
+        if (tid == 0) sm.again = 0;
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (STREAM_ROWS * t >= n_rows) break;
+            const int cc = STREAM_ROWS * t + col;
+            const float mt = fmaxf(fmaxf(sm.m[0][cc], sm.m[1][cc]), fmaxf(sm.m[2][cc], sm.m[3][cc])), ms = mt == -INFINITY ? 0.0f : mt;
+            const float scale = __builtin_amdgcn_exp2f(m[t] - ms);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < F; e += 4) {
+                    const f4 v = {o[t][e][r] * scale, o[t][e + 1][r] * scale, o[t][e + 2][r] * scale, o[t][e + 3][r] * scale};
+                    *reinterpret_cast<f4*>(&sm.o[wave][col][F * (4 * quarter + r) + e]) = v;
+                }
+            __syncthreads();
+            // thread: row tid / 16, features F (tid % 16) ..
+            const int rr = tid >> 4, f0 = F * (tid & 15), ri = STREAM_ROWS * t + rr;
+            const float m0 = sm.m[0][ri], m1 = sm.m[1][ri], m2 = sm.m[2][ri], m3 = sm.m[3][ri];
+            float M2 = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+            const float Ms = M2 == -INFINITY ? 0.0f : M2;
+            float L = sm.l[0][ri] * __builtin_amdgcn_exp2f(m0 - Ms) + sm.l[1][ri] * __builtin_amdgcn_exp2f(m1 - Ms) +
+                      sm.l[2][ri] * __builtin_amdgcn_exp2f(m2 - Ms) + sm.l[3][ri] * __builtin_amdgcn_exp2f(m3 - Ms);
+            float v[F];
+            float total = 0.0f;
+#pragma unroll
+            for (int e = 0; e < F; ++e) {
+                v[e] = (sm.o[0][rr][f0 + e] + sm.o[1][rr][f0 + e]) + (sm.o[2][rr][f0 + e] + sm.o[3][rr][f0 + e]);
+                total += v[e];
+            }
+            if (q.len > 1) {                           // a later token's row may have spoilt the sums of an earlier one
+                if (ri < n_rows && !__builtin_isfinite(total)) atomicOr(&sm.again, 1u << rr);
+                __syncthreads();
+                uint32_t again = sm.again;
+                __syncthreads();
+                if (again) {
+                    for (uint32_t left = again; left; left &= left - 1) {
+                        const int k = __builtin_ctz(left), r = row0 + STREAM_ROWS * t + k, tok = r / a.group, head = g.h * a.group + r % a.group;
+                        if (k % 4 != wave) continue;
+                        float wm, wl, acc[D / 64];
+                        row_walk<DT, D>(a, q, g.h, a.qkv + (size_t)(q.first + tok) * cols + head * D, q.pos0 + tok, ALIBI ? a.slopes[head] * LOG2E : 0.0f,
+                                        STREAM_BLOCK * b0, STREAM_BLOCK * b1, wm, wl, acc);
+#pragma unroll
+                        for (int i = 0; i < D / 64; ++i) sm.o[0][k][64 * i + lane] = acc[i];
+                        if (lane == 0) sm.m[0][STREAM_ROWS * t + k] = wm, sm.l[0][STREAM_ROWS * t + k] = wl;
+                    }
+                    __syncthreads();
+                    if (again >> rr & 1) {
+                        M2 = sm.m[0][ri];
+                        L = sm.l[0][ri];
+#pragma unroll
+                        for (int e = 0; e < F; ++e) v[e] = sm.o[0][rr][f0 + e];
+                    }
+                    if (tid == 0) sm.again = 0;
+                }
+            }
+            if (ri < n_rows) {
+                if (whole) {
+                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+                    const int r = row0 + ri, tok = r / a.group, head = g.h * a.group + r % a.group;
+                    vchunk x;
+#pragma unroll
+                    for (int e = 0; e < F; e += 2) x[e / 2] = Elem<DT>::pack(v[e] * inv, v[e + 1] * inv);
+                    *reinterpret_cast<vchunk*>(a.out + (size_t)(q.first + tok) * a.heads * D + head * D + f0) = x;
+                } else {
+                    float* ps = slot + (size_t)ri * (D + 2);
+#pragma unroll
+                    for (int e = 0; e < F; e += 2) *reinterpret_cast<f2*>(ps + f0 + e) = f2{v[e], v[e + 1]};
+                    if (f0 == 0) *reinterpret_cast<f2*>(ps + D) = f2{M2, L};
+                }
+            }
+            __syncthreads();                           // before the next column tile's, or segment's, sums
+        }
+        u = g.first + b1;
+    }
+}
+
+// Adds up the parts of the row tile that begins in worker blockIdx.x's range and goes on behind it, if there is one; a row per blockIdx.y.
+template <int DT, int D, int NT>
+__global__ __launch_bounds__(256) void stream_combine_kernel(AttnArgs a)
+{
+    constexpr int TILE_ROWS = STREAM_ROWS * NT, SLOT = TILE_ROWS * (D + 2);
+    __shared__ uint64_t scan[4];
+    __shared__ int64_t begin_s;
+    __shared__ int seq_s;
+    __shared__ float red[256 / D][D + 2];
+    const int64_t units = units_total(a, TILE_ROWS, scan);
+    const int W = (int)min<int64_t>(a.workers, units), w = blockIdx.x;
+    if (w >= W) return;
+    const int64_t u0 = stream_begin(units, w, W), u1 = stream_begin(units, w + 1, W);
+    units_find(a, TILE_ROWS, u1 - 1, scan, &seq_s, &begin_s);
+    const Segment g = segment_of(a, seq_s, begin_s, u1 - 1, TILE_ROWS);
+    if (g.first < u0 || g.first + g.blocks <= u1) return;
+    const int row0 = g.rt * TILE_ROWS, ri = blockIdx.y;
+    if (ri >= min(TILE_ROWS, g.q.rows - row0)) return;
+    const int last = stream_worker(units, g.first + g.blocks - 1, W);
+    // part k: worker w + k; the first is in its slot 1, the others, which begin inside the row tile, in their slot 0
+    auto part = [&](int k) { return a.part + (size_t)(2 * (w + k) + (k == 0 ? 1 : 0)) * SLOT + (size_t)ri * (D + 2); };
+    const int parts = last - w + 1, f = threadIdx.x % D, lane_part = threadIdx.x / D;
+    float m = -INFINITY, l = 0.0f, v = 0.0f;
+    for (int k = lane_part; k < parts; k += 256 / D) {
+        const float* ps = part(k);
+        const f2 ml = *reinterpret_cast<const f2*>(ps + D);
+        const float mn = fmaxf(m, ml[0]), ms = mn == -INFINITY ? 0.0f : mn, x = __builtin_amdgcn_exp2f(m - ms), y = __builtin_amdgcn_exp2f(ml[0] - ms);
+        m = mn;
+        l = l * x + ml[1] * y;
+        v = v * x + ps[f] * y;
+    }
+    red[lane_part][f] = v;
+    if (f == 0) red[lane_part][D] = m, red[lane_part][D + 1] = l;
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 256 / D; ++k) mt = fmaxf(mt, red[k][D]);
+    const float ms = mt == -INFINITY ? 0.0f : mt;
+    float num = 0.0f, den = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 256 / D; ++k) {
+        const float y = __builtin_amdgcn_exp2f(red[k][D] - ms);
+        num += y * red[k][f];
+        den += y * red[k][D + 1];
+    }
+    const int r = row0 + ri, tok = r / a.group, head = g.h * a.group + r % a.group;
+    const uint32_t x = Elem<DT>::pack(num * (den == 0.0f ? 0.0f : 1.0f / den), 0.0f);
+    a.out[(size_t)(g.q.first + tok) * a.heads * D + head * D + f] = (uint16_t)x;
+}
+
+// ---- tile kernel ----------------------------------------------------------------------------------
+// Bound by the matrix and vector units together.  A workgroup takes 128 rows (token, head of the group) of one sequence and K/V head, each of its four
+// waves 32 of them, and walks the visible keys 64 at a time; K and V tiles are shared through LDS (two buffers each, filled by global-to-LDS loads
+// while the tile before is multiplied; 64 KB at D = 128, two workgroups per compute unit).
+// Both products are transposed, on 32x32x16: S^T = K . Q^T, O^T = V^T . P^T; a lane holds scores of one row (column lane % 32), so the softmax needs
+// one exchange between the halves of the wave.  Register v of a score tile is key 8 (v / 4) + 4 half + v % 4; registers 8 c .. 8 c + 7 of a lane go as they are
+// into the weights' operand of 16-key step c, which contracts half h over keys {4 h + 0..3, 8 + 4 h + 0..3}.  V^T operands in that order are read from row-major
+// tiles by the transposing LDS read: each 16 lanes fetch four keys x 16 features and lane i gets feature i of the four.
+// 16-byte chunks are swizzled: K's by the row (16 lanes read 16 rows), V's by the row modulo 4 in steps of four chunks (32 lanes read four rows x 64 bytes).
+// Workgroup ids go round-robin over the 8 XCDs; a head of keys, or a class of row tiles of it where there are fewer than eight, stays on one of them.
+template <int D> __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
+
+constexpr int LEAST_KEY_TILES = 4;       // of a split
+constexpr float LAZY = 8.0f;             // a row's maximum is renewed once it has grown by 2^8: its sums are then at most 2^8 larger, and the weights exact all the same
+
+// The sequence of virtual tile v, or -1.  Every wave for itself: two rounds of 64 candidates.
+__device__ __forceinline__ int tile_sequence(const AttnArgs& a, int v)
+{
+    const int lane = threadIdx.x & 63, stride = (a.n_seqs + 63) / 64;
+    auto begins = [&](int s) { return s < a.n_seqs && tile_start(clamp_int(a.cu_q[s], 0, a.M), a.group, s) <= v; };
+    const int block = __popcll(__ballot(begins(lane * stride))) - 1;
+    if (block < 0 || stride == 1) return block;
+    return block * stride + __popcll(__ballot(lane < stride && begins(block * stride + lane))) - 1;
+}
+
+// What a workgroup of the tile kernel, or of its combining kernel, is about.
+struct Tile { Seq q; int row0, n_rows, key_end, key_tiles; };
+__device__ __forceinline__ bool tile_of(const AttnArgs& a, int v, Tile* t)
+{
+    const int s = __builtin_amdgcn_readfirstlane(tile_sequence(a, v));
+    if (s < 0) return false;
+    t->q = load_seq(a, s);
+    t->row0 = TILE_ROWS_Q * (v - tile_start(t->q.first, a.group, s));
+    if (!takes(a, t->q.rows) || t->row0 < 0 || t->row0 >= t->q.rows) return false;
+    t->n_rows = min((int)TILE_ROWS_Q, t->q.rows - t->row0);
+    t->key_end = max(0, min(t->q.ctx, t->q.pos0 + (t->row0 + t->n_rows - 1) / a.group + 1));
+    t->key_tiles = max(1, (t->key_end + TILE_KEYS - 1) / TILE_KEYS);
+    return true;
+}
+
+template <int DT, int D, bool ALIBI, bool PAGED>
+__global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
+{
+    typedef typename Elem<DT>::v8 V8;
+    constexpr int CH = D / 8, KS = D / 16, DTL = D / 32, ROWS = 512 / D, FILLS = 16 / ROWS;       // chunks of a row; feature steps; feature tiles; keys per load; loads of a wave's 16 keys
+    constexpr int TILE_BYTES = TILE_KEYS * D * 2;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];          // K, K, V, V (dynamic: ahead of a read of a named array the compiler waits for every load into it)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+    // (head, row tile, split) of this workgroup
+    const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
+    const int per_xcd = a.kv_heads * classes / 8, per_class = (a.tiles + classes - 1) / classes;
+    const int slot = (int)(blockIdx.x >> 3), combo = (int)(blockIdx.x & 7) + 8 * (slot % per_xcd), rest = slot / per_xcd;
+    const int h = combo % a.kv_heads, split = rest / per_class;
+    const int v = a.tiles - 1 - ((rest % per_class) * classes + combo / a.kv_heads);
+    if (v < 0) return;
+    Tile tl;
+    if (!tile_of(a, v, &tl)) return;
+    const Seq q = tl.q;
+    const KeySplit ks = key_split(tl.key_tiles, a.splits, LEAST_KEY_TILES, split);
+    if (split >= ks.used) return;
+    const int cols = (a.heads + 2 * a.kv_heads) * D;
+    const int wr0 = 32 * wave;                                                  // this wave's first row of the tile
+    const bool active = wr0 < tl.n_rows;
+    const int r = tl.row0 + min(wr0 + col, tl.n_rows - 1), tok = r / a.group, head = h * a.group + r % a.group, p = q.pos0 + tok;
+    const float c = LOG2E / sqrtf((float)D);
+    const float slope = ALIBI ? a.slopes[head] * LOG2E : 0.0f;
+    const int all_see = min(tl.key_end, q.pos0 + (tl.row0 + min(wr0, tl.n_rows - 1)) / a.group + 1);        // keys below: every row of the wave sees them
+    const int my_end = active ? min(ks.end, (max(0, min(q.ctx, q.pos0 + (tl.row0 + min(wr0 + 31, tl.n_rows - 1)) / a.group + 1)) + TILE_KEYS - 1) / TILE_KEYS) : 0;
+
+    // fills: this wave brings keys 16 wave .. 16 wave + 15 of a tile, of one page
+    int ids = 0, ids_from = ks.begin;
+    uint64_t bad_ids = 0;
+    auto load_ids = [&](int j) {
+        ids_from = j;
+        const int g = 4 * j + lane;
+        ids = 16 * g < tl.key_end ? page_of_group(a, q.s, g) : -1;
+        bad_ids = __ballot(ids < 0);
+    };
+    const uint32_t kl = (uint32_t)((lane / CH) * (PAGED ? D : cols) + 8 * ((lane % CH) ^ k_swizzle<D>(lane / CH))) * 2u;
+    const uint32_t vl = (uint32_t)((lane / CH) * (PAGED ? D : cols) + 8 * ((lane % CH) ^ v_swizzle<D>(lane / CH))) * 2u;
+    // asks for tile j; which of its 16-key groups have no page
+    auto fill = [&](int j, int buf) -> uint32_t {
+        uint8_t *ks_ = smem_raw + buf * TILE_BYTES + 16 * wave * D * 2, *vs_ = ks_ + 2 * TILE_BYTES;
+        uint32_t bad = 0;
+        if constexpr (PAGED) {
+            if (j - ids_from >= 16) load_ids(j);
+            const int id = max(__builtin_amdgcn_readlane(ids, 4 * (j - ids_from) + wave), 0);
+            bad = (uint32_t)(bad_ids >> (4 * (j - ids_from))) & 15u;
+            const size_t at = (size_t)page_element(id, h, a.kv_heads, a.shift, D) + (size_t)((TILE_KEYS * j + 16 * wave) & ((1 << a.shift) - 1)) * D;
+            const uint8_t *kb = reinterpret_cast<const uint8_t*>(a.kp + at), *vb = reinterpret_cast<const uint8_t*>(a.vp + at);
+#pragma unroll
+            for (int i = 0; i < FILLS; ++i) {
+                const uint32_t ko = kl ^ (uint32_t)(k_swizzle<D>(ROWS * i) * 16);
+                __builtin_amdgcn_global_load_lds((gptr_t)(kb + ROWS * i * D * 2 + ko), (lptr_t)(ks_ + 1024 * i), 16, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < FILLS; ++i) __builtin_amdgcn_global_load_lds((gptr_t)(vb + ROWS * i * D * 2 + vl), (lptr_t)(vs_ + 1024 * i), 16, 0, 0);
+        } else {
+            const int k0 = TILE_KEYS * j + 16 * wave;
+            const uint8_t* base = reinterpret_cast<const uint8_t*>(a.qkv + (size_t)q.first * cols + (a.heads + h) * D);
+            if (TILE_KEYS * (j + 1) <= q.len) {
+#pragma unroll
+                for (int i = 0; i < FILLS; ++i) {
+                    const uint8_t* kb = base + (size_t)(k0 + ROWS * i) * cols * 2;
+                    const uint32_t ko = kl ^ (uint32_t)(k_swizzle<D>(ROWS * i) * 16);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kb + ko), (lptr_t)(ks_ + 1024 * i), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kb + a.kv_heads * D * 2 + vl), (lptr_t)(vs_ + 1024 * i), 16, 0, 0);
+                }
+            } else {                                   // rows behind the sequence's last: that one, in their place
+#pragma unroll
+                for (int i = 0; i < FILLS; ++i) {
+                    const int row = ROWS * i + lane / CH;
+                    const uint8_t* kb = base + (size_t)min(k0 + row, q.len - 1) * cols * 2;
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kb + 16 * ((lane % CH) ^ k_swizzle<D>(row))), (lptr_t)(ks_ + 1024 * i), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kb + a.kv_heads * D * 2 + 16 * ((lane % CH) ^ v_swizzle<D>(row))), (lptr_t)(vs_ + 1024 * i), 16, 0, 0);
+                }
+            }
+        }
+        return bad;
+    };
+
+    V8 qf[KS];                                         // Q^T operands: lane (row col, features 16 k + 8 half ..)
+    {
+        const uint16_t* qp = a.qkv + (size_t)(q.first + tok) * cols + head * D + 8 * half;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const V8*>(qp + 16 * k);
+    }
+    f16x o[DTL];
+#pragma unroll
+    for (int d = 0; d < DTL; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = -INFINITY, l = 0.0f;                     // the maximum in use of the lane's row; this lane's part of its sum
+    // operand reads, bytes within a buffer
+    uint32_t ka[KS], va[DTL];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) ka[k] = (uint32_t)(col * D * 2 + 16 * ((2 * k + half) ^ k_swizzle<D>(col)));
+#pragma unroll
+    for (int d = 0; d < DTL; ++d) {
+        const int row = 4 * half + (lane & 15) / 4, chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        va[d] = (uint32_t)(2 * TILE_BYTES + row * D * 2 + 16 * (chunk ^ v_swizzle<D>(row)) + 8 * (lane & 1));
+    }
+
+    if constexpr (PAGED) load_ids(ks.begin);
+    uint32_t bad = 0, bad_next = fill(ks.begin, 0);
+    for (int j = ks.begin; j < ks.end; ++j) {
+        const int buf = (j - ks.begin) & 1, j0 = TILE_KEYS * j;
+        bad = bad_next;
+        __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): this wave's part of tile j has landed
+        if (bad != 0 || j0 + TILE_KEYS > tl.key_end) { // values of keys that no row sees: zero, like their weights
+#pragma unroll
+            for (int i = 0; i < FILLS; ++i) {
+                const int row = 16 * wave + ROWS * i + lane / CH;
+                if ((bad >> wave & 1) || j0 + row >= tl.key_end) *reinterpret_cast<u32x4*>(smem_raw + 2 * TILE_BYTES + buf * TILE_BYTES + (16 * wave + ROWS * i) * D * 2 + 16 * lane) = u32x4{};
+            }
+        }
+        __syncthreads();                               // everybody's part has landed, and tile j - 1 is no longer read
+        if (j + 1 < ks.end) bad_next = fill(j + 1, buf ^ 1);
+        if (j >= my_end) continue;
+        // Operands are read a batch ahead of the matrix instructions that take them, and the wait for a batch stands ahead of the next batch's issue:
+        // with global-to-LDS loads under way the compiler waits for every LDS read at each use.
+        auto wait_reads = [] { __builtin_amdgcn_s_waitcnt(0xC07F); __builtin_amdgcn_sched_barrier(0); };
+        const uint8_t* tile = smem_raw + buf * TILE_BYTES;
+        V8 ra[8], rb[8];
+        auto read_k = [&](V8 (&x)[8], int kt) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) x[k] = *reinterpret_cast<const V8*>(tile + ka[k] + 32 * kt * D * 2);
+        };
+        auto read_v = [&](V8 (&x)[8], int d0) {        // features 32 d0 .. 32 d0 + 63, the tile's four 16-key steps
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint8_t* at = tile + va[d0 + i / 4] + 16 * (i % 4) * D * 2;
+                typedef __attribute__((address_space(3))) s16x4* tr_t;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(at + 8 * D * 2));
+                x[i] = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
+        f16x s[2];
+        constexpr f16x zero = {};
+        read_k(ra, 0);
+        wait_reads();
+        read_k(rb, 1);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) s[0] = Elem<DT>::mfma32(ra[k], qf[k], k == 0 ? zero : s[0]);
+        wait_reads();
+        read_v(ra, 0);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) s[1] = Elem<DT>::mfma32(rb[k], qf[k], k == 0 ? zero : s[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (ALIBI) {                         // to base 2, with the linear bias
+            const float base = slope * (float)(j0 + 4 * half - p);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kt][i] = __builtin_fmaf(s[kt][i], c, __builtin_fmaf(slope, (float)(32 * kt + 8 * (i / 4) + i % 4), base));
+        }
+        if (bad != 0 || j0 + TILE_KEYS > all_see) {    // some key of the tile is not for some row of the wave
+            const int rel = min(p, tl.key_end - 1) - j0 - 4 * half;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[kt][i] = 32 * kt + 8 * (i / 4) + i % 4 <= rel && !(bad >> (2 * kt + i / 8) & 1) ? s[kt][i] : -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
+        const f2 m2 = both_halves(mx);
+        mx = fmaxf(m2[0], m2[1]);
+        if constexpr (!ALIBI) mx *= c;
+        if (__any(mx > m + LAZY)) {
+            const float mn = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DTL; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        }
+        const float ms = m == -INFINITY ? 0.0f : m;
+        V8 pf[4];                                      // P^T operands of the four 16-key steps
+        float ls = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 8) {
+                u32x4 x;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e] - ms : __builtin_fmaf(s[kt][i + e], c, -ms));
+                    const float e1 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e + 1] - ms : __builtin_fmaf(s[kt][i + e + 1], c, -ms));
+                    ls += e0;
+                    ls += e1;
+                    x[e / 2] = Elem<DT>::pack(e0, e1);
+                }
+                pf[2 * kt + i / 8] = __builtin_bit_cast(V8, x);
+            }
+        l += ls;
+#pragma unroll
+        for (int d0 = 0; d0 < DTL; d0 += 2) {
+            V8 (&cur)[8] = (d0 & 2) ? rb : ra;
+            wait_reads();
+            if (d0 + 2 < DTL) read_v((d0 & 2) ? ra : rb, d0 + 2);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[d0 + i / 4] = Elem<DT>::mfma32(cur[i], pf[i % 4], o[d0 + i / 4]);
+        }
+    }
+    if (!active) return;
+    const f2 l2 = both_halves(l);
+    l = l2[0] + l2[1];
+    // the lane holds features 32 d + 8 a + 4 half + 0 .. 3 of its row; the halves trade so that each stores 16 bytes
+    const bool mine = wr0 + col < tl.n_rows;
+    float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};         // finite if all the lane's sums are
+#pragma unroll
+    for (int d = 0; d < DTL; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) total[i % 4] += o[d][i];
+    uint64_t again = __ballot(!__builtin_isfinite((total[0] + total[1]) + (total[2] + total[3])) && mine);
+    again = (again | again >> 32) & 0xffffffffu;       // rows to be done again: a bit per column, of either half
+    const bool store = mine && !(again >> col & 1);
+    float* const part = ks.used == 1 ? nullptr : a.part + (((size_t)h * a.tiles + v) * a.splits + split) * (TILE_ROWS_Q * (D + 2));
+    uint16_t* const orow = a.out + (size_t)(q.first + tok) * a.heads * D + head * D;
+    if (part) {
+        if (store) {
+#pragma unroll
+            for (int d = 0; d < DTL; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f4*>(part + (size_t)(wr0 + col) * D + 32 * d + 2 * i + 4 * half) = f4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+            if (half == 0) *reinterpret_cast<f2*>(part + TILE_ROWS_Q * D + 2 * (wr0 + col)) = f2{m, l};
+        }
+    } else {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int d = 0; d < DTL; ++d)
+#pragma unroll
+            for (int b = 0; b < 4; b += 2) {
+                u32x4 x;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x2 t = __builtin_amdgcn_permlane32_swap(Elem<DT>::pack(o[d][4 * b + 2 * i] * inv, o[d][4 * b + 2 * i + 1] * inv),
+                                                                     Elem<DT>::pack(o[d][4 * b + 4 + 2 * i] * inv, o[d][4 * b + 5 + 2 * i] * inv), false, false);
+                    x[i] = t[0];
+                    x[2 + i] = t[1];
+                }
+                if (store) *reinterpret_cast<u32x4*>(orow + 8 * half + 32 * d + 8 * b) = x;
+            }
+    }
+    while (__builtin_expect(again != 0, 0)) {
+        const int k = __builtin_ctzll(again), rk = tl.row0 + wr0 + k, tk = rk / a.group, hk = h * a.group + rk % a.group;
+        again &= again - 1;
+        float wm, wl, acc[D / 64];
+        row_walk<DT, D>(a, q, h, a.qkv + (size_t)(q.first + tk) * cols + hk * D, q.pos0 + tk, ALIBI ? a.slopes[hk] * LOG2E : 0.0f, TILE_KEYS * ks.begin,
+                        TILE_KEYS * ks.end, wm, wl, acc);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            if (part) part[(size_t)(wr0 + k) * D + 64 * i + lane] = acc[i];
+            else a.out[(size_t)(q.first + tk) * a.heads * D + hk * D + 64 * i + lane] = (uint16_t)Elem<DT>::pack(acc[i] * (wl == 0.0f ? 0.0f : 1.0f / wl), 0.0f);
+        }
+        if (part && lane == 0) *reinterpret_cast<f2*>(part + TILE_ROWS_Q * D + 2 * (wr0 + k)) = f2{wm, wl};
+    }
+}
+
+// Adds up the splits of 16 rows (blockIdx.y) of a row tile and head (blockIdx.x), in order.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void tile_combine_kernel(AttnArgs a)
+{
+    const int h = (int)blockIdx.x / a.tiles, v = (int)blockIdx.x % a.tiles;
+    Tile tl;
+    if (!tile_of(a, v, &tl)) return;
+    const KeySplit ks = key_split(tl.key_tiles, a.splits, LEAST_KEY_TILES, 0);
+    if (ks.used == 1) return;
+    const float* base = a.part + ((size_t)h * a.tiles + v) * a.splits * (TILE_ROWS_Q * (D + 2));
+    for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
+        const int rr = 16 * (int)blockIdx.y + i / (D / 4), f = 4 * (i % (D / 4));
+        if (rr >= tl.n_rows) break;
+        float m = -INFINITY;
+        for (int k = 0; k < ks.used; ++k) m = fmaxf(m, base[(size_t)k * (TILE_ROWS_Q * (D + 2)) + TILE_ROWS_Q * D + 2 * rr]);
+        const float ms = m == -INFINITY ? 0.0f : m;
+        f4 num = {0.0f, 0.0f, 0.0f, 0.0f};
+        float den = 0.0f;
+#pragma unroll 4
+        for (int k = 0; k < ks.used; ++k) {
+            const float* ps = base + (size_t)k * (TILE_ROWS_Q * (D + 2));
+            const f2 ml = *reinterpret_cast<const f2*>(ps + TILE_ROWS_Q * D + 2 * rr);
+            const float w = __builtin_amdgcn_exp2f(ml[0] - ms);
+            den += w * ml[1];
+            num += w * *reinterpret_cast<const f4*>(ps + (size_t)rr * D + f);
+        }
+        const float inv = den == 0.0f ? 0.0f : 1.0f / den;
+        const int r = tl.row0 + rr, tok = r / a.group, head = h * a.group + r % a.group;
+        const u32x2 x = {Elem<DT>::pack(num[0] * inv, num[1] * inv), Elem<DT>::pack(num[2] * inv, num[3] * inv)};
+        *reinterpret_cast<u32x2*>(a.out + (size_t)(tl.q.first + tok) * a.heads * D + head * D + f) = x;
+    }
+}
+
+}  // namespace
+
+// ---- host ------------------------------------------------------------------------------------------
+
+// What a call launches: the streaming kernel, the tile kernel or, where a batch may have sequences of both kinds, both.
+AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int M, int max_q, int max_kv, int cus)
+{
+    AttentionPlan p{};
+    const int group = c.n_heads / c.n_kv_heads;
+    const int64_t most = (int64_t)std::min(max_q, M) * group;
+    p.stream_tiles = 0;
+    if (paged && most <= 2 * STREAM_ROWS) p.stream_tiles = most <= STREAM_ROWS ? 1 : 2;
+    else if (paged && n_seqs > 1 && group <= 2 * STREAM_ROWS) p.stream_tiles = group <= STREAM_ROWS ? 1 : 2;
+    p.tile = !(paged && most <= 2 * STREAM_ROWS);
+    p.workers = 2 * cus;
+    p.tiles = (int)tile_bound(M, group, n_seqs);
+    p.splits = 1;
+    if (p.tile) {
+        // workgroups that have rows, two to a compute unit
+        const int64_t wgs = std::max<int64_t>(1, ((int64_t)M * group + TILE_ROWS_Q - 1) / TILE_ROWS_Q) * c.n_kv_heads, slots = 2 * (int64_t)cus;
+        const int64_t key_tiles = ((int64_t)max_kv + TILE_KEYS - 1) / TILE_KEYS;
+        if (wgs < slots) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / wgs, 16), key_tiles / LEAST_KEY_TILES));
+    }
+    const size_t d2 = (size_t)c.head_dim + 2;
+    if (p.stream_tiles) p.stream_floats = (size_t)2 * p.workers * STREAM_ROWS * p.stream_tiles * d2;
+    if (p.splits > 1) p.tile_floats = (size_t)p.tiles * c.n_kv_heads * p.splits * TILE_ROWS_Q * d2;
+    return p;
+}
+
+template <int DT, int D>
+static hipError_t launch_attention(const AttentionPlan& p, AttnArgs a, float* part, hipStream_t s)
+{
+    const bool alibi = a.slopes != nullptr;
+    const bool both = p.stream_tiles && p.tile;
+    if (p.stream_tiles) {
+        a.rows_from = 1;
+        a.rows_to = both ? 2 * STREAM_ROWS + 1 : INT32_MAX;
+        a.workers = p.workers;
+        a.part = p.stream_floats ? part : nullptr;
+        const unsigned grid = (unsigned)p.workers;
+#define LPQ_STREAM(NT)                                                                                                  \
+        do {                                                                                                            \
+            if (alibi) stream_attention_kernel<DT, D, NT, true><<<grid, 256, 0, s>>>(a);                                \
+            else       stream_attention_kernel<DT, D, NT, false><<<grid, 256, 0, s>>>(a);                               \
+            if (a.part) stream_combine_kernel<DT, D, NT><<<dim3(grid, STREAM_ROWS * NT), 256, 0, s>>>(a);               \
+        } while (0)
+        if (p.stream_tiles == 1) LPQ_STREAM(1);
+        else LPQ_STREAM(2);
+#undef LPQ_STREAM
+    }
+    if (p.tile) {
+        a.rows_from = both ? 2 * STREAM_ROWS + 1 : 1;
+        a.rows_to = INT32_MAX;
+        a.tiles = p.tiles;
+        a.splits = p.splits;
+        a.part = part;
+        const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
+        const unsigned grid = (unsigned)(a.kv_heads * classes) * (unsigned)((p.tiles + classes - 1) / classes) * (unsigned)p.splits;
+        constexpr size_t smem = 4 * TILE_KEYS * D * 2;
+        if (a.kp) {
+            if (alibi) tile_attention_kernel<DT, D, true, true><<<grid, 256, smem, s>>>(a);
+            else       tile_attention_kernel<DT, D, false, true><<<grid, 256, smem, s>>>(a);
+        } else {
+            if (alibi) tile_attention_kernel<DT, D, true, false><<<grid, 256, smem, s>>>(a);
+            else       tile_attention_kernel<DT, D, false, false><<<grid, 256, smem, s>>>(a);
+        }
+        if (p.splits > 1) tile_combine_kernel<DT, D><<<dim3((unsigned)(p.tiles * a.kv_heads), TILE_ROWS_Q / 16), 256, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_batch_attention(const AttentionPlan& p, const lpq_attn_cfg& c, const void* qkv, const void* kp, const void* vp, const int32_t* table,
+                                  int shift, int n_pages, int max_pages, const int32_t* cu_q, const int32_t* kv_lens, const float* slopes, int n_seqs, int M,
+                                  void* out, float* part, hipStream_t s)
+{
+    AttnArgs a{};
+    a.qkv = static_cast<const uint16_t*>(qkv);
+    a.kp = static_cast<const uint16_t*>(kp);
+    a.vp = static_cast<const uint16_t*>(vp);
+    a.table = table;
+    a.cu_q = cu_q;
+    a.kv_lens = kv_lens;
+    a.slopes = slopes;
+    a.out = static_cast<uint16_t*>(out);
+    a.n_seqs = n_seqs;
+    a.M = M;
+    a.heads = c.n_heads;
+    a.kv_heads = c.n_kv_heads;
+    a.group = c.n_heads / c.n_kv_heads;
+    a.shift = shift;
+    a.n_pages = n_pages;
+    a.max_pages = max_pages;
+    if (c.dtype == LPQ_DT_FP16) return c.head_dim == 128 ? launch_attention<LPQ_DT_FP16, 128>(p, a, part, s) : launch_attention<LPQ_DT_FP16, 64>(p, a, part, s);
+    return c.head_dim == 128 ? launch_attention<LPQ_DT_BF16, 128>(p, a, part, s) : launch_attention<LPQ_DT_BF16, 64>(p, a, part, s);
+}
+
+}  // namespace lpq

@@ -1,0 +1,660 @@
+"""GPU parity of the operators over paged caches and packed rows: the plan (integers, equal), the append (bit-exact) and both attentions against
+plain 64-bit implementations, at the sizes, layouts and masks where they can go wrong, and a run of them together.
+
+Tolerance of an attention output, element by element.  With weights w_j (summing to 1), A = sum w_j |v_j| and u half a step of the output's type
+(2^-11 fp16, 2^-8 bf16):
+  * the weights are rounded to that type ahead of their product:                          u A
+  * a weight exp2(s) has the error of its exponent: the score is a 32-bit sum of D products of 16-bit numbers ((D + 4) 2^-24 sum |q_i k_i|),
+    scaled, biased and shifted by the row's maximum in 32 bits (3 roundings of at most 2^-24 (|s| + |max|)), and exp2 itself 2^-22;
+    the error counts for the weight and for the sum it is divided by:                     2 (ln 2 * that + 2^-22) A
+  * 32-bit sums over n keys, of the products and of the weights:                          2 n 2^-24 A
+  * the output's own rounding, u |out|, and half the smallest step where it is subnormal (fp16: 2^-25)."""
+import math
+import random
+
+import numpy as np
+import pytest
+
+import paper_2403_01136_amd as lpq
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"fp16": 0, "bf16": 1}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU (no fallback path)"
+    lpq.load_library()
+
+
+def dtype_of(name):
+    import torch
+    return {"fp16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def ints(values):
+    import torch
+    return torch.tensor(np.asarray(values), dtype=torch.int32, device="cuda")
+
+
+def gen(seed):
+    import torch
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+# ---- the plan ---------------------------------------------------------------------------------------------------------
+
+def plan_ref(past, q_lens, table, ring, head, free, P, M):
+    """The step one sequence, page and token after the other."""
+    n_pages, width = len(ring), len(table[0])
+    table, ring = [list(t) for t in table], list(ring)
+    supply = [ring[(head + i) % n_pages] for i in range(free)]
+    cu, kv, slots, pos = [0], [], [-1] * M, [0] * M
+    rows = wanted = taken = starved = 0
+    back = []
+    for s, (p, q) in enumerate(zip(past, q_lens)):
+        p = max(p, 0)
+        if q < 0:
+            back += table[s][:min(-(-p // P), width)]
+            cu.append(min(rows, M)), kv.append(0)
+            continue
+        start, rows = rows, rows + q
+        cu.append(min(rows, M))
+        ok = q == 0 or (rows <= M and p + q <= width * P)
+        if ok and q:
+            held, need = -(-p // P), -(-(p + q) // P) - -(-p // P)
+            wanted += need
+            ok = need == 0 or wanted <= free
+            if ok:
+                if need:
+                    table[s][held:held + need] = supply[wanted - need:wanted]
+                    taken = wanted
+                for t in range(q):
+                    page = table[s][(p + t) // P]
+                    pos[start + t] = p + t
+                    slots[start + t] = page * P + (p + t) % P if 0 <= page < n_pages else -1
+        starved += not ok
+        kv.append(p + q if ok else p)
+    back = back[:n_pages - free]
+    for i, page in enumerate(back):
+        ring[(head + free + i) % n_pages] = page
+    return dict(cu_q=cu, kv_lens=kv, slots=slots, positions=pos, counters=[(head + taken) % n_pages, free - taken + len(back)],
+                info=[cu[-1], taken, len(back), starved], table=table, ring=ring)
+
+
+def plan_case(seed, n, P, q_of, past_hi, spare, width_extra=2, pad=3):
+    """(past, q_lens, table, ring, head, free, M): sequences that hold the pages of their positions, the rest on the ring from a random place on."""
+    r = random.Random(seed)
+    past = [r.choice((0, 1, P - 1, P, r.randint(0, past_hi))) for _ in range(n)]
+    q = [q_of(r) for _ in range(n)]
+    held = [-(-p // P) for p in past]
+    need = [-(-(p + max(x, 0)) // P) - h for p, x, h in zip(past, q, held)]
+    free = max(0, sum(need) + spare)
+    n_pages = sum(held) + free + r.randint(0, 3) or 1
+    ids = list(range(n_pages))
+    r.shuffle(ids)
+    width = max(h + e for h, e in zip(held, need)) + width_extra
+    table, at = [], 0
+    for h in held:
+        table.append(ids[at:at + h] + [-7] * (width - h))
+        at += h
+    head = r.randrange(n_pages)
+    ring = [-9] * n_pages
+    for i in range(free):
+        ring[(head + i) % n_pages] = ids[at + i]
+    return past, q, table, ring, head, free, max(1, sum(max(x, 0) for x in q) + pad)
+
+
+def run_plan(past, q, table, ring, head, free, P, M, in_place=False):
+    import torch
+    past_d, q_d, table_d, ring_d, counters = ints(past), ints(q), ints(table), ints(ring), ints([head, free])
+    n = len(past)
+    plan = tuple(torch.full((m,), -123, dtype=torch.int32, device="cuda") for m in (n + 1, n, M, M, 2, 4))
+    if in_place:
+        plan = (plan[0], past_d, plan[2], plan[3], counters, plan[5])
+    got = lpq.lpq_paged_plan(past_d, q_d, table_d, ring_d, counters, P, M, plan=plan)
+    out = {k: getattr(got, k).tolist() for k in got._fields}
+    out.update(table=table_d.tolist(), ring=ring_d.tolist())
+    return out
+
+
+def check_plan(case, P, **k):
+    want = plan_ref(*case[:6], P, case[6])
+    got = run_plan(*case[:6], P, case[6], **k)
+    for name, w in want.items():
+        assert got[name] == w, name
+    return want
+
+
+DECODE, MIXED = (lambda r: 1), (lambda r: r.choice((1, 1, 1, 0, -1, r.randint(2, 90))))
+
+
+@pytest.mark.parametrize("in_place", [False, True], ids=["apart", "in_place"])
+@pytest.mark.parametrize("P", [16, 64, 256])
+@pytest.mark.parametrize("n", [1, 2, 7, 64, 65, 129, 300, 2048])
+def test_plan(n, P, in_place):
+    for i, q_of in enumerate((DECODE, MIXED)):
+        check_plan(plan_case(100 * n + P + i, n, P, q_of, 700, 5), P, in_place=in_place)
+
+
+@pytest.mark.parametrize("n,lo,hi", [(3, 1500, 2500), (24, 100, 900), (200, 0, 60), (1, 9000, 9000)])
+def test_plan_many_rows(n, lo, hi):
+    """More rows than one launch takes: the second launch's path."""
+    case = plan_case(n, n, 32, lambda r: r.choice((r.randint(lo, hi), r.randint(lo, hi), -1 if n > 3 else hi)), 400, 9)
+    check_plan(case, 32)
+    check_plan(case, 32, in_place=True)
+
+
+@pytest.mark.parametrize("n", [5, 40, 257])
+def test_plan_starved(n):
+    """Too few pages, rows behind the batch, positions behind the table, an empty pool; finished sequences return theirs all the same."""
+    case = plan_case(n, n, 16, MIXED, 300, 0)
+    past, q, table, ring, head, free, M = case
+    for f in (0, 1, free // 2, max(free - 1, 0)):
+        assert check_plan((past, q, table, ring, head, f, M), 16)["info"][1] <= f
+    rows = sum(max(x, 0) for x in q)
+    for m in (1, rows // 2, max(rows - 1, 1)):
+        check_plan((past, q, table, ring, head, free, m), 16)
+    narrow = [t[:max(1, len(t) - 3)] for t in table]
+    check_plan((past, q, narrow, ring, head, free, M), 16)
+    check_plan((past, [-1] * n, table, ring, head, free, M), 16)            # everybody has finished
+    check_plan((past, [0] * n, table, ring, head, free, M), 16)             # nobody has anything
+
+
+def test_plan_odd_integers():
+    """Lengths at the ends of their type, counters out of range, tables with ids that are no pages: defined results, nothing out of place."""
+    big = 2**31 - 1
+    past, q, table = [big, 5, -4, big, 20, 33], [1, big, 3, -1, 2, 0], [[-1, 90, 4]] * 6
+    want = plan_ref([big, 5, 0, big, 20, 33], q, table, list(range(10)), 3, 4, 16, 50)
+    got = run_plan(past, q, table, list(range(10)), 3, 4, 16, 50)
+    for name in want:
+        assert got[name] == want[name], name
+    for head, free, h, f in ((-5, 3, 0, 3), (23, 3, 3, 3), (2, -1, 2, 0), (2, 99, 2, 10)):
+        want = plan_ref([0, 17], [1, 20], [[-1] * 4] * 2, list(range(10)), h, f, 16, 30)
+        got = run_plan([0, 17], [1, 20], [[-1] * 4] * 2, list(range(10)), head, free, 16, 30)
+        for name in want:
+            assert got[name] == want[name], name
+
+
+# ---- the append -------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("H,KV,d,P,M", [(1, 1, 64, 16, 1), (4, 2, 128, 16, 7), (12, 12, 64, 64, 33), (7, 7, 128, 256, 5), (10, 2, 64, 32, 300), (64, 8, 128, 128, 129)])
+def test_append_bit_exact(H, KV, d, P, M, dt):
+    import torch
+    n_pages = M // P + 5
+    g = gen(M + d)
+    qkv = torch.randn((M, (H + 2 * KV) * d), generator=g, device="cuda").to(dtype_of(dt))
+    k, v = (torch.randn((n_pages, KV, P, d), generator=g, device="cuda").to(dtype_of(dt)) for _ in range(2))
+    r = random.Random(M)
+    slots = r.sample(range(n_pages * P), M)
+    for bad, at in ((-1, 0), (n_pages * P, 2), (2**31 - 1, 4), (-2**31, 6)):
+        if at < M and M > 1:
+            slots[at] = bad
+    k_ref, v_ref = k.clone(), v.clone()
+    for row, s in enumerate(slots):
+        if 0 <= s < n_pages * P:
+            new = qkv[row, H * d:].view(2, KV, d)
+            k_ref[s // P, :, s % P], v_ref[s // P, :, s % P] = new[0], new[1]
+    lpq.lpq_paged_append(qkv, k, v, ints(slots))
+    assert torch.equal(k.view(torch.int16), k_ref.view(torch.int16)) and torch.equal(v.view(torch.int16), v_ref.view(torch.int16))
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+
+def attention_ref(q, k, v, ok, pos, slopes):
+    """q [T][H][d], k, v [L][KV][d] (any values where ok is false), ok [L], pos [T] -> (out [T][H][d], bound without the output's rounding and the weights')
+    in 64 bits; per head."""
+    import torch
+    T, H, d = q.shape
+    L, KV = k.shape[0], k.shape[1]
+    out, A, E = (torch.zeros((T, H, d), dtype=torch.float64, device="cuda") for _ in range(3))
+    if L == 0:
+        return out, A, E
+    j = torch.arange(L, device="cuda")
+    vis = ok[None, :] & (j[None, :] <= pos[:, None])
+    dist = (j[None, :] - pos[:, None]).double()
+    for h in range(H):
+        kh, vh = k[:, h // (H // KV)].double(), v[:, h // (H // KV)].double()
+        kh = torch.where(ok[:, None], kh, torch.zeros_like(kh))
+        qh = q[:, h].double()
+        s = (qh @ kh.t().contiguous()) / math.sqrt(d)
+        mag = (qh.abs() @ kh.abs().t().contiguous()) / math.sqrt(d)
+        if slopes is not None:
+            s = s + float(slopes[h]) * dist
+            mag = mag + (float(slopes[h]) * dist).abs()
+        s = torch.where(vis, s, torch.full_like(s, -math.inf))
+        top = s.amax(1, keepdim=True)
+        w = torch.exp(s - torch.where(torch.isinf(top), torch.zeros_like(top), top))
+        total = w.sum(1, keepdim=True)
+        w = w / torch.where(total > 0, total, torch.ones_like(total))
+        # values that a row may not see have weight zero, whatever they are: 0 * inf is left out
+        vz = torch.where(torch.isfinite(vh), vh, torch.zeros_like(vh))
+        o = w @ vz
+        odd = (~torch.isfinite(vh)).any(1)
+        if bool(odd.any()):
+            seen = (vis & odd[None, :]).any(1)
+            o[seen] = (w[seen][:, :, None] * vh[None]).sum(1) if int(seen.sum()) * L * d < 2e8 else math.nan
+        out[:, h] = o
+        A[:, h] = w @ vz.abs()
+        lg = math.log2(math.e)
+        fin = lambda x: torch.where(torch.isfinite(x), x, torch.zeros_like(x))
+        arg = ((d + 4) * mag * lg + 3 * (fin(s).abs() * lg + fin(top).abs() * lg)) * 2.0**-24
+        E[:, h] = (w * (2 * (math.log(2) * torch.where(vis, arg, torch.zeros_like(arg)).amax(1, keepdim=True) + 2.0**-22) + 2 * L * 2.0**-24)) @ vz.abs()
+    return out, A, E
+
+
+def check_attention(got, parts, what=""):
+    """parts: [(rows, reference)]; rows that no part names have to be as they were: 77."""
+    import torch
+    u = {torch.float16: 2.0**-11, torch.bfloat16: 2.0**-8}[got.dtype]
+    left = torch.ones(got.shape[0], dtype=torch.bool, device="cuda")
+    for (r0, r1), (out, A, E) in parts:
+        left[r0:r1] = False
+        if r1 == r0:
+            continue
+        g = got[r0:r1].double().view(out.shape)
+        nan = torch.isnan(out)
+        assert torch.equal(torch.isnan(g), nan), what + ": NaN at other places"
+        tol = u * A + E + u * (out.abs() + u * A + E) + 2.0**-25
+        far = torch.where(nan, torch.zeros_like(out), (g - out).abs() / tol)
+        assert float(far.max()) <= 1.0, "%s: rows %d..%d, %.2f of the bound at %s" % (what, r0, r1, float(far.max()), np.unravel_index(int(far.argmax()), far.shape))
+    assert bool((got[left] == 77).all()), what + ": rows behind the last sequence"
+
+
+def slopes_of(H, alibi):
+    import torch
+    return torch.tensor([2.0 ** (-8.0 * (i + 1) / H) for i in range(H)], dtype=torch.float32, device="cuda") if alibi else None
+
+
+def packed_run(lens, H, KV, d, dt, alibi, pad=0, seed=0, max_q=None, edit=None):
+    import torch
+    M = max(1, sum(lens) + pad)
+    qkv = torch.randn((M, (H + 2 * KV) * d), generator=gen(seed + M + H), device="cuda")
+    qkv[:, :H * d] *= 2
+    qkv = qkv.to(dtype_of(dt))
+    if edit:
+        edit(qkv)
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    out = torch.full((M, H * d), 77.0, dtype=qkv.dtype, device="cuda")
+    slopes = slopes_of(H, alibi)
+    lpq.lpq_packed_attention(qkv, ints(cu), H, KV, max_q=max_q, alibi_slopes=slopes, out=out)
+    parts = []
+    for s, n in enumerate(lens):
+        rows = qkv[cu[s]:cu[s + 1]]
+        q, k, v = rows[:, :H * d].view(n, H, d), rows[:, H * d:(H + KV) * d].view(n, KV, d), rows[:, (H + KV) * d:].view(n, KV, d)
+        parts.append(((cu[s], cu[s + 1]), attention_ref(q, k, v, torch.ones(n, dtype=torch.bool, device="cuda"), torch.arange(n, device="cuda"), slopes)))
+    return out, parts
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("alibi", [False, True], ids=["plain", "alibi"])
+@pytest.mark.parametrize("lens,H,KV,d,pad", [
+    ([1], 1, 1, 64, 0), ([1, 1, 1], 4, 2, 128, 2), ([64], 3, 3, 128, 0), ([63, 65, 0, 2], 6, 2, 64, 5), ([127, 128, 129], 4, 4, 64, 1), ([200, 1, 17, 0, 300], 12, 12, 64, 9),
+    ([130, 33], 14, 2, 128, 0), ([5, 90], 40, 1, 64, 3), ([700], 2, 2, 128, 0), ([513, 31], 20, 4, 128, 40), ([16] * 70, 8, 8, 64, 0), ([300], 130, 1, 64, 0),
+], ids=lambda v: "x".join(map(str, v[:5])) if isinstance(v, list) else str(v))
+def test_packed_attention(lens, H, KV, d, pad, alibi, dt):
+    check_attention(*packed_run(lens, H, KV, d, dt, alibi, pad), what="packed %s" % lens)
+
+
+def test_packed_attention_long():
+    """Longer than a tile's and a split's worth, with few rows elsewhere; a length expected that is not the longest."""
+    check_attention(*packed_run([2300, 40], 4, 1, 128, "fp16", False), what="long")
+    check_attention(*packed_run([1900, 40], 4, 1, 64, "bf16", True, max_q=8), what="long, unexpected")
+
+
+@pytest.mark.parametrize("n", [64, 65, 100, 2048])
+def test_packed_attention_many_sequences(n):
+    r = random.Random(n)
+    check_attention(*packed_run([r.choice((0, 1, 2, 9, 40)) if n < 2048 else r.choice((0, 1, 2)) for _ in range(n)], 4, 2, 64, "fp16", False, 3), what="many")
+
+
+class Paged:
+    """A pool filled with random values (stale ones everywhere), sequences (cached positions, new tokens) on pages in random order."""
+
+    def __init__(self, seqs, H, KV, d, P, dt, pad=0, seed=0, spare=3, width_extra=1):
+        import torch
+        self.seqs, self.H, self.KV, self.d, self.P = seqs, H, KV, d, P
+        g = gen(seed + 17 * len(seqs) + H + P)
+        have = [-(-(p + q) // P) for p, q in seqs]
+        self.n_pages = sum(have) + spare
+        ids = torch.randperm(self.n_pages, generator=g, device="cuda").tolist()
+        width = max(have) + width_extra
+        self.table, at = [], 0
+        for h in have:
+            self.table.append(ids[at:at + h] + [-1] * (width - h))
+            at += h
+        self.cu = np.concatenate([[0], np.cumsum([q for _, q in seqs])])
+        self.M = max(1, int(self.cu[-1]) + pad)
+        qkv = torch.randn((self.M, (H + 2 * KV) * d), generator=g, device="cuda")
+        qkv[:, :H * d] *= 2
+        self.qkv = qkv.to(dtype_of(dt))
+        self.k, self.v = (torch.randn((self.n_pages, KV, P, d), generator=g, device="cuda").to(dtype_of(dt)) for _ in range(2))
+
+    def run(self, alibi=False, max_q=None, max_kv=None, kv_lens=None, out=None):
+        import torch
+        kv = [p + q for p, q in self.seqs] if kv_lens is None else kv_lens
+        out = torch.full((self.M, self.H * self.d), 77.0, dtype=self.qkv.dtype, device="cuda") if out is None else out
+        slopes = slopes_of(self.H, alibi)
+        lpq.lpq_paged_attention(self.qkv, self.k, self.v, ints(self.table), ints(self.cu), ints(kv), max_q=max_q, max_kv=max_kv, alibi_slopes=slopes, out=out)
+        return out, self.parts(kv, slopes)
+
+    def parts(self, kv, slopes):
+        import torch
+        res = []
+        for s, (past, q) in enumerate(self.seqs):
+            L = min(max(kv[s], 0), len(self.table[s]) * self.P)
+            ids = torch.tensor([self.table[s][j // self.P] for j in range(L)], dtype=torch.long, device="cuda")
+            ok = (ids >= 0) & (ids < self.n_pages)
+            off = torch.arange(L, device="cuda") % self.P
+            k, v = (t[torch.where(ok, ids, torch.zeros_like(ids)), :, off] for t in (self.k, self.v))
+            v = torch.where(ok[:, None, None], v, torch.zeros_like(v))
+            r0, r1 = self.cu[s], self.cu[s + 1]
+            pos = max(kv[s], 0) - q + torch.arange(q, device="cuda")
+            res.append(((r0, r1), attention_ref(self.qkv[r0:r1, :self.H * self.d].view(q, self.H, self.d), k, v, ok, pos, slopes)))
+        return res
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("alibi", [False, True], ids=["plain", "alibi"])
+@pytest.mark.parametrize("seqs,H,KV,d,P,pad", [
+    ([(0, 1)], 1, 1, 64, 16, 0), ([(0, 1), (15, 1), (16, 1), (17, 1)], 4, 2, 128, 16, 3), ([(31, 1), (32, 1), (127, 1), (128, 1), (700, 1)], 5, 5, 64, 32, 0),
+    ([(1000, 1)], 12, 12, 128, 64, 0), ([(3000, 1), (2, 1)], 8, 1, 128, 256, 1), ([(450, 1)] * 9, 32, 2, 64, 64, 0), ([(777, 1), (1290, 1)], 14, 2, 128, 128, 2),
+    ([(5000, 1)], 40, 2, 64, 16, 0), ([(600, 1), (60, 1)], 34, 1, 128, 32, 0), ([(333, 1)], 80, 2, 128, 64, 0),
+], ids=lambda v: "_".join("%d+%d" % x for x in v[:4]) if isinstance(v, list) else str(v))
+def test_paged_decode(seqs, H, KV, d, P, pad, alibi, dt):
+    check_attention(*Paged(seqs, H, KV, d, P, dt, pad).run(alibi, max_q=1), what="decode")
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("alibi", [False, True], ids=["plain", "alibi"])
+@pytest.mark.parametrize("seqs,H,KV,d,P,pad", [
+    ([(0, 5)], 1, 1, 64, 16, 0), ([(100, 3), (9, 2), (0, 4)], 8, 2, 128, 16, 2), ([(900, 8), (30, 1)], 4, 1, 64, 64, 0), ([(40, 16), (0, 1), (7, 0)], 2, 2, 128, 32, 0),
+    ([(64, 64)], 2, 2, 64, 64, 0), ([(0, 130), (250, 33)], 6, 2, 128, 256, 7), ([(1500, 100)], 16, 2, 128, 128, 0), ([(2000, 40), (100, 200)], 4, 4, 64, 16, 1),
+    ([(3000, 20)], 7, 1, 128, 64, 0), ([(500, 1), (700, 90), (3, 1), (0, 1), (90, 31)], 8, 4, 64, 16, 5), ([(10, 1), (900, 300), (1200, 1)], 34, 1, 64, 32, 2),
+    ([(200, 1), (2100, 300)], 56, 8, 128, 32, 3),
+], ids=lambda v: "_".join("%d+%d" % x for x in v[:4]) if isinstance(v, list) else str(v))
+def test_paged_chunks_and_mixed(seqs, H, KV, d, P, pad, alibi, dt):
+    """Chunks short and long, alone and beside sequences that decode: the streaming kernel's one and two column tiles, the tile kernel, its splits, and both."""
+    p = Paged(seqs, H, KV, d, P, dt, pad)
+    check_attention(*p.run(alibi, max_q=max(q for _, q in seqs), max_kv=max(a + b for a, b in seqs)), what="chunks")
+
+
+@pytest.mark.parametrize("hints", [(1, 1), (10000, 10**6), (None, None), (5, 100)], ids=str)
+def test_paged_hints_do_not_change_the_result(hints):
+    p = Paged([(300, 1), (0, 60), (1700, 2), (40, 17)], 8, 2, 128, 32, "fp16", 4)
+    check_attention(*p.run(False, max_q=hints[0], max_kv=hints[1]), what="hints")
+
+
+@pytest.mark.parametrize("n", [64, 257, 2048])
+def test_paged_decode_many_sequences(n):
+    r = random.Random(n)
+    top = 500 if n < 1000 else 40
+    check_attention(*Paged([(r.choice((0, 3, r.randint(0, top))), r.choice((1, 1, 1, 0))) for _ in range(n)], 4, 2, 64, 16, "bf16", 3).run(max_q=1), what="many")
+
+
+def test_paged_long_context():
+    """Many parts of one row tile, ids reloaded many times, small pages."""
+    check_attention(*Paged([(40000, 1)], 4, 1, 128, 16, "fp16").run(max_q=1), what="long")
+    check_attention(*Paged([(20011, 1), (5, 1), (9000, 1)], 6, 2, 64, 64, "bf16").run(True, max_q=1), what="long, ragged")
+    check_attention(*Paged([(9000, 20)], 8, 1, 128, 16, "fp16").run(max_q=20), what="long chunk")
+
+
+@pytest.mark.parametrize("q", [1, 3, 50])
+def test_paged_rows_that_see_nothing(q):
+    """No keys, fewer keys than new tokens, tables without pages: zeros, and the other sequences as ever."""
+    p = Paged([(0, q), (20, q), (100, q), (0, q)], 4, 2, 64, 16, "fp16", 2)
+    p.table[0] = [-1] * len(p.table[0])
+    out, parts = p.run(max_q=q, kv_lens=[0, 20 + q, -3, max(q - 1, 0)])
+    check_attention(out, parts, what="nothing to see")
+    assert bool((out[:q] == 0).all()) and bool((out[2 * q:3 * q] == 0).all())
+
+
+@pytest.mark.parametrize("alibi", [False, True], ids=["plain", "alibi"])
+@pytest.mark.parametrize("q,P", [(1, 16), (1, 64), (3, 32), (60, 16), (150, 64)])
+def test_paged_bad_pages_are_masked(q, P, alibi):
+    """Ids that are no pages of the pool, at the front, in the middle and at the end, and lengths beyond the table."""
+    p = Paged([(400, q), (333, q), (300, q)], 6, 2, 128, P, "fp16", 1, width_extra=0)
+    p.table[0][0] = -1
+    p.table[0][3] = p.n_pages
+    p.table[1][2] = -2**31
+    p.table[1][-2] = 2**31 - 1
+    p.table[2] = [-5] * len(p.table[2])
+    cap = len(p.table[0]) * P
+    check_attention(*p.run(alibi, max_q=q), what="bad pages")
+    check_attention(*p.run(alibi, max_q=q, kv_lens=[cap + 20, cap + 5, 10]), what="beyond the table")
+
+
+@pytest.mark.parametrize("q,H,KV", [(1, 8, 2), (1, 4, 4), (4, 4, 2), (20, 4, 4), (100, 8, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_paged_stale_values_do_not_matter(q, H, KV, d):
+    """NaN and infinities in every position that no sequence has: behind the last one in its page, and in pages of nobody."""
+    import torch
+    p = Paged([(37, q), (250, q), (1030, q), (0, q)], H, KV, d, 64, "fp16")
+    want, _ = p.run(max_q=q)
+    used = torch.zeros((p.n_pages, 64), dtype=torch.bool, device="cuda")
+    for s, (past, n) in enumerate(p.seqs):
+        for j in range(past + n):
+            used[p.table[s][j // 64], j % 64] = True
+    for pages, val in ((p.k, math.nan), (p.v, math.inf), (p.v, math.nan), (p.k, math.inf)):
+        pages.copy_(torch.where(used[:, None, :, None], pages, torch.full_like(pages, val)))
+        got, _ = p.run(max_q=q)
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("q", [2, 4, 16, 40, 140])
+@pytest.mark.parametrize("val", [math.nan, math.inf, -math.inf], ids=str)
+def test_later_tokens_do_not_matter(q, val):
+    """A value row of the newest token that is not finite: NaN or infinite for the tokens that see it, as without it for the others; the same for keys."""
+    import torch
+    past = 70
+    for where in ("v", "k"):
+        p = Paged([(past, q), (10, q)], 8, 2, 64, 16, "fp16")
+        want, _ = p.run(max_q=q)
+        j = past + q - 1
+        getattr(p, where)[p.table[0][j // 16], :, j % 16] = val
+        got, _ = p.run(max_q=q)
+        assert torch.equal(got[q:], want[q:])
+        assert torch.allclose(got[:q - 1].float(), want[:q - 1].float(), rtol=2.0**-9, atol=2.0**-10)
+        if where == "v" or math.isnan(val):
+            assert not bool(torch.isfinite(got[q - 1]).any())
+
+    out, _ = packed_run([q, 30], 8, 1, 64, "bf16", False, edit=lambda x: x[q - 1, 9 * 64:].fill_(val))     # the first prompt's last value row
+    ref, _ = packed_run([q, 30], 8, 1, 64, "bf16", False)
+    assert torch.equal(out[q:], ref[q:])
+    assert torch.allclose(out[:q - 1].float(), ref[:q - 1].float(), rtol=2.0**-6, atol=2.0**-7)
+    assert not bool(torch.isfinite(out[q - 1]).any())
+
+
+def test_large_scores():
+    """Scores in the thousands: one key takes all; and all scores equal."""
+    import torch
+    p = Paged([(500, 1), (300, 30)], 4, 2, 128, 32, "fp16")
+    p.qkv *= 20
+    check_attention(*p.run(max_q=30), what="large")
+    p.k.zero_()
+    check_attention(*p.run(max_q=30), what="equal")
+
+
+def test_pool_past_32_bits():
+    """Pages more than 2^31 elements into the pool."""
+    import torch
+    P, KV, d = 256, 16, 128
+    n_pages = 2**31 // (KV * P * d) + 40
+    k, v = (torch.zeros((n_pages, KV, P, d), dtype=torch.float16, device="cuda") for _ in range(2))
+    p = Paged([(700, 1), (100, 40)], 16, KV, d, P, "fp16")
+    off = n_pages - p.n_pages
+    k[off:], v[off:] = p.k, p.v
+    want, parts = p.run(max_q=40)
+    p.table = [[t + off if t >= 0 else t for t in row] for row in p.table]
+    p.k, p.v, p.n_pages = k, v, n_pages
+    got, _ = p.run(max_q=40)
+    assert torch.equal(got, want)
+    slots = [(n_pages - 1) * P + 255, 3]
+    rows = p.qkv[:2].contiguous()
+    lpq.lpq_paged_append(rows, k, v, ints(slots))
+    assert torch.equal(k[n_pages - 1, :, 255], rows[0, 16 * d:32 * d].view(KV, d)) and torch.equal(v[0, :, 3], rows[1, 32 * d:].view(KV, d))
+
+
+def test_same_inputs_same_bits():
+    import torch
+    p = Paged([(3000, 1), (700, 60), (10, 1)], 8, 2, 128, 16, "fp16")
+    a, _ = p.run(max_q=60)
+    for _ in range(3):
+        assert torch.equal(p.run(max_q=60)[0], a)
+
+
+def test_binding_checks():
+    import torch
+    p = Paged([(30, 1), (20, 1)], 4, 2, 64, 16, "fp16")
+    t, cu, kv = ints(p.table), ints(p.cu), ints([31, 21])
+    call = lambda **k: lpq.lpq_paged_attention(**{**dict(qkv=p.qkv, k_pages=p.k, v_pages=p.v, table=t, cu_q=cu, kv_lens=kv), **k})
+    call()
+    for bad in (dict(qkv=p.qkv.bfloat16()), dict(qkv=p.qkv[:, :-8].contiguous()), dict(k_pages=p.k[:, :1].contiguous()), dict(v_pages=p.v[1:]), dict(table=t.long()),
+                dict(table=t[:1]), dict(cu_q=cu[:2]), dict(kv_lens=kv.cpu()), dict(table=t.t()), dict(out=p.qkv), dict(out=torch.zeros((2, 256), device="cuda")),
+                dict(alibi_slopes=torch.ones(3, device="cuda")), dict(qkv=p.qkv.cpu())):
+        with pytest.raises(ValueError):
+            call(**bad)
+    for bad in (dict(max_q=0), dict(max_kv=0), dict(qkv=p.qkv[:, :-64].contiguous())):      # 3 heads over 2 K/V heads
+        with pytest.raises(lpq.LpqError):
+            call(**bad)
+    with pytest.raises(ValueError):
+        lpq.lpq_paged_append(p.qkv, p.k, p.v, ints([1]))
+    with pytest.raises(ValueError):
+        lpq.lpq_paged_plan(kv, kv, t, ints([0] * 9), ints([0, 9, 1]), 16, 2)
+    with pytest.raises(ValueError):
+        lpq.lpq_packed_attention(p.qkv, cu, 3, 2)
+
+
+# ---- a run of them together -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("alibi", [False, True], ids=["plain", "alibi"])
+def test_serving_run(alibi):
+    """Requests come, are prefilled (whole and in chunks) and decode side by side through a quantised QKV linear; some finish, their pages go to others.
+    Every step's output against 64 bits on the step's own qkv and all the keys and values appended so far."""
+    import torch
+    H, KV, d, P, n_pages, width, N, M = 8, 2, 64, 16, 40, 12, 6, 96
+    cols = (H + 2 * KV) * d
+    g = gen(5)
+    w = lpq.lpq_quantize_pack((torch.randn((cols, H * d), generator=g, device="cuda") * 0.06).half(), 4, lpq.LPQ_ASYM_GROUP)
+    k, v = (torch.full((n_pages, KV, P, d), math.nan, dtype=torch.float16, device="cuda") for _ in range(2))
+    table, ring, counters = torch.full((N, width), -1, dtype=torch.int32, device="cuda"), torch.arange(n_pages, dtype=torch.int32, device="cuda"), ints([0, n_pages])
+    lens = torch.zeros(N, dtype=torch.int32, device="cuda")
+    plan = None
+    history = [([], []) for _ in range(N)]
+    steps = [[50, 0, 20, 0, 0, 0], [1, 30, 1, 40, 0, 0], [1, 1, 1, 30, 9, 0], [1, 1, -1, 1, 1, 60], [1, -1, 25, 1, 1, 20], [1, 33, 1, -1, 30, 1], [40, 1, 1, 45, 1, 1], [1, 1, 1, 1, 1, 1]]
+    slopes = slopes_of(H, alibi)
+    for step, q in enumerate(steps):
+        x = torch.randn((M, H * d), generator=g, device="cuda").half()
+        qkv = lpq.lpq_qlinear_fused(w, x, lpq.LPQ_PREFILL)
+        plan = lpq.lpq_paged_plan(lens, ints(q), table, ring, counters, P, M, plan=None if plan is None else plan)
+        if plan.kv_lens.data_ptr() != lens.data_ptr():
+            lens.copy_(plan.kv_lens), counters.copy_(plan.counters)
+            plan = plan._replace(kv_lens=lens, counters=counters)          # in place from now on
+        lpq.lpq_paged_append(qkv, k, v, plan.slots)
+        out = torch.full((M, H * d), 77.0, dtype=torch.float16, device="cuda")
+        lpq.lpq_paged_attention(qkv, k, v, table, plan.cu_q, lens, max_q=max(q), alibi_slopes=slopes, out=out)
+        assert plan.info[3].item() == 0, "the pool is large enough for these requests"
+        parts, r0 = [], 0
+        for s, n in enumerate(q):
+            if n < 0:
+                history[s] = ([], [])
+                continue
+            rows = qkv[r0:r0 + n]
+            history[s][0].append(rows[:, H * d:(H + KV) * d].reshape(n, KV, d)), history[s][1].append(rows[:, (H + KV) * d:].reshape(n, KV, d))
+            ks, vs = torch.cat(history[s][0]), torch.cat(history[s][1])
+            L = ks.shape[0]
+            assert lens[s].item() == L
+            parts.append(((r0, r0 + n), attention_ref(rows[:, :H * d].reshape(n, H, d), ks, vs, torch.ones(L, dtype=torch.bool, device="cuda"),
+                                                      L - n + torch.arange(n, device="cuda"), slopes)))
+            r0 += n
+        check_attention(out, parts, what="step %d" % step)
+    held = sum(-(-int(n) // P) for n in lens.tolist())
+    assert counters[1].item() == n_pages - held
+    # every page is somebody's or free, none twice
+    head, free = counters.tolist()
+    owned = [t for s in range(N) for t in table[s, :-(-int(lens[s]) // P)].tolist()]
+    assert sorted(owned + [ring[(head + i) % n_pages].item() for i in range(free)]) == list(range(n_pages))
+
+
+def test_paged_against_packed_and_contiguous():
+    """The same prompts through the packed rows, through pages, and (one length, as many K/V heads as heads) through the contiguous cache."""
+    import torch
+    H, d, T, B, P = 5, 128, 150, 3, 32
+    qkv = torch.randn((B * T, 3 * H * d), generator=gen(9), device="cuda").half()
+    one = torch.ones(H * d, dtype=torch.float16, device="cuda")
+    st = lpq.LayerState(H, d, 192, B, torch.device("cuda"), (one, one), (one, one))
+    lpq.lpq_kv_append(qkv, st, B, T, 0)
+    want = lpq.lpq_attention(qkv, st, B, T, 0).float()
+    cu = ints([0, T, 2 * T, 3 * T])
+    table, ring = torch.full((B, 5), -1, dtype=torch.int32, device="cuda"), torch.arange(20, dtype=torch.int32, device="cuda").flip(0).contiguous()
+    plan = lpq.lpq_paged_plan(ints([0] * B), ints([T] * B), table, ring, ints([0, 20]), P, B * T)
+    assert torch.equal(plan.cu_q, cu)
+    k, v = (torch.zeros((20, H, P, d), dtype=torch.float16, device="cuda") for _ in range(2))
+    lpq.lpq_paged_append(qkv, k, v, plan.slots)
+    # each side is within its rounding of the exact result: weights and output in fp16, |v| up to about 4.5
+    for got in (lpq.lpq_packed_attention(qkv, cu, H, H), lpq.lpq_paged_attention(qkv, k, v, table, cu, plan.kv_lens)):
+        assert float((got.float() - want).abs().max()) <= 2 * 2 * 2.0**-11 * 4.5
+
+
+# ---- streams and graphs -----------------------------------------------------------------------------------------------
+
+def test_on_another_stream():
+    import torch
+    p = Paged([(900, 1), (40, 30)], 8, 2, 64, 16, "fp16")
+    want, _ = p.run(max_q=30)
+    s = torch.cuda.Stream()
+    t, cu, kv, out = ints(p.table), ints(p.cu), ints([901, 70]), torch.full_like(want, 77.0)
+    torch.cuda.synchronize()
+    lpq.lpq_paged_attention(p.qkv, p.k, p.v, t, cu, kv, max_q=30, out=out, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_captured_decode_loop():
+    """A decode step (plan in place, append, attention) captured once and replayed: each replay is the next step, as the eager loop has it; eager work of other
+    sizes, with its own use of the workspace, runs between the replays."""
+    import torch
+    H, KV, d, P, N, n_pages = 8, 2, 128, 16, 5, 80
+
+    def fresh():
+        g = gen(3)
+        return dict(k=torch.zeros((n_pages, KV, P, d), dtype=torch.float16, device="cuda"), v=torch.zeros((n_pages, KV, P, d), dtype=torch.float16, device="cuda"),
+                    table=torch.full((N, 14), -1, dtype=torch.int32, device="cuda"), ring=torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32),
+                    counters=ints([7, n_pages]), lens=ints([0] * N), q=ints([60, 15, 16, 131, 1]), x=torch.zeros((230, (H + 2 * KV) * d), dtype=torch.float16, device="cuda"),
+                    out=torch.zeros((230, H * d), dtype=torch.float16, device="cuda"),
+                    plan=[torch.empty(m, dtype=torch.int32, device="cuda") for m in (N + 1, N, 230, 230, 2, 4)])
+
+    def step(s, max_q):
+        plan = (s["plan"][0], s["lens"], s["plan"][2], s["plan"][3], s["counters"], s["plan"][5])
+        lpq.lpq_paged_plan(s["lens"], s["q"], s["table"], s["ring"], s["counters"], P, 230, plan=plan)
+        lpq.lpq_paged_append(s["x"], s["k"], s["v"], s["plan"][2])
+        lpq.lpq_paged_attention(s["x"], s["k"], s["v"], s["table"], s["plan"][0], s["lens"], max_q=max_q, max_kv=14 * P, out=s["out"])
+
+    xs = [torch.randn((230, (H + 2 * KV) * d), generator=gen(50 + i), device="cuda").half() for i in range(6)]
+    eager, want = fresh(), []
+    for i, x in enumerate(xs):
+        eager["x"].copy_(x)
+        step(eager, 131 if i == 0 else 1)
+        want.append(eager["out"].clone())
+        eager["q"].fill_(1)
+    s = fresh()
+    s["x"].copy_(xs[0])
+    step(s, 131)
+    assert torch.equal(s["out"], want[0])
+    s["q"].fill_(1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(s, 1)
+    other = Paged([(3000, 1), (100, 40)], 8, 2, 128, 32, "fp16")
+    other_want, _ = other.run(max_q=40)
+    for i in range(1, 6):
+        s["x"].copy_(xs[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(s["out"], want[i]), "replay %d" % i
+        assert torch.equal(other.run(max_q=40)[0], other_want)
+    for name in ("k", "v", "table", "ring", "counters", "lens"):
+        assert torch.equal(s[name], eager[name]), name
