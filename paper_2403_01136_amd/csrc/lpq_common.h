@@ -212,7 +212,8 @@ hipError_t launch_paged_plan(const lpq_page_pool& pool, int shift, const int32_t
 hipError_t launch_paged_append(const void* qkv, const lpq_attn_cfg& c, int shift, int n_pages, void* k_pages, void* v_pages, const int32_t* slots, int M,
                                hipStream_t s);
 struct AttentionPlan {
-    int stream_tiles, workers;           // streaming kernel: column tiles of 16 rows (0: not launched), workgroups
+    int stream_tiles, stream_rows, workers;      // streaming kernel: column tiles of 16 rows (0: not launched), rows that a tile is expected to have, waves
+    bool long_lists;                     // few row tiles, cut into many parts each
     bool tile;                           // tile kernel launched
     int tiles, splits;                   // its virtual row tiles and K splits
     size_t stream_floats, tile_floats;   // partial results of either (0: whole row tiles only)

@@ -54,7 +54,7 @@ struct AttnArgs {
     float* part;                         // partial results, or null: nothing is split
     int32_t n_seqs, M, heads, kv_heads, group, shift, n_pages, max_pages;
     int32_t rows_from, rows_to;          // sequences with rows_from <= rows < rows_to are this launch's
-    int32_t workers, splits, tiles;      // streaming: workgroups; tile kernel: K splits, virtual row tiles
+    int32_t workers, splits, tiles;      // streaming: waves; tile kernel: K splits, virtual row tiles
 };
 
 // A sequence as a kernel sees it.
@@ -139,9 +139,10 @@ __device__ __forceinline__ void row_walk(const AttnArgs& a, const Seq& q, int h,
 }
 
 // ---- streaming kernel ---------------------------------------------------------------------------
-// Bound by the memory: 4 D bytes per key and K/V head.  A persistent launch; the units of 128 keys of all (sequence, head, row tile) are one list, cut into
-// equal shares, so contexts of any lengths fill the chip evenly.  A wave takes every fourth 32 keys of its workgroup's range, keeps the
-// next 32 under way in registers (16 KB per wave at D = 128) and meets the other waves only where a row tile ends.
+// Bound by the memory: 4 D bytes per key and K/V head.  A persistent launch whose workers are single waves, four to a compute unit: the units of 32 keys of
+// all (sequence, head, row tile) are one list, cut into equal shares, so contexts of any lengths fill the chip evenly.  A wave walks its share by itself:
+// nothing waits for another wave.  Two units (K and V of 8 KB each at D = 128) have register buffers, and the next unit's K or V is asked for as soon as
+// a buffer's contents are used up.
 //
 // Products on 16x16x32 matrix instructions, columns = rows of the problem (16 per column tile), so that scores land where the weights are wanted:
 //   S^T = K . Q^T    A = K: lane (i = lane % 16, q = lane / 16) holds key i, features 32 step + 8 q + 0..7, loaded as they lie;
@@ -149,22 +150,12 @@ __device__ __forceinline__ void row_walk(const AttnArgs& a, const Seq& q, int h,
 //   O^T = V^T . P^T  over 32 keys: lane quarter q contracts over keys {4 q + 0..3, 16 + 4 q + 0..3}: its own scores of the two key tiles, so
 //                    the weights go from result to operand in place.  V is read in whole rows (lane i: features F i .. F i + F - 1, F = D / 16, of the quarter's
 //                    eight keys); V^T operand e, features F i + e, is one v_perm per register, no LDS.  Register r of result e: feature F (4 q + r) + e.
-// A range's cut row tiles leave (unnormalised sums, maximum, sum) in two slots per workgroup, added up by stream_combine_kernel in the order of the keys.
-template <int DT, int D, int NT> struct StreamSmem {
-    float o[4][STREAM_ROWS][D + 4];      // one column tile at a time
-    float m[4][STREAM_ROWS * NT], l[4][STREAM_ROWS * NT];
-    uint64_t scan[4];
-    int64_t begin;                       // the worker's first unit's sequence: units before it
-    int seq;
-    uint32_t again;
-};
-
-__device__ __forceinline__ int64_t seq_units(const AttnArgs& a, int s, int tile_rows)
-{
-    if (s >= a.n_seqs) return 0;
-    const Seq q = load_seq(a, s);
-    return takes(a, q.rows) ? (int64_t)a.kv_heads * stream_row_tiles(q.rows, tile_rows) * stream_key_blocks(q.ctx) : 0;
-}
+// A row tile that a share's border cuts is left in parts (unnormalised sums, maximum, sum), two slots per worker, which stream_combine_kernel adds up in the
+// order of the keys; the worker in whose share it begins says so in its entry of `cuts`.
+// (With workgroups of four waves as workers, units of 128 keys, the waves' sums added through LDS where a row tile ends, and a combining kernel that found
+// the cut tiles by the same search: 16 sequences of 40 heads 36.5 + 18.3 us, 61 of 8 K/V heads 89.0 + 20.6, one of 90001 positions 61.4 + 27.5.)
+constexpr int CUTS_PER_WG = 16;          // of the combining kernel
+struct Cut { int32_t parts, first, row0, head_rows; };   // parts: 0: none; first row of the sequence; first row of the tile; K/V head * 64 + rows of the tile
 
 __device__ __forceinline__ int64_t uniform64(int64_t v)
 {
@@ -174,7 +165,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t v)
 __device__ __forceinline__ int64_t shfl64(int64_t v, int from)
 {
     const int lo = __shfl((int)(uint32_t)v, from), hi = __shfl((int)(v >> 32), from);
-    return (int64_t)(uint32_t)lo | (int64_t)hi << 32;
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
 }
 __device__ __forceinline__ int64_t scan64(int64_t v)                              // inclusive, over the wave
 {
@@ -186,103 +177,122 @@ __device__ __forceinline__ int64_t scan64(int64_t v)                            
     }
     return v;
 }
-// Total of the launch's units, by a workgroup of 256; scan: a word per wave.
-__device__ __forceinline__ int64_t units_total(const AttnArgs& a, int tile_rows, uint64_t* scan)
+
+__device__ __forceinline__ int64_t seq_units(const AttnArgs& a, int s, int tile_rows)
 {
-    int64_t v = 0;
-    for (int s = threadIdx.x; s < a.n_seqs; s += 256) v += seq_units(a, s, tile_rows);
-    v = shfl64(scan64(v), 63);
-    if ((threadIdx.x & 63) == 0) scan[threadIdx.x >> 6] = (uint64_t)v;
-    __syncthreads();
-    const int64_t total = (int64_t)(scan[0] + scan[1] + scan[2] + scan[3]);
-    __syncthreads();
-    return uniform64(total);
+    if (s >= a.n_seqs) return 0;
+    const Seq q = load_seq(a, s);
+    return takes(a, q.rows) ? (int64_t)a.kv_heads * stream_row_tiles(q.rows, tile_rows) * stream_key_steps(q.ctx) : 0;
 }
-// The sequence that has unit u, and the units before it, into *seq and *begin (LDS).
-__device__ __forceinline__ void units_find(const AttnArgs& a, int tile_rows, int64_t u, uint64_t* scan, int* seq, int64_t* begin)
+
+// A wave's share: units [u, end), the sequence that has unit u and the units before that sequence.
+struct Share { int64_t u, end, units, seq_begin; int workers, s; };
+struct ShareSmem { int64_t scan[4], begin[4]; int seq[4]; };
+__device__ __forceinline__ Share find_share(const AttnArgs& a, int tile_rows, ShareSmem& sm)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t first = seq_units(a, tid, tile_rows);                          // the usual batch has no more than 256 sequences: one pass
+    int64_t mine = first;
+    for (int s = tid + 256; s < a.n_seqs; s += 256) mine += seq_units(a, s, tile_rows);
+    int64_t sum = scan64(mine);
+    if (lane == 63) sm.scan[wave] = sum;
+    __syncthreads();
+    Share r;
+    r.units = uniform64(sm.scan[0] + sm.scan[1] + sm.scan[2] + sm.scan[3]);
+    r.workers = (int)min<int64_t>(a.workers, r.units);
+    const int w0 = 4 * (int)blockIdx.x;
     int64_t carry = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 256) {
-        const int64_t mine = seq_units(a, s0 + (int)threadIdx.x, tile_rows), sum = scan64(mine);
-        if (lane == 63) scan[wave] = (uint64_t)sum;
-        __syncthreads();
+        if (a.n_seqs > 256) {
+            mine = s0 == 0 ? first : seq_units(a, s0 + tid, tile_rows);
+            sum = scan64(mine);
+            __syncthreads();
+            if (lane == 63) sm.scan[wave] = sum;
+            __syncthreads();
+        }
         int64_t before = carry + sum - mine;
         for (int w = 0; w < 4; ++w) {
-            if (w < wave) before += (int64_t)scan[w];
-            carry += (int64_t)scan[w];
+            if (w < wave) before += sm.scan[w];
+            carry += sm.scan[w];
         }
-        if (u >= before && u < before + mine) *seq = s0 + (int)threadIdx.x, *begin = before;
-        __syncthreads();
+        for (int w = 0; w < 4; ++w) {
+            if (w0 + w >= r.workers) break;
+            const int64_t u = stream_begin(r.units, w0 + w, r.workers);
+            if (u >= before && u < before + mine) sm.seq[w] = s0 + tid, sm.begin[w] = before;
+        }
     }
+    __syncthreads();
+    const int w = __builtin_amdgcn_readfirstlane(w0 + wave);
+    r.u = r.end = r.seq_begin = 0;
+    r.s = 0;
+    if (w < r.workers) {
+        r.u = stream_begin(r.units, w, r.workers);
+        r.end = stream_begin(r.units, w + 1, r.workers);
+        r.s = __builtin_amdgcn_readfirstlane(sm.seq[wave]);
+        r.seq_begin = uniform64(sm.begin[wave]);
+    }
+    return r;
 }
 
-// A row tile of a sequence and head, and the units that it has.
-struct Segment {
-    Seq q;
-    int h, rt, blocks;
-    int64_t first;                       // its first unit
-};
-__device__ __forceinline__ Segment segment_of(const AttnArgs& a, int s, int64_t seq_begin, int64_t u, int tile_rows)
-{
-    Segment g;
-    g.q = load_seq(a, s);
-    g.blocks = stream_key_blocks(g.q.ctx);
-    const int tiles = stream_row_tiles(g.q.rows, tile_rows);
-    const int64_t at = u - seq_begin;
-    const int64_t t = at >> 31 ? at / g.blocks : (int64_t)((uint32_t)at / (uint32_t)g.blocks);
-    g.h = tiles == 1 ? (int)t : (int)(t / tiles);
-    g.rt = tiles == 1 ? 0 : (int)(t % tiles);
-    g.first = seq_begin + t * g.blocks;
-    return g;
-}
+// log2 of what a maximum may fall behind the largest score: a row's sums are then at most 2^8 larger, and its weights as exact as ever.  (Renewed with every
+// larger score there is hardly a tile without 16 or 32 rows' sums being multiplied.)
+constexpr float LAZY = 8.0f;
+
+// One wave per SIMD, two units under way: few, long, contiguous streams suit the memory.  Waves per SIMD / units, us, 61 sequences of 8 K/V heads and one of 90001
+// positions: 1 / 1 77.8, 66.0; 1 / 2 76.9, 63.2; 1 / 3 77.6, 62.7; 2 / 1 80.4, 66.4; 2 / 2 81.6, 66.5; 3 / 1 85.0, 72.4.
+constexpr int STREAM_WAVES = 1, DEPTH = 2;
 
 template <int DT, int D, int NT, bool ALIBI>
-__global__ __launch_bounds__(256, 2) void stream_attention_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, STREAM_WAVES) void stream_attention_kernel(AttnArgs a)
 {
     typedef typename Elem<DT>::v8 V8;
     constexpr int KJ = D / 32, F = D / 16, TILE_ROWS = STREAM_ROWS * NT;         // feature steps of S^T; features of a lane's V chunk
     constexpr int SLOT = TILE_ROWS * (D + 2);
     typedef uint32_t vchunk __attribute__((ext_vector_type(F / 2)));
-    __shared__ __attribute__((aligned(16))) StreamSmem<DT, D, NT> sm;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ ShareSmem sm;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const float c = LOG2E / sqrtf((float)D);
-    const int cols = (a.heads + 2 * a.kv_heads) * D;
+    const int cols = (a.heads + 2 * a.kv_heads) * D, page_mask = (1 << a.shift) - 1;
 
-    const int64_t units = units_total(a, TILE_ROWS, sm.scan);
-    const int W = (int)min<int64_t>(a.workers, units), w = blockIdx.x;
-    if (w >= W) return;
-    int64_t u = stream_begin(units, w, W);
-    const int64_t u_end = stream_begin(units, w + 1, W), u_begin = u;
-    units_find(a, TILE_ROWS, u, sm.scan, &sm.seq, &sm.begin);
-    int s = __builtin_amdgcn_readfirstlane(sm.seq);
-    int64_t s_begin = uniform64(sm.begin), s_units = seq_units(a, s, TILE_ROWS);
+    const Share share = find_share(a, TILE_ROWS, sm);
+    const int w = 4 * (int)blockIdx.x + wave;
+    int64_t u = share.u, s_begin = share.seq_begin;
+    int s = share.s;
+    Cut cut{0, 0, 0, 0};
+    int64_t s_units = u < share.end ? seq_units(a, s, TILE_ROWS) : 0;
 
-    while (u < u_end) {
+    while (u < share.end) {
         while (u >= s_begin + s_units) {               // the next sequence with units: there is one, u is below the total
             s_begin += s_units;
             s_units = seq_units(a, ++s, TILE_ROWS);
         }
-        const Segment g = segment_of(a, s, s_begin, u, TILE_ROWS);
-        const Seq q = g.q;
-        if (!a.part && g.first < u) {                  // nowhere to leave parts: a worker takes the row tiles that begin in its range, whole
-            u = g.first + g.blocks;
+        const Seq q = load_seq(a, s);
+        const int steps = stream_key_steps(q.ctx), tiles = stream_row_tiles(q.rows, TILE_ROWS);
+        const int64_t at = u - s_begin, tile = at >> 31 ? at / steps : (int64_t)((uint32_t)at / (uint32_t)steps), first = s_begin + tile * steps;
+        const int h = tiles == 1 ? (int)tile : (int)(tile / tiles), rt = tiles == 1 ? 0 : (int)(tile % tiles);
+        if (!a.part && first < u) {                    // nowhere to leave parts: a worker takes the row tiles that begin in its share, whole
+            u = first + steps;
             continue;
         }
-        const int b0 = (int)(u - g.first), b1 = a.part ? (int)min<int64_t>(g.blocks, u_end - g.first) : g.blocks;
-        const int row0 = g.rt * TILE_ROWS, n_rows = min(TILE_ROWS, q.rows - row0);
+        const int n0 = (int)(u - first), n1 = a.part ? (int)min<int64_t>(steps, share.end - first) : steps;
+        const int row0 = rt * TILE_ROWS, n_rows = min(TILE_ROWS, q.rows - row0);
         const int t_first = row0 / a.group, t_last = (row0 + n_rows - 1) / a.group;
         const int key_end = min(q.ctx, q.pos0 + t_last + 1);                     // no row sees a key from here on (may be below 1)
-        const int all_see = q.pos0 + t_first + 1;                               // every row sees the keys below
+        const int all_see = min(key_end, q.pos0 + t_first + 1);                 // every row sees the keys below
+        const int n_last = max(n0, min(n1, (key_end + STREAM_KEYS - 1) / STREAM_KEYS));
 
+        // pages: lane 2 n + i holds the page of 16-key group i of step k + n, 32 steps at a time
+        int ids = 0;
+        auto load_ids = [&](int k) { ids = k + lane / 2 < n_last ? page_of_group(a, s, 2 * k + lane) : -1; };
+        if (n0 < n_last) load_ids(n0);
         // the lane's column(s): query row, position, slope
         V8 qf[NT][KJ];
         int p[NT];
         float slope[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int r = row0 + min(STREAM_ROWS * t + col, n_rows - 1), tok = r / a.group, head = g.h * a.group + r % a.group;
+            const int r = row0 + min(STREAM_ROWS * t + col, n_rows - 1), tok = r / a.group, head = h * a.group + r % a.group;
             const uint16_t* qp = a.qkv + (size_t)(q.first + tok) * cols + head * D + 8 * quarter;
 #pragma unroll
             for (int j = 0; j < KJ; ++j) qf[t][j] = *reinterpret_cast<const V8*>(qp + 32 * j);
@@ -299,32 +309,101 @@ __global__ __launch_bounds__(256, 2) void stream_attention_kernel(AttnArgs a)
             for (int e = 0; e < F; ++e) o[t][e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 
-        // pages: lane 2 n + i holds the page of 16-key group i of step n, counted from step n0, 32 steps at a time
-        const int steps = max(0, min(b1 - b0, (key_end - 32 * wave - STREAM_BLOCK * b0 + STREAM_BLOCK - 1) / STREAM_BLOCK));       // of this wave
-        int ids = 0;
-        auto load_ids = [&](int n0) {
-            const int n = n0 + lane / 2;
-            ids = n < steps ? page_of_group(a, q.s, (STREAM_BLOCK / 16) * (b0 + n) + 2 * wave + (lane & 1)) : -1;
-        };
         const uint32_t koff = (uint32_t)(col * D + 8 * quarter) * 2u, voff = (uint32_t)(4 * quarter * D + F * col) * 2u;
-        V8 kf[2][2][KJ];
-        vchunk vf[2][2][4];
-        auto load = [&](int n, int x) {
-            const int key0 = STREAM_BLOCK * (b0 + n) + 32 * wave;
+        V8 kf[DEPTH][2][KJ];
+        vchunk vf[DEPTH][2][4];
+        uint32_t bad_of[DEPTH];                        // of the buffers' steps: bit i: 16-key group i has no page
+        uint64_t bad_ids = 0;                          // bit l: lane l's group has none
+        int ids_from = n0;
+        // step n's loads from the pages `from`: an address is a scalar base and a 32-bit lane offset
+        auto page_bytes = [&](const uint16_t* pages, int n, int i) {
+            const int id = max(__builtin_amdgcn_readlane(ids, 2 * (n - ids_from) + i), 0);
+            return reinterpret_cast<const uint8_t*>(pages + (size_t)page_element(id, h, a.kv_heads, a.shift, D) + (size_t)((STREAM_KEYS * n + 16 * i) & page_mask) * D);
+        };
+        auto load_k = [&](int n, int x) {
+            if (n - ids_from == 32) {
+                ids_from = n;
+                load_ids(n);
+                bad_ids = __ballot(ids < 0);
+            }
+            bad_of[x] = (uint32_t)(bad_ids >> (2 * (n - ids_from))) & 3u;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int id = max(__builtin_amdgcn_readlane(ids, 2 * (n & 31) + i), 0);
-                const size_t at = (size_t)page_element(id, g.h, a.kv_heads, a.shift, D) + (size_t)((key0 + 16 * i) & ((1 << a.shift) - 1)) * D;
-                const uint8_t *kb = reinterpret_cast<const uint8_t*>(a.kp + at), *vb = reinterpret_cast<const uint8_t*>(a.vp + at);
+                const uint8_t* b = page_bytes(a.kp, n, i);
 #pragma unroll
-                for (int j = 0; j < KJ; ++j) kf[x][i][j] = __builtin_nontemporal_load(reinterpret_cast<const V8*>(kb + koff + 64 * j));
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vf[x][i][r] = __builtin_nontemporal_load(reinterpret_cast<const vchunk*>(vb + voff + 2 * D * r));
+                for (int j = 0; j < KJ; ++j) kf[x][i][j] = __builtin_nontemporal_load(reinterpret_cast<const V8*>(b + koff + 64 * j));
             }
         };
-        auto compute = [&](int n, int x, uint32_t bad) {       // bad: bit i set: 16-key group i has no page
-            const int key0 = STREAM_BLOCK * (b0 + n) + 32 * wave;
-            const bool plain = bad == 0 && key0 + 32 <= min(all_see, key_end);
+        auto load_v = [&](int n, int x) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint8_t* b = page_bytes(a.vp, n, i);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vf[x][i][r] = __builtin_nontemporal_load(reinterpret_cast<const vchunk*>(b + voff + 2 * D * r));
+            }
+        };
+        if (n0 < n_last) bad_ids = __ballot(ids < 0);
+#pragma unroll
+        for (int x = 0; x < DEPTH; ++x)
+            if (n0 + x < n_last) {
+                load_k(n0 + x, x);
+                load_v(n0 + x, x);
+            }
+        auto step = [&](int n, int x) {
+            const int key0 = STREAM_KEYS * n;
+            const uint32_t bad = bad_of[x];
+            const bool plain = bad == 0 && key0 + STREAM_KEYS <= all_see, more = n + DEPTH < n_last;
+            f4 sc[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    sc[t][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < KJ; ++j) sc[t][i] = Elem<DT>::mfma16(kf[x][i][j], qf[t][j], sc[t][i]);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) load_k(n + DEPTH, x);
+            __builtin_amdgcn_sched_barrier(0);
+            V8 pf[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int key = key0 + 16 * i + 4 * quarter + r;
+                        float v = sc[t][i][r] * c;
+                        if constexpr (ALIBI) v = __builtin_fmaf(slope[t], (float)(key - p[t]), v);
+                        if (!plain) v = (bad >> i & 1) || key > p[t] || key >= key_end ? -INFINITY : v;
+                        sc[t][i][r] = v;
+                        mx = fmaxf(mx, v);
+                    }
+                f2 z = both_rows(mx);
+                z = both_halves(fmaxf(z[0], z[1]));
+                mx = fmaxf(z[0], z[1]);
+                if (__any(mx > m[t] + LAZY)) {
+                    const float mn = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - (mn == -INFINITY ? 0.0f : mn));
+                    l[t] *= alpha;
+#pragma unroll
+                    for (int e = 0; e < F; ++e) o[t][e] *= alpha;
+                    m[t] = mn;
+                }
+                const float ms = m[t] == -INFINITY ? 0.0f : m[t];
+                u32x4 pk;
+                float ls = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; r += 2) {
+                        const float e0 = __builtin_amdgcn_exp2f(sc[t][i][r] - ms), e1 = __builtin_amdgcn_exp2f(sc[t][i][r + 1] - ms);
+                        ls += e0 + e1;
+                        pk[2 * i + r / 2] = Elem<DT>::pack(e0, e1);
+                    }
+                l[t] += ls;
+                pf[t] = __builtin_bit_cast(V8, pk);
+            }
             if (!plain)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -332,221 +411,140 @@ __global__ __launch_bounds__(256, 2) void stream_attention_kernel(AttnArgs a)
                     for (int r = 0; r < 4; ++r)
                         if ((bad >> i & 1) || key0 + 16 * i + 4 * quarter + r >= key_end) vf[x][i][r] = vchunk{};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                f4 sc[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    sc[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int j = 0; j < KJ; ++j) sc[i] = Elem<DT>::mfma16(kf[x][i][j], qf[t][j], sc[i]);
-                }
-                float mx = -INFINITY;
+            for (int e = 0; e < F; ++e) {
+                u32x4 vt;                              // element e of the lane's chunks of the quarter's eight keys
+                const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int key = key0 + 16 * i + 4 * quarter + r;
-                        float v = sc[i][r] * c;
-                        if constexpr (ALIBI) v = __builtin_fmaf(slope[t], (float)(key - p[t]), v);
-                        if (!plain) v = (bad >> i & 1) || key > p[t] || key >= key_end ? -INFINITY : v;
-                        sc[i][r] = v;
-                        mx = fmaxf(mx, v);
-                    }
-                f2 z = both_rows(mx);
-                z = both_halves(fmaxf(z[0], z[1]));
-                const float mn = fmaxf(m[t], fmaxf(z[0], z[1])), ms = mn == -INFINITY ? 0.0f : mn;
-                if (__any(mn > m[t])) {
-                    const float alpha = __builtin_amdgcn_exp2f(m[t] - ms);
-                    l[t] *= alpha;
+                    for (int r = 0; r < 4; r += 2) vt[2 * i + r / 2] = __builtin_amdgcn_perm(vf[x][i][r + 1][e / 2], vf[x][i][r][e / 2], sel);
 #pragma unroll
-                    for (int e = 0; e < F; ++e) o[t][e] *= alpha;
-                    m[t] = mn;
-                }
-                u32x4 pk;
-                float ls = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; r += 2) {
-                        const float e0 = __builtin_amdgcn_exp2f(sc[i][r] - ms), e1 = __builtin_amdgcn_exp2f(sc[i][r + 1] - ms);
-                        ls += e0 + e1;
-                        pk[2 * i + r / 2] = Elem<DT>::pack(e0, e1);
-                    }
-                l[t] += ls;
-                const V8 pf = __builtin_bit_cast(V8, pk);
-#pragma unroll
-                for (int e = 0; e < F; ++e) {
-                    u32x4 vt;                          // element e of the lane's chunks of the quarter's eight keys
-                    const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int r = 0; r < 4; r += 2) vt[2 * i + r / 2] = __builtin_amdgcn_perm(vf[x][i][r + 1][e / 2], vf[x][i][r][e / 2], sel);
-                    o[t][e] = Elem<DT>::mfma16(__builtin_bit_cast(V8, vt), pf, o[t][e]);
-                }
+                for (int t = 0; t < NT; ++t) o[t][e] = Elem<DT>::mfma16(__builtin_bit_cast(V8, vt), pf[t], o[t][e]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) load_v(n + DEPTH, x);
+            __builtin_amdgcn_sched_barrier(0);
         };
-        uint64_t bad_ids = 0;
-        if (steps > 0) {
-            load_ids(0);
-            bad_ids = __ballot(ids < 0);
-            load(0, 0);
-        }
-        for (int n = 0; n < steps; n += 2) {
+        for (int n = n0; n < n_last; n += DEPTH)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {              // buffers by name
-                const int k = n + x;
-                if (k >= steps) break;
-                const uint32_t bad = (uint32_t)(bad_ids >> (2 * (k & 31))) & 3u;
-                if (k + 1 < steps) {
-                    if (((k + 1) & 31) == 0) {
-                        load_ids(k + 1);
-                        bad_ids = __ballot(ids < 0);
-                    }
-                    load(k + 1, x ^ 1);
-                }
-                compute(k, x, bad);
-            }
-        }
+            for (int x = 0; x < DEPTH; ++x)            // buffers by name
+                if (n + x < n_last) step(n + x, x);
 
-        // the four waves' sums, a column tile at a time
-        const bool whole = b0 == 0 && b1 == g.blocks;
-        float* slot = a.part + (size_t)(2 * w + (g.first < u_begin ? 0 : 1)) * SLOT;
+        // a whole row tile's results, or a part's sums
+        const bool whole = n0 == 0 && n1 == steps;
+        float* const slot = a.part + (size_t)(2 * w + (first < share.u ? 0 : 1)) * SLOT;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            const int ri = STREAM_ROWS * t + col, r = row0 + min(ri, n_rows - 1), tok = r / a.group, head = h * a.group + r % a.group;
             f2 z = both_rows(l[t]);
             z = both_halves(z[0] + z[1]);
-            if (quarter == 0) {
-                sm.m[wave][STREAM_ROWS * t + col] = m[t];
-                sm.l[wave][STREAM_ROWS * t + col] = z[0] + z[1];
+            const float L = z[0] + z[1];
+            uint32_t again = 0;                        // rows whose sums a later token's values have spoilt: a bit per column
+            if (q.len > 1) {
+                float total = 0.0f;
+#pragma unroll
+                for (int e = 0; e < F; ++e) total += (o[t][e][0] + o[t][e][1]) + (o[t][e][2] + o[t][e][3]);
+                uint64_t odd = __ballot(!__builtin_isfinite(total) && ri < n_rows);
+                odd |= odd >> 32;
+                again = (uint32_t)(odd | odd >> 16) & 0xffffu;
             }
-        }
-        if (tid == 0) sm.again = 0;
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (STREAM_ROWS * t >= n_rows) break;
-            const int cc = STREAM_ROWS * t + col;
-            const float mt = fmaxf(fmaxf(sm.m[0][cc], sm.m[1][cc]), fmaxf(sm.m[2][cc], sm.m[3][cc])), ms = mt == -INFINITY ? 0.0f : mt;
-            const float scale = __builtin_amdgcn_exp2f(m[t] - ms);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int e = 0; e < F; e += 4) {
-                    const f4 v = {o[t][e][r] * scale, o[t][e + 1][r] * scale, o[t][e + 2][r] * scale, o[t][e + 3][r] * scale};
-                    *reinterpret_cast<f4*>(&sm.o[wave][col][F * (4 * quarter + r) + e]) = v;
-                }
-            __syncthreads();
-            // thread: row tid / 16, features F (tid % 16) ..
-            const int rr = tid >> 4, f0 = F * (tid & 15), ri = STREAM_ROWS * t + rr;
-            const float m0 = sm.m[0][ri], m1 = sm.m[1][ri], m2 = sm.m[2][ri], m3 = sm.m[3][ri];
-            float M2 = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-            const float Ms = M2 == -INFINITY ? 0.0f : M2;
-            float L = sm.l[0][ri] * __builtin_amdgcn_exp2f(m0 - Ms) + sm.l[1][ri] * __builtin_amdgcn_exp2f(m1 - Ms) +
-                      sm.l[2][ri] * __builtin_amdgcn_exp2f(m2 - Ms) + sm.l[3][ri] * __builtin_amdgcn_exp2f(m3 - Ms);
-            float v[F];
-            float total = 0.0f;
-#pragma unroll
-            for (int e = 0; e < F; ++e) {
-                v[e] = (sm.o[0][rr][f0 + e] + sm.o[1][rr][f0 + e]) + (sm.o[2][rr][f0 + e] + sm.o[3][rr][f0 + e]);
-                total += v[e];
-            }
-            if (q.len > 1) {                           // a later token's row may have spoilt the sums of an earlier one
-                if (ri < n_rows && !__builtin_isfinite(total)) atomicOr(&sm.again, 1u << rr);
-                __syncthreads();
-                uint32_t again = sm.again;
-                __syncthreads();
-                if (again) {
-                    for (uint32_t left = again; left; left &= left - 1) {
-                        const int k = __builtin_ctz(left), r = row0 + STREAM_ROWS * t + k, tok = r / a.group, head = g.h * a.group + r % a.group;
-                        if (k % 4 != wave) continue;
-                        float wm, wl, acc[D / 64];
-                        row_walk<DT, D>(a, q, g.h, a.qkv + (size_t)(q.first + tok) * cols + head * D, q.pos0 + tok, ALIBI ? a.slopes[head] * LOG2E : 0.0f,
-                                        STREAM_BLOCK * b0, STREAM_BLOCK * b1, wm, wl, acc);
-#pragma unroll
-                        for (int i = 0; i < D / 64; ++i) sm.o[0][k][64 * i + lane] = acc[i];
-                        if (lane == 0) sm.m[0][STREAM_ROWS * t + k] = wm, sm.l[0][STREAM_ROWS * t + k] = wl;
-                    }
-                    __syncthreads();
-                    if (again >> rr & 1) {
-                        M2 = sm.m[0][ri];
-                        L = sm.l[0][ri];
-#pragma unroll
-                        for (int e = 0; e < F; ++e) v[e] = sm.o[0][rr][f0 + e];
-                    }
-                    if (tid == 0) sm.again = 0;
-                }
-            }
-            if (ri < n_rows) {
+            if (ri < n_rows && !(again >> col & 1)) {
                 if (whole) {
                     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-                    const int r = row0 + ri, tok = r / a.group, head = g.h * a.group + r % a.group;
-                    vchunk x;
+                    uint16_t* op = a.out + (size_t)(q.first + tok) * a.heads * D + head * D;
 #pragma unroll
-                    for (int e = 0; e < F; e += 2) x[e / 2] = Elem<DT>::pack(v[e] * inv, v[e + 1] * inv);
-                    *reinterpret_cast<vchunk*>(a.out + (size_t)(q.first + tok) * a.heads * D + head * D + f0) = x;
+                    for (int g = 0; g < 4; ++g) {
+                        vchunk y;
+#pragma unroll
+                        for (int e = 0; e < F; e += 2) y[e / 2] = Elem<DT>::pack(o[t][e][g] * inv, o[t][e + 1][g] * inv);
+                        *reinterpret_cast<vchunk*>(op + F * (4 * quarter + g)) = y;
+                    }
                 } else {
-                    float* ps = slot + (size_t)ri * (D + 2);
 #pragma unroll
-                    for (int e = 0; e < F; e += 2) *reinterpret_cast<f2*>(ps + f0 + e) = f2{v[e], v[e + 1]};
-                    if (f0 == 0) *reinterpret_cast<f2*>(ps + D) = f2{M2, L};
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int e = 0; e < F; e += 4)
+                            *reinterpret_cast<f4*>(slot + ri * D + F * (4 * quarter + g) + e) = f4{o[t][e][g], o[t][e + 1][g], o[t][e + 2][g], o[t][e + 3][g]};
+                    if (quarter == 0) *reinterpret_cast<f2*>(slot + TILE_ROWS * D + 2 * ri) = f2{m[t], L};
                 }
             }
-            __syncthreads();                           // before the next column tile's, or segment's, sums
+            while (__builtin_expect(again != 0, 0)) {
+                const int k = __builtin_ctz(again), rk = row0 + STREAM_ROWS * t + k, tk = rk / a.group, hk = h * a.group + rk % a.group;
+                again &= again - 1;
+                float wm, wl, acc[D / 64];
+                row_walk<DT, D>(a, q, h, a.qkv + (size_t)(q.first + tk) * cols + hk * D, q.pos0 + tk, ALIBI ? a.slopes[hk] * LOG2E : 0.0f, STREAM_KEYS * n0,
+                                STREAM_KEYS * n1, wm, wl, acc);
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    if (whole) a.out[(size_t)(q.first + tk) * a.heads * D + hk * D + 64 * i + lane] = (uint16_t)Elem<DT>::pack(acc[i] * (wl == 0.0f ? 0.0f : 1.0f / wl), 0.0f);
+                    else slot[(STREAM_ROWS * t + k) * D + 64 * i + lane] = acc[i];
+                }
+                if (!whole && lane == 0) *reinterpret_cast<f2*>(slot + TILE_ROWS * D + 2 * (STREAM_ROWS * t + k)) = f2{wm, wl};
+            }
         }
-        u = g.first + b1;
+        if (!whole && first >= share.u)                // it begins here and ends in another worker's share
+            cut = Cut{stream_worker(share.units, first + steps - 1, share.workers) - w + 1, q.first, row0, 64 * h + n_rows};
+        u = first + n1;
     }
+    if (a.part && lane == 0) reinterpret_cast<Cut*>(a.part + (size_t)2 * a.workers * SLOT)[w] = cut;
 }
 
-// Adds up the parts of the row tile that begins in worker blockIdx.x's range and goes on behind it, if there is one; a row per blockIdx.y.
-template <int DT, int D, int NT>
+// Adds up the parts of the row tiles that the entries of `cuts` name, 16 entries a workgroup; blockIdx.y: rows and, if LONG, slices of 32 features.  Many
+// short lists of parts: a wave takes a row of a cut, D / 4 lanes of four features each for every (256 / D)-th part.  LONG, for few lists of hundreds of parts:
+// the workgroup takes a slice, 8 lanes for every 32nd part, the sums added through LDS.  Either is right for any list.
+template <int DT, int D, int NT, bool LONG>
 __global__ __launch_bounds__(256) void stream_combine_kernel(AttnArgs a)
 {
-    constexpr int TILE_ROWS = STREAM_ROWS * NT, SLOT = TILE_ROWS * (D + 2);
-    __shared__ uint64_t scan[4];
-    __shared__ int64_t begin_s;
-    __shared__ int seq_s;
-    __shared__ float red[256 / D][D + 2];
-    const int64_t units = units_total(a, TILE_ROWS, scan);
-    const int W = (int)min<int64_t>(a.workers, units), w = blockIdx.x;
-    if (w >= W) return;
-    const int64_t u0 = stream_begin(units, w, W), u1 = stream_begin(units, w + 1, W);
-    units_find(a, TILE_ROWS, u1 - 1, scan, &seq_s, &begin_s);
-    const Segment g = segment_of(a, seq_s, begin_s, u1 - 1, TILE_ROWS);
-    if (g.first < u0 || g.first + g.blocks <= u1) return;
-    const int row0 = g.rt * TILE_ROWS, ri = blockIdx.y;
-    if (ri >= min(TILE_ROWS, g.q.rows - row0)) return;
-    const int last = stream_worker(units, g.first + g.blocks - 1, W);
-    // part k: worker w + k; the first is in its slot 1, the others, which begin inside the row tile, in their slot 0
-    auto part = [&](int k) { return a.part + (size_t)(2 * (w + k) + (k == 0 ? 1 : 0)) * SLOT + (size_t)ri * (D + 2); };
-    const int parts = last - w + 1, f = threadIdx.x % D, lane_part = threadIdx.x / D;
-    float m = -INFINITY, l = 0.0f, v = 0.0f;
-    for (int k = lane_part; k < parts; k += 256 / D) {
-        const float* ps = part(k);
-        const f2 ml = *reinterpret_cast<const f2*>(ps + D);
-        const float mn = fmaxf(m, ml[0]), ms = mn == -INFINITY ? 0.0f : mn, x = __builtin_amdgcn_exp2f(m - ms), y = __builtin_amdgcn_exp2f(ml[0] - ms);
-        m = mn;
-        l = l * x + ml[1] * y;
-        v = v * x + ps[f] * y;
-    }
-    red[lane_part][f] = v;
-    if (f == 0) red[lane_part][D] = m, red[lane_part][D + 1] = l;
-    __syncthreads();
-    if (threadIdx.x >= D) return;
-    float mt = -INFINITY;
+    constexpr int TILE_ROWS = STREAM_ROWS * NT, SLOT = TILE_ROWS * (D + 2), SLICES = LONG ? D / 32 : 1, LANES = D / SLICES / 4, WAYS = (LONG ? 256 : 64) / LANES;
+    __shared__ __attribute__((aligned(16))) float red[4][36];                    // LONG only: a wave's sums
+    const Cut* cuts = reinterpret_cast<const Cut*>(a.part + (size_t)2 * a.workers * SLOT);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = LONG ? (int)threadIdx.x : lane;
+    const int f = 32 * ((int)blockIdx.y % SLICES) + 4 * (team % LANES), way = team / LANES, row_step = (int)gridDim.y / SLICES;
+    const int w0 = CUTS_PER_WG * (int)blockIdx.x;
+    Cut mine{0, 0, 0, 0};
+    if (lane < CUTS_PER_WG && w0 + lane < a.workers) mine = cuts[w0 + lane];
+    uint64_t todo = __ballot(mine.parts != 0);
+    for (int i = 0; todo; ++i, todo &= todo - 1) {
+        if (!LONG && i % 4 != wave) continue;
+        const int k0 = __builtin_ctzll(todo), w = w0 + k0;
+        const int parts = __builtin_amdgcn_readlane(mine.parts, k0), first = __builtin_amdgcn_readlane(mine.first, k0);
+        const int row0 = __builtin_amdgcn_readlane(mine.row0, k0), hr = __builtin_amdgcn_readlane(mine.head_rows, k0), h = hr >> 6;
+        for (int ri = (int)blockIdx.y / SLICES; ri < (hr & 63); ri += row_step) {
+            float m = -INFINITY, l = 0.0f;
+            f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+            auto add = [&](float km, float kl, const f4& kv) {
+                const float mn = fmaxf(m, km), ms = mn == -INFINITY ? 0.0f : mn, x = __builtin_amdgcn_exp2f(m - ms), y = __builtin_amdgcn_exp2f(km - ms);
+                m = mn;
+                l = l * x + kl * y;
+                v = v * x + kv * y;
+            };
+#pragma unroll 4
+            for (int k = way; k < parts; k += WAYS) {  // part k: worker w + k; the first is in its slot 1, the others, which begin inside the row tile, in their slot 0
+                const float* ps = a.part + (size_t)(2 * (w + k) + (k == 0 ? 1 : 0)) * SLOT;
+                const f2 ml = *reinterpret_cast<const f2*>(ps + TILE_ROWS * D + 2 * ri);
+                const f4 o = *reinterpret_cast<const f4*>(ps + ri * D + f);
+                add(ml[0], ml[1], o);
+            }
 #pragma unroll
-    for (int k = 0; k < 256 / D; ++k) mt = fmaxf(mt, red[k][D]);
-    const float ms = mt == -INFINITY ? 0.0f : mt;
-    float num = 0.0f, den = 0.0f;
+            for (int d = LANES; d < 64; d *= 2) add(__shfl_xor(m, d), __shfl_xor(l, d), f4{__shfl_xor(v[0], d), __shfl_xor(v[1], d), __shfl_xor(v[2], d), __shfl_xor(v[3], d)});
+            if constexpr (LONG) {
+                __syncthreads();                       // the last row's sums are read
+                if (lane < LANES) {
+                    *reinterpret_cast<f4*>(&red[wave][4 * lane]) = v;
+                    if (lane == 0) red[wave][32] = m, red[wave][33] = l;
+                }
+                __syncthreads();
+                if (way != 0) continue;
 #pragma unroll
-    for (int k = 0; k < 256 / D; ++k) {
-        const float y = __builtin_amdgcn_exp2f(red[k][D] - ms);
-        num += y * red[k][f];
-        den += y * red[k][D + 1];
+                for (int k = 1; k < 4; ++k) add(red[k][32], red[k][33], *reinterpret_cast<const f4*>(&red[k][4 * lane]));
+            }
+            if (way != 0) continue;
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const int r = row0 + ri, tok = r / a.group, head = h * a.group + r % a.group;
+            *reinterpret_cast<u32x2*>(a.out + (size_t)(first + tok) * a.heads * D + head * D + f) =
+                u32x2{Elem<DT>::pack(v[0] * inv, v[1] * inv), Elem<DT>::pack(v[2] * inv, v[3] * inv)};
+        }
     }
-    const int r = row0 + ri, tok = r / a.group, head = g.h * a.group + r % a.group;
-    const uint32_t x = Elem<DT>::pack(num * (den == 0.0f ? 0.0f : 1.0f / den), 0.0f);
-    a.out[(size_t)(g.q.first + tok) * a.heads * D + head * D + f] = (uint16_t)x;
 }
 
 // ---- tile kernel ----------------------------------------------------------------------------------
@@ -563,7 +561,6 @@ template <int D> __device__ __forceinline__ int k_swizzle(int row) { return D ==
 template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
 
 constexpr int LEAST_KEY_TILES = 4;       // of a split
-constexpr float LAZY = 8.0f;             // a row's maximum is renewed once it has grown by 2^8: its sums are then at most 2^8 larger, and the weights exact all the same
 
 // The sequence of virtual tile v, or -1.  Every wave for itself: two rounds of 64 candidates.
 __device__ __forceinline__ int tile_sequence(const AttnArgs& a, int v)
@@ -902,7 +899,7 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
     if (paged && most <= 2 * STREAM_ROWS) p.stream_tiles = most <= STREAM_ROWS ? 1 : 2;
     else if (paged && n_seqs > 1 && group <= 2 * STREAM_ROWS) p.stream_tiles = group <= STREAM_ROWS ? 1 : 2;
     p.tile = !(paged && most <= 2 * STREAM_ROWS);
-    p.workers = 2 * cus;
+    p.workers = 4 * STREAM_WAVES * cus;
     p.tiles = (int)tile_bound(M, group, n_seqs);
     p.splits = 1;
     if (p.tile) {
@@ -912,7 +909,9 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
         if (wgs < slots) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / wgs, 16), key_tiles / LEAST_KEY_TILES));
     }
     const size_t d2 = (size_t)c.head_dim + 2;
-    if (p.stream_tiles) p.stream_floats = (size_t)2 * p.workers * STREAM_ROWS * p.stream_tiles * d2;
+    if (p.stream_tiles) p.stream_floats = (size_t)p.workers * (2 * STREAM_ROWS * p.stream_tiles * d2 + sizeof(Cut) / sizeof(float));
+    p.long_lists = (int64_t)n_seqs * c.n_kv_heads * 32 <= p.workers;
+    p.stream_rows = (int)std::min<int64_t>(STREAM_ROWS * p.stream_tiles, p.tile ? 2 * STREAM_ROWS : most);
     if (p.splits > 1) p.tile_floats = (size_t)p.tiles * c.n_kv_heads * p.splits * TILE_ROWS_Q * d2;
     return p;
 }
@@ -927,12 +926,13 @@ static hipError_t launch_attention(const AttentionPlan& p, AttnArgs a, float* pa
         a.rows_to = both ? 2 * STREAM_ROWS + 1 : INT32_MAX;
         a.workers = p.workers;
         a.part = p.stream_floats ? part : nullptr;
-        const unsigned grid = (unsigned)p.workers;
+        const unsigned grid = (unsigned)p.workers / 4, cuts = (unsigned)((p.workers + CUTS_PER_WG - 1) / CUTS_PER_WG);
 #define LPQ_STREAM(NT)                                                                                                  \
         do {                                                                                                            \
             if (alibi) stream_attention_kernel<DT, D, NT, true><<<grid, 256, 0, s>>>(a);                                \
             else       stream_attention_kernel<DT, D, NT, false><<<grid, 256, 0, s>>>(a);                               \
-            if (a.part) stream_combine_kernel<DT, D, NT><<<dim3(grid, STREAM_ROWS * NT), 256, 0, s>>>(a);               \
+            if (a.part && p.long_lists) stream_combine_kernel<DT, D, NT, true><<<dim3(cuts, (unsigned)p.stream_rows * (D / 32)), 256, 0, s>>>(a); \
+            else if (a.part) stream_combine_kernel<DT, D, NT, false><<<dim3(cuts, (unsigned)p.stream_rows), 256, 0, s>>>(a);             \
         } while (0)
         if (p.stream_tiles == 1) LPQ_STREAM(1);
         else LPQ_STREAM(2);

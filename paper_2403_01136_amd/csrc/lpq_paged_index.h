@@ -12,7 +12,7 @@ namespace lpq {
 
 enum { PAGED_MAX_SEQS = 2048,            // sequences of a call: the plan keeps four numbers of each in LDS
        STREAM_ROWS = 16,                 // rows (tokens x query heads of a K/V head) of a column tile of the streaming kernel
-       STREAM_BLOCK = 128,               // keys of its work unit: four waves, 32 each
+       STREAM_KEYS = 32,                 // keys of its work unit: a step of one wave
        TILE_ROWS_Q = 128, TILE_KEYS = 64 };  // rows of a workgroup of the tile kernel; keys of a step
 
 LPQ_BOTH int clamp_int(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -63,10 +63,10 @@ LPQ_BOTH KeySplit key_split(int tiles, int splits, int least, int sp)
     return k;
 }
 
-// ---- the streaming kernel's list: units of 128 keys, ordered sequence, K/V head, row tile, keys.  A sequence with rows but no keys has one unit per
+// ---- the streaming kernel's list: units of 32 keys, ordered sequence, K/V head, row tile, keys.  A sequence with rows but no keys has one unit per
 // row tile (its rows are set to zero).
 LPQ_BOTH int stream_row_tiles(int rows, int tile_rows) { return (rows + tile_rows - 1) / tile_rows; }
-LPQ_BOTH int stream_key_blocks(int ctx) { return ctx > STREAM_BLOCK ? (ctx + STREAM_BLOCK - 1) / STREAM_BLOCK : 1; }
+LPQ_BOTH int stream_key_steps(int ctx) { return ctx > STREAM_KEYS ? (ctx + STREAM_KEYS - 1) / STREAM_KEYS : 1; }
 // Unit at which worker w of W begins, out of `units`.
 LPQ_BOTH int64_t stream_begin(int64_t units, int w, int W) { return units / W * w + units % W * w / W; }
 // The worker that has unit u.

@@ -30,7 +30,7 @@ int64_t t_tile_bound(int M, int g, int n) { return tile_bound(M, g, n); }
 void t_key_split(int tiles, int splits, int least, int sp, int* out) { const KeySplit k = key_split(tiles, splits, least, sp); out[0] = k.begin; out[1] = k.end; out[2] = k.used; }
 int64_t t_stream_begin(int64_t u, int w, int W) { return stream_begin(u, w, W); }
 int t_stream_worker(int64_t units, int64_t u, int W) { return stream_worker(units, u, W); }
-int t_key_blocks(int ctx) { return stream_key_blocks(ctx); }
+int t_key_steps(int ctx) { return stream_key_steps(ctx); }
 }
 '''
 
@@ -85,7 +85,7 @@ def test_lengths(idx):
             assert k == min(max(kv, 0), pages << shift)
     assert [idx.t_token_position(10, 3, t) for t in range(3)] == [7, 8, 9]
     assert idx.t_token_position(2, 5, 0) == -3 and idx.t_token_position(-4, 5, 0) == -5
-    assert [idx.t_key_blocks(c) for c in (0, 1, 128, 129, 1 << 30)] == [1, 1, 1, 2, 1 << 23]
+    assert [idx.t_key_steps(c) for c in (0, 1, 32, 33, 1 << 30)] == [1, 1, 1, 2, 1 << 25]
 
 
 def test_every_row_tile_has_a_place(idx):
