@@ -215,7 +215,7 @@ struct AttentionPlan {
     int stream_tiles, stream_rows, workers;      // streaming kernel: column tiles of 16 rows (0: not launched), rows that a tile is expected to have, waves
     bool long_lists;                     // few row tiles, cut into many parts each
     bool tile;                           // tile kernel launched
-    int tiles, splits;                   // its virtual row tiles and K splits
+    int tiles, splits, least;            // its virtual row tiles, K splits at most and key tiles of one at least
     size_t stream_floats, tile_floats;   // partial results of either (0: whole row tiles only)
 };
 AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int M, int max_q, int max_kv, int cus);

@@ -54,7 +54,8 @@ struct AttnArgs {
     float* part;                         // partial results, or null: nothing is split
     int32_t n_seqs, M, heads, kv_heads, group, shift, n_pages, max_pages;
     int32_t rows_from, rows_to;          // sequences with rows_from <= rows < rows_to are this launch's
-    int32_t workers, splits, tiles;      // streaming: waves; tile kernel: K splits, virtual row tiles
+    int32_t workers;                     // streaming kernel: waves
+    int32_t splits, least, tiles;        // tile kernel: K splits at most, key tiles of one at least; virtual row tiles
 };
 
 // A sequence as a kernel sees it.
@@ -560,13 +561,13 @@ __global__ __launch_bounds__(256) void stream_combine_kernel(AttnArgs a)
 template <int D> __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
 template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
 
-constexpr int LEAST_KEY_TILES = 4;       // of a split
+constexpr int LEAST_KEY_TILES = 4, LONG_KEY_TILES = 48;      // of a split
 
 // The sequence of virtual tile v, or -1.  Every wave for itself: two rounds of 64 candidates.
 __device__ __forceinline__ int tile_sequence(const AttnArgs& a, int v)
 {
     const int lane = threadIdx.x & 63, stride = (a.n_seqs + 63) / 64;
-    auto begins = [&](int s) { return s < a.n_seqs && tile_start(clamp_int(a.cu_q[s], 0, a.M), a.group, s) <= v; };
+    auto begins = [&](int s) { return s < a.n_seqs && tile_start(clamp_int(a.cu_q[s], 0, a.M), a.group, s, TILE_ROWS_Q) <= v; };
     const int block = __popcll(__ballot(begins(lane * stride))) - 1;
     if (block < 0 || stride == 1) return block;
     return block * stride + __popcll(__ballot(lane < stride && begins(block * stride + lane))) - 1;
@@ -579,12 +580,79 @@ __device__ __forceinline__ bool tile_of(const AttnArgs& a, int v, Tile* t)
     const int s = __builtin_amdgcn_readfirstlane(tile_sequence(a, v));
     if (s < 0) return false;
     t->q = load_seq(a, s);
-    t->row0 = TILE_ROWS_Q * (v - tile_start(t->q.first, a.group, s));
+    t->row0 = TILE_ROWS_Q * (v - tile_start(t->q.first, a.group, s, TILE_ROWS_Q));
     if (!takes(a, t->q.rows) || t->row0 < 0 || t->row0 >= t->q.rows) return false;
     t->n_rows = min((int)TILE_ROWS_Q, t->q.rows - t->row0);
     t->key_end = max(0, min(t->q.ctx, t->q.pos0 + (t->row0 + t->n_rows - 1) / a.group + 1));
     t->key_tiles = max(1, (t->key_end + TILE_KEYS - 1) / TILE_KEYS);
     return true;
+}
+
+// Where a split leaves its sums ([rows][D], then maximum and sum of each row), or null: there is only one.
+template <int D>
+__device__ __forceinline__ float* tile_part(const AttnArgs& a, const KeySplit& ks, int h, int v, int split)
+{
+    return ks.used == 1 ? nullptr : a.part + (((size_t)h * a.tiles + v) * a.splits + split) * ((size_t)TILE_ROWS_Q * (D + 2));
+}
+
+// The results (part null) or sums of 32 rows of a tile from row wr on: a lane has row wr + lane % 32 = (tok, head) and its features 32 d + 8 i + 4 (lane / 32) +
+// 0 .. 3 in registers 4 i .. 4 i + 3 of o[d], the maximum m and the sum l.
+template <int DT, int D>
+__device__ __forceinline__ void store_rows(const AttnArgs& a, const Tile& tl, int h, const KeySplit& ks, float* part, const f16x (&o)[D / 32], float m, float l,
+                                           int wr, int tok, int head)
+{
+    constexpr int DTL = D / 32;
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, cols = (a.heads + 2 * a.kv_heads) * D;
+    const bool mine = wr + col < tl.n_rows;
+    float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};         // finite if all the lane's sums are
+#pragma unroll
+    for (int d = 0; d < DTL; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) total[i % 4] += o[d][i];
+    uint64_t again = __ballot(!__builtin_isfinite((total[0] + total[1]) + (total[2] + total[3])) && mine);
+    again = (again | again >> 32) & 0xffffffffu;       // rows to be done again: a bit per column, of either half
+    const bool store = mine && !(again >> col & 1);
+    float* const ml = part + (size_t)TILE_ROWS_Q * D;
+    if (part) {
+        if (store) {
+#pragma unroll
+            for (int d = 0; d < DTL; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f4*>(part + (size_t)(wr + col) * D + 32 * d + 2 * i + 4 * half) = f4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+            if (half == 0) *reinterpret_cast<f2*>(ml + 2 * (wr + col)) = f2{m, l};
+        }
+    } else {                                           // the halves trade so that each stores 16 bytes
+        uint16_t* const orow = a.out + (size_t)(tl.q.first + tok) * a.heads * D + head * D;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int d = 0; d < DTL; ++d)
+#pragma unroll
+            for (int b = 0; b < 4; b += 2) {
+                u32x4 x;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x2 t = __builtin_amdgcn_permlane32_swap(Elem<DT>::pack(o[d][4 * b + 2 * i] * inv, o[d][4 * b + 2 * i + 1] * inv),
+                                                                     Elem<DT>::pack(o[d][4 * b + 4 + 2 * i] * inv, o[d][4 * b + 5 + 2 * i] * inv), false, false);
+                    x[i] = t[0];
+                    x[2 + i] = t[1];
+                }
+                if (store) *reinterpret_cast<u32x4*>(orow + 8 * half + 32 * d + 8 * b) = x;
+            }
+    }
+    while (__builtin_expect(again != 0, 0)) {
+        const int k = __builtin_ctzll(again), rk = tl.row0 + wr + k, tk = rk / a.group, hk = h * a.group + rk % a.group;
+        again &= again - 1;
+        float wm, wl, acc[D / 64];
+        row_walk<DT, D>(a, tl.q, h, a.qkv + (size_t)(tl.q.first + tk) * cols + hk * D, tl.q.pos0 + tk, a.slopes ? a.slopes[hk] * LOG2E : 0.0f, TILE_KEYS * ks.begin,
+                        TILE_KEYS * ks.end, wm, wl, acc);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            if (part) part[(size_t)(wr + k) * D + 64 * i + lane] = acc[i];
+            else a.out[(size_t)(tl.q.first + tk) * a.heads * D + hk * D + 64 * i + lane] = (uint16_t)Elem<DT>::pack(acc[i] * (wl == 0.0f ? 0.0f : 1.0f / wl), 0.0f);
+        }
+        if (part && lane == 0) *reinterpret_cast<f2*>(ml + 2 * (wr + k)) = f2{wm, wl};
+    }
 }
 
 template <int DT, int D, bool ALIBI, bool PAGED>
@@ -595,18 +663,16 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
     constexpr int TILE_BYTES = TILE_KEYS * D * 2;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];          // K, K, V, V (dynamic: ahead of a read of a named array the compiler waits for every load into it)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    // (head, row tile, split) of this workgroup
+    // (head, split, row tile) of this workgroup: the last row tiles, with the longest walks, first
     const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
     const int per_xcd = a.kv_heads * classes / 8, per_class = (a.tiles + classes - 1) / classes;
     const int slot = (int)(blockIdx.x >> 3), combo = (int)(blockIdx.x & 7) + 8 * (slot % per_xcd), rest = slot / per_xcd;
-    const int h = combo % a.kv_heads, split = rest / per_class;
-    const int v = a.tiles - 1 - ((rest % per_class) * classes + combo / a.kv_heads);
-    if (v < 0) return;
+    const int h = combo % a.kv_heads, split = rest / per_class, v = a.tiles - 1 - ((rest % per_class) * classes + combo / a.kv_heads);
     Tile tl;
-    if (!tile_of(a, v, &tl)) return;
-    const Seq q = tl.q;
-    const KeySplit ks = key_split(tl.key_tiles, a.splits, LEAST_KEY_TILES, split);
+    if (v < 0 || !tile_of(a, v, &tl)) return;
+    const KeySplit ks = key_split(tl.key_tiles, a.splits, a.least, split);
     if (split >= ks.used) return;
+    const Seq& q = tl.q;
     const int cols = (a.heads + 2 * a.kv_heads) * D;
     const int wr0 = 32 * wave;                                                  // this wave's first row of the tile
     const bool active = wr0 < tl.n_rows;
@@ -690,6 +756,11 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
         va[d] = (uint32_t)(2 * TILE_BYTES + row * D * 2 + 16 * (chunk ^ v_swizzle<D>(row)) + 8 * (lane & 1));
     }
 
+    float near[ALIBI ? 16 : 1];                        // bias of a register's key within its 32
+    if constexpr (ALIBI)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) near[i] = slope * (float)(8 * (i / 4) + i % 4);
+
     if constexpr (PAGED) load_ids(ks.begin);
     uint32_t bad = 0, bad_next = fill(ks.begin, 0);
     for (int j = ks.begin; j < ks.end; ++j) {
@@ -736,13 +807,14 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
 #pragma unroll
         for (int k = 0; k < KS; ++k) s[1] = Elem<DT>::mfma32(rb[k], qf[k], k == 0 ? zero : s[1]);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (ALIBI) {                         // to base 2, with the linear bias
-            const float base = slope * (float)(j0 + 4 * half - p);
+        float base[2] = {0.0f, 0.0f};                  // bias of a 32-key tile's first key; the others' are in near[]
+        if constexpr (ALIBI)                           // to base 2, with the bias within the 32 keys
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < 2; ++kt) {
+                base[kt] = slope * (float)(j0 + 32 * kt + 4 * half - p);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[kt][i] = __builtin_fmaf(s[kt][i], c, __builtin_fmaf(slope, (float)(32 * kt + 8 * (i / 4) + i % 4), base));
-        }
+                for (int i = 0; i < 16; ++i) s[kt][i] = __builtin_fmaf(s[kt][i], c, near[i]);
+            }
         if (bad != 0 || j0 + TILE_KEYS > all_see) {    // some key of the tile is not for some row of the wave
             const int rel = min(p, tl.key_end - 1) - j0 - 4 * half;
 #pragma unroll
@@ -751,14 +823,14 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
                 for (int i = 0; i < 16; ++i)
                     s[kt][i] = 32 * kt + 8 * (i / 4) + i % 4 <= rel && !(bad >> (2 * kt + i / 8) & 1) ? s[kt][i] : -INFINITY;
         }
-        float mx = -INFINITY;
+        float mk[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
+            for (int i = 0; i < 16; ++i) mk[kt] = fmaxf(mk[kt], s[kt][i]);
+        float mx = ALIBI ? fmaxf(mk[0] + base[0], mk[1] + base[1]) : fmaxf(mk[0], mk[1]) * c;
         const f2 m2 = both_halves(mx);
         mx = fmaxf(m2[0], m2[1]);
-        if constexpr (!ALIBI) mx *= c;
         if (__any(mx > m + LAZY)) {
             const float mn = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
             m = mn;
@@ -778,8 +850,8 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
                 u32x4 x;
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e] - ms : __builtin_fmaf(s[kt][i + e], c, -ms));
-                    const float e1 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e + 1] - ms : __builtin_fmaf(s[kt][i + e + 1], c, -ms));
+                    const float e0 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e] + (base[kt] - ms) : __builtin_fmaf(s[kt][i + e], c, -ms));
+                    const float e1 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e + 1] + (base[kt] - ms) : __builtin_fmaf(s[kt][i + e + 1], c, -ms));
                     ls += e0;
                     ls += e1;
                     x[e / 2] = Elem<DT>::pack(e0, e1);
@@ -798,91 +870,47 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
     }
     if (!active) return;
     const f2 l2 = both_halves(l);
-    l = l2[0] + l2[1];
-    // the lane holds features 32 d + 8 a + 4 half + 0 .. 3 of its row; the halves trade so that each stores 16 bytes
-    const bool mine = wr0 + col < tl.n_rows;
-    float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};         // finite if all the lane's sums are
-#pragma unroll
-    for (int d = 0; d < DTL; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) total[i % 4] += o[d][i];
-    uint64_t again = __ballot(!__builtin_isfinite((total[0] + total[1]) + (total[2] + total[3])) && mine);
-    again = (again | again >> 32) & 0xffffffffu;       // rows to be done again: a bit per column, of either half
-    const bool store = mine && !(again >> col & 1);
-    float* const part = ks.used == 1 ? nullptr : a.part + (((size_t)h * a.tiles + v) * a.splits + split) * (TILE_ROWS_Q * (D + 2));
-    uint16_t* const orow = a.out + (size_t)(q.first + tok) * a.heads * D + head * D;
-    if (part) {
-        if (store) {
-#pragma unroll
-            for (int d = 0; d < DTL; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<f4*>(part + (size_t)(wr0 + col) * D + 32 * d + 2 * i + 4 * half) = f4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
-            if (half == 0) *reinterpret_cast<f2*>(part + TILE_ROWS_Q * D + 2 * (wr0 + col)) = f2{m, l};
-        }
-    } else {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-        for (int d = 0; d < DTL; ++d)
-#pragma unroll
-            for (int b = 0; b < 4; b += 2) {
-                u32x4 x;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const u32x2 t = __builtin_amdgcn_permlane32_swap(Elem<DT>::pack(o[d][4 * b + 2 * i] * inv, o[d][4 * b + 2 * i + 1] * inv),
-                                                                     Elem<DT>::pack(o[d][4 * b + 4 + 2 * i] * inv, o[d][4 * b + 5 + 2 * i] * inv), false, false);
-                    x[i] = t[0];
-                    x[2 + i] = t[1];
-                }
-                if (store) *reinterpret_cast<u32x4*>(orow + 8 * half + 32 * d + 8 * b) = x;
-            }
-    }
-    while (__builtin_expect(again != 0, 0)) {
-        const int k = __builtin_ctzll(again), rk = tl.row0 + wr0 + k, tk = rk / a.group, hk = h * a.group + rk % a.group;
-        again &= again - 1;
-        float wm, wl, acc[D / 64];
-        row_walk<DT, D>(a, q, h, a.qkv + (size_t)(q.first + tk) * cols + hk * D, q.pos0 + tk, ALIBI ? a.slopes[hk] * LOG2E : 0.0f, TILE_KEYS * ks.begin,
-                        TILE_KEYS * ks.end, wm, wl, acc);
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            if (part) part[(size_t)(wr0 + k) * D + 64 * i + lane] = acc[i];
-            else a.out[(size_t)(q.first + tk) * a.heads * D + hk * D + 64 * i + lane] = (uint16_t)Elem<DT>::pack(acc[i] * (wl == 0.0f ? 0.0f : 1.0f / wl), 0.0f);
-        }
-        if (part && lane == 0) *reinterpret_cast<f2*>(part + TILE_ROWS_Q * D + 2 * (wr0 + k)) = f2{wm, wl};
-    }
+    store_rows<DT, D>(a, tl, h, ks, tile_part<D>(a, ks, h, v, split), o, m, l2[0] + l2[1], wr0, tok, head);
 }
 
-// Adds up the splits of 16 rows (blockIdx.y) of a row tile and head (blockIdx.x), in order.
+// Adds up the splits of a row tile and head (blockIdx.x), in order: a thread has four features of a row, a workgroup 1024 / D rows (blockIdx.y).  The loads of four
+// splits are under way together.
 template <int DT, int D>
 __global__ __launch_bounds__(256) void tile_combine_kernel(AttnArgs a)
 {
+    constexpr int AHEAD = 4;
     const int h = (int)blockIdx.x / a.tiles, v = (int)blockIdx.x % a.tiles;
     Tile tl;
     if (!tile_of(a, v, &tl)) return;
-    const KeySplit ks = key_split(tl.key_tiles, a.splits, LEAST_KEY_TILES, 0);
-    if (ks.used == 1) return;
-    const float* base = a.part + ((size_t)h * a.tiles + v) * a.splits * (TILE_ROWS_Q * (D + 2));
-    for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
-        const int rr = 16 * (int)blockIdx.y + i / (D / 4), f = 4 * (i % (D / 4));
-        if (rr >= tl.n_rows) break;
-        float m = -INFINITY;
-        for (int k = 0; k < ks.used; ++k) m = fmaxf(m, base[(size_t)k * (TILE_ROWS_Q * (D + 2)) + TILE_ROWS_Q * D + 2 * rr]);
-        const float ms = m == -INFINITY ? 0.0f : m;
-        f4 num = {0.0f, 0.0f, 0.0f, 0.0f};
-        float den = 0.0f;
-#pragma unroll 4
-        for (int k = 0; k < ks.used; ++k) {
-            const float* ps = base + (size_t)k * (TILE_ROWS_Q * (D + 2));
-            const f2 ml = *reinterpret_cast<const f2*>(ps + TILE_ROWS_Q * D + 2 * rr);
-            const float w = __builtin_amdgcn_exp2f(ml[0] - ms);
-            den += w * ml[1];
-            num += w * *reinterpret_cast<const f4*>(ps + (size_t)rr * D + f);
+    const KeySplit ks = key_split(tl.key_tiles, a.splits, a.least, 0);
+    const int rr = (1024 / D) * (int)blockIdx.y + (int)threadIdx.x / (D / 4), f = 4 * ((int)threadIdx.x % (D / 4));
+    if (ks.used == 1 || rr >= tl.n_rows) return;
+    constexpr size_t SIZE = (size_t)TILE_ROWS_Q * (D + 2), ML = (size_t)TILE_ROWS_Q * D;
+    const float* base = a.part + ((size_t)h * a.tiles + v) * a.splits * SIZE;
+    float m = -INFINITY, l = 0.0f;
+    f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = 0; k0 < ks.used; k0 += AHEAD) {
+        f2 ml[AHEAD];
+        f4 o[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float* ps = base + min(k0 + k, ks.used - 1) * SIZE;
+            ml[k] = *reinterpret_cast<const f2*>(ps + ML + 2 * rr);
+            o[k] = *reinterpret_cast<const f4*>(ps + (size_t)rr * D + f);
         }
-        const float inv = den == 0.0f ? 0.0f : 1.0f / den;
-        const int r = tl.row0 + rr, tok = r / a.group, head = h * a.group + r % a.group;
-        const u32x2 x = {Elem<DT>::pack(num[0] * inv, num[1] * inv), Elem<DT>::pack(num[2] * inv, num[3] * inv)};
-        *reinterpret_cast<u32x2*>(a.out + (size_t)(tl.q.first + tok) * a.heads * D + head * D + f) = x;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (k0 + k >= ks.used) break;
+            const float mn = fmaxf(m, ml[k][0]), ms = mn == -INFINITY ? 0.0f : mn, x = __builtin_amdgcn_exp2f(m - ms), y = __builtin_amdgcn_exp2f(ml[k][0] - ms);
+            m = mn;
+            l = l * x + ml[k][1] * y;
+            sum = sum * x + o[k] * y;
+        }
     }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int r = tl.row0 + rr, tok = r / a.group, head = h * a.group + r % a.group;
+    const u32x2 x = {Elem<DT>::pack(sum[0] * inv, sum[1] * inv), Elem<DT>::pack(sum[2] * inv, sum[3] * inv)};
+    *reinterpret_cast<u32x2*>(a.out + (size_t)(tl.q.first + tok) * a.heads * D + head * D + f) = x;
 }
 
 }  // namespace
@@ -900,13 +928,17 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
     else if (paged && n_seqs > 1 && group <= 2 * STREAM_ROWS) p.stream_tiles = group <= STREAM_ROWS ? 1 : 2;
     p.tile = !(paged && most <= 2 * STREAM_ROWS);
     p.workers = 4 * STREAM_WAVES * cus;
-    p.tiles = (int)tile_bound(M, group, n_seqs);
+    p.tiles = (int)tile_bound(M, group, n_seqs, TILE_ROWS_Q);
     p.splits = 1;
     if (p.tile) {
-        // workgroups that have rows, two to a compute unit
+        // Workgroups that have rows, two to a compute unit: splits make one round of them, or two where the walks are long.  One round / two, us with the
+        // combining kernel: 512 tokens of 32 heads (8 K/V heads) behind 8000 positions 80 / 83, behind 30000 240 / 223; of 40 heads (40) behind 4000 52 / 62; two
+        // chunks of 512 beside 9 sequences that decode, 56 heads (8), up to 6000 positions 122 / 114.
         const int64_t wgs = std::max<int64_t>(1, ((int64_t)M * group + TILE_ROWS_Q - 1) / TILE_ROWS_Q) * c.n_kv_heads, slots = 2 * (int64_t)cus;
         const int64_t key_tiles = ((int64_t)max_kv + TILE_KEYS - 1) / TILE_KEYS;
-        if (wgs < slots) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(slots / wgs, 16), key_tiles / LEAST_KEY_TILES));
+        const int64_t fill = std::max<int64_t>(slots / wgs, std::min<int64_t>(2 * slots / wgs, key_tiles / LONG_KEY_TILES));
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({fill, 16, key_tiles / LEAST_KEY_TILES}));
+        p.least = (int)std::max<int64_t>(LEAST_KEY_TILES, (key_tiles + p.splits - 1) / p.splits);
     }
     const size_t d2 = (size_t)c.head_dim + 2;
     if (p.stream_tiles) p.stream_floats = (size_t)p.workers * (2 * STREAM_ROWS * p.stream_tiles * d2 + sizeof(Cut) / sizeof(float));
@@ -943,6 +975,7 @@ static hipError_t launch_attention(const AttentionPlan& p, AttnArgs a, float* pa
         a.rows_to = INT32_MAX;
         a.tiles = p.tiles;
         a.splits = p.splits;
+        a.least = p.least;
         a.part = part;
         const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
         const unsigned grid = (unsigned)(a.kv_heads * classes) * (unsigned)((p.tiles + classes - 1) / classes) * (unsigned)p.splits;
@@ -954,7 +987,7 @@ static hipError_t launch_attention(const AttentionPlan& p, AttnArgs a, float* pa
             if (alibi) tile_attention_kernel<DT, D, true, false><<<grid, 256, smem, s>>>(a);
             else       tile_attention_kernel<DT, D, false, false><<<grid, 256, smem, s>>>(a);
         }
-        if (p.splits > 1) tile_combine_kernel<DT, D><<<dim3((unsigned)(p.tiles * a.kv_heads), TILE_ROWS_Q / 16), 256, 0, s>>>(a);
+        if (p.splits > 1) tile_combine_kernel<DT, D><<<dim3((unsigned)(p.tiles * a.kv_heads), TILE_ROWS_Q * D / 1024), 256, 0, s>>>(a);
     }
     return hipGetLastError();
 }

@@ -45,10 +45,10 @@ LPQ_BOTH int keys_of(int kv_len, int max_pages, int page_shift)
 // The position of token t of q_len new ones; below zero where kv_len is less than q_len.
 LPQ_BOTH int token_position(int kv_len, int q_len, int t) { return (kv_len < 0 ? 0 : kv_len) - q_len + t; }
 
-// ---- the tile kernel's list: virtual tile v of 128 rows; sequence s starts at v = floor(first row * group / 128) + s, which leaves every
+// ---- the tile kernel's list: virtual tile v of tile_rows rows; sequence s starts at v = floor(first row * group / tile_rows) + s, which leaves every
 // sequence room for its tiles (and at most one more, which has no rows), whatever the lengths, without a prefix sum.
-LPQ_BOTH int tile_start(int first_row, int group, int s) { return (int)((int64_t)first_row * group / TILE_ROWS_Q) + s; }
-LPQ_BOTH int64_t tile_bound(int M, int group, int n_seqs) { return (int64_t)M * group / TILE_ROWS_Q + n_seqs; }
+LPQ_BOTH int tile_start(int first_row, int group, int s, int tile_rows) { return (int)((int64_t)first_row * group / tile_rows) + s; }
+LPQ_BOTH int64_t tile_bound(int M, int group, int n_seqs, int tile_rows) { return (int64_t)M * group / tile_rows + n_seqs; }
 // Key tiles [begin, end) of split `sp` out of `splits` for a row tile that sees `tiles` of them; used: splits that have any (at least one).
 struct KeySplit { int begin, end, used; };
 LPQ_BOTH KeySplit key_split(int tiles, int splits, int least, int sp)

@@ -25,8 +25,8 @@ int t_slot_checked(int s, int n, int shift) { return slot_checked(s, n, shift); 
 int64_t t_page_element(int p, int h, int kv, int shift, int d) { return page_element(p, h, kv, shift, d); }
 int t_keys_of(int kv, int mp, int shift) { return keys_of(kv, mp, shift); }
 int t_token_position(int kv, int q, int t) { return token_position(kv, q, t); }
-int t_tile_start(int f, int g, int s) { return tile_start(f, g, s); }
-int64_t t_tile_bound(int M, int g, int n) { return tile_bound(M, g, n); }
+int t_tile_start(int f, int g, int s, int rows) { return tile_start(f, g, s, rows); }
+int64_t t_tile_bound(int M, int g, int n, int rows) { return tile_bound(M, g, n, rows); }
 void t_key_split(int tiles, int splits, int least, int sp, int* out) { const KeySplit k = key_split(tiles, splits, least, sp); out[0] = k.begin; out[1] = k.end; out[2] = k.used; }
 int64_t t_stream_begin(int64_t u, int w, int W) { return stream_begin(u, w, W); }
 int t_stream_worker(int64_t units, int64_t u, int W) { return stream_worker(units, u, W); }
@@ -95,12 +95,13 @@ def test_every_row_tile_has_a_place(idx):
         lens = r.choice([0, 1, 2, 5, 16, 17, 127, 128, 129, 400], n)
         cu = np.concatenate([[0], np.cumsum(lens)])
         M = int(cu[-1] + r.integers(0, 5)) or 1
-        starts = [idx.t_tile_start(int(c), group, s) for s, c in enumerate(cu)]
-        assert all(b > a for a, b in zip(starts, starts[1:]))            # the search for a tile's sequence goes by this
-        for s in range(n):
-            tiles = -(-int(lens[s]) * group // 128)
-            assert tiles <= starts[s + 1] - starts[s] <= tiles + 1
-        assert starts[-1] <= idx.t_tile_bound(M, group, n)
+        for rows in (128, 256):
+            starts = [idx.t_tile_start(int(c), group, s, rows) for s, c in enumerate(cu)]
+            assert all(b > a for a, b in zip(starts, starts[1:]))        # the search for a tile's sequence goes by this
+            for s in range(n):
+                tiles = -(-int(lens[s]) * group // rows)
+                assert tiles <= starts[s + 1] - starts[s] <= tiles + 1
+            assert starts[-1] <= idx.t_tile_bound(M, group, n, rows)
 
 
 def test_splits_cover_the_keys_once(idx):
