@@ -348,52 +348,66 @@ def lpq_attention(qkv, state, n_seqs, T, pos0, out=None, stream=None):
 PagePlan = collections.namedtuple("PagePlan", "cu_q kv_lens slots positions counters info")
 
 
-def _on(device, **tensors):
-    """Each tensor (name=(tensor, dtype, dimensions)) is contiguous, of that type, and on the current CUDA device, where the kernels run."""
+def _device_of(t):
+    """Index of the current CUDA device, where the kernels run and t has to be."""
     import torch
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError("tensors must be on the current CUDA device")
-    for name, (t, dtype, dims) in tensors.items():
-        if t.dtype != dtype or t.dim() != dims or t.device != device or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous %d-D %s tensor on %s" % (name, dims, dtype, device))
+    return dev
+
+
+def _check_tensor(name, t, dtype, dims, dev):
+    if t.dtype is not dtype or t.dim() != dims or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %d-D %s tensor on CUDA device %d" % (name, dims, dtype, dev))
+
+
+def _stream_on(stream, dev):
+    """The stream's handle as an integer; the current one is asked for without a stream object, which costs more than the rest of a small call."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _attn_cfg(qkv, n_heads, n_kv_heads):
     import torch
-    if qkv.dtype not in (torch.float16, torch.bfloat16) or qkv.dim() != 2:
-        raise ValueError("qkv must be 2-D, fp16 or bf16")
-    heads = n_heads + 2 * n_kv_heads
-    if n_heads < 1 or n_kv_heads < 1 or qkv.shape[1] % heads:
-        raise ValueError("qkv has %d columns, not a multiple of %d heads" % (qkv.shape[1], heads))
-    return lpq_attn_cfg(n_heads, n_kv_heads, qkv.shape[1] // heads, LPQ_DT_FP16 if qkv.dtype == torch.float16 else LPQ_DT_BF16)
+    if qkv.dtype is not torch.float16 and qkv.dtype is not torch.bfloat16:
+        raise ValueError("qkv must be fp16 or bf16")
+    cols, heads = qkv.shape[1], n_heads + 2 * n_kv_heads
+    if n_heads < 1 or n_kv_heads < 1 or cols % heads:
+        raise ValueError("qkv has %d columns, not a multiple of %d heads" % (cols, heads))
+    return lpq_attn_cfg(n_heads, n_kv_heads, cols // heads, LPQ_DT_FP16 if qkv.dtype is torch.float16 else LPQ_DT_BF16)
 
 
 def _paged_cfg(qkv, k_pages, v_pages):
-    """(attention cfg, page size, pages): K and V pages are [n_pages][kv heads][page_size][head_dim]."""
-    _on(qkv.device, qkv=(qkv, qkv.dtype, 2), k_pages=(k_pages, qkv.dtype, 4), v_pages=(v_pages, qkv.dtype, 4))
-    n_pages, kv, page_size, d = k_pages.shape
-    if v_pages.shape != k_pages.shape:
+    """(device index, attention cfg, page size, pages): K and V pages are [n_pages][kv heads][page_size][head_dim]."""
+    dev, dtype = _device_of(qkv), qkv.dtype
+    _check_tensor("qkv", qkv, dtype, 2, dev)
+    _check_tensor("k_pages", k_pages, dtype, 4, dev)
+    _check_tensor("v_pages", v_pages, dtype, 4, dev)
+    n_pages, kv, page_size, d = shape = k_pages.shape
+    if v_pages.shape != shape:
         raise ValueError("k_pages and v_pages must have the same shape")
     cfg = _attn_cfg(qkv, qkv.shape[1] // max(d, 1) - 2 * kv, kv)
     if cfg.head_dim != d:
         raise ValueError("qkv's columns do not match the pages' heads")
-    return cfg, page_size, n_pages
+    return dev, cfg, page_size, n_pages
 
 
-def _out_and_slopes(qkv, cfg, out, alibi_slopes):
+def _out_and_slopes(qkv, cfg, out, alibi_slopes, dev):
     import torch
-    shape = (qkv.shape[0], cfg.n_heads * cfg.head_dim)
+    M, cols = qkv.shape[0], cfg.n_heads * cfg.head_dim
     if out is None:
-        out = torch.zeros(shape, dtype=qkv.dtype, device=qkv.device)          # rows that no sequence has stay as they are: zero
+        out = torch.zeros((M, cols), dtype=qkv.dtype, device=qkv.device)      # rows that no sequence has stay as they are: zero
     else:
-        _on(qkv.device, out=(out, qkv.dtype, 2))
-        if tuple(out.shape) != shape:
-            raise ValueError("out must be [%d][%d]" % shape)
-    if alibi_slopes is not None:
-        _on(qkv.device, alibi_slopes=(alibi_slopes, torch.float32, 1))
-        if alibi_slopes.shape[0] != cfg.n_heads:
-            raise ValueError("alibi_slopes must have a value per head")
-    return out, alibi_slopes.data_ptr() if alibi_slopes is not None else None
+        _check_tensor("out", out, qkv.dtype, 2, dev)
+        if out.shape[0] != M or out.shape[1] != cols:
+            raise ValueError("out must be [%d][%d]" % (M, cols))
+    if alibi_slopes is None:
+        return out, None
+    _check_tensor("alibi_slopes", alibi_slopes, torch.float32, 1, dev)
+    if alibi_slopes.shape[0] != cfg.n_heads:
+        raise ValueError("alibi_slopes must have a value per head")
+    return out, alibi_slopes.data_ptr()
 
 
 def lpq_paged_plan(past, q_lens, table, ring, counters, page_size, M, plan=None, stream=None):
@@ -401,32 +415,35 @@ def lpq_paged_plan(past, q_lens, table, ring, counters, page_size, M, plan=None,
     pool's, the first two updated in place.  plan: the outputs (PagePlan or a tuple in its order), of which kv_lens may be `past` and counters the pool's
     own; None allocates them.  -> PagePlan."""
     import torch
-    i32, n = torch.int32, past.shape[0]
+    i32, n, dev = torch.int32, past.shape[0], _device_of(past)
     if plan is None:
-        plan = PagePlan(*(torch.empty(m, dtype=i32, device=past.device) for m in (n + 1, n, M, M, 2, 4)))
-    plan = PagePlan(*plan)
-    _on(past.device, past=(past, i32, 1), q_lens=(q_lens, i32, 1), table=(table, i32, 2), ring=(ring, i32, 1), counters=(counters, i32, 1),
-        cu_q=(plan.cu_q, i32, 1), kv_lens=(plan.kv_lens, i32, 1), slots=(plan.slots, i32, 1), positions=(plan.positions, i32, 1),
-        new_counters=(plan.counters, i32, 1), info=(plan.info, i32, 1))
-    sizes = (q_lens.shape[0], table.shape[0], counters.shape[0], *(t.shape[0] for t in plan))
-    if sizes != (n, n, 2, n + 1, n, M, M, 2, 4):
-        raise ValueError("sizes of the plan's tensors do not match %d sequences and %d rows" % (n, M))
+        plan = [torch.empty(m, dtype=i32, device=past.device) for m in (n + 1, n, M, M, 2, 4)]
+    plan = cu_q, kv_lens, slots, positions, new_counters, info = PagePlan(*plan)
+    _check_tensor("table", table, i32, 2, dev)
+    for name, t, size in (("past", past, n), ("q_lens", q_lens, n), ("ring", ring, None), ("counters", counters, 2), ("cu_q", cu_q, n + 1), ("kv_lens", kv_lens, n),
+                          ("slots", slots, M), ("positions", positions, M), ("the plan's counters", new_counters, 2), ("info", info, 4)):
+        _check_tensor(name, t, i32, 1, dev)
+        if size is not None and t.shape[0] != size:
+            raise ValueError("%s must have %d elements" % (name, size))
+    if table.shape[0] != n:
+        raise ValueError("table must have %d rows" % n)
     p = lpq_page_pool(page_size, ring.shape[0], table.shape[1], table.data_ptr(), ring.data_ptr(), counters.data_ptr())
-    o = lpq_page_plan(plan.counters.data_ptr(), plan.cu_q.data_ptr(), plan.kv_lens.data_ptr(), plan.slots.data_ptr(), plan.positions.data_ptr(), plan.info.data_ptr())
-    _check(load_library().lpq_paged_plan(ctypes.byref(p), past.data_ptr(), q_lens.data_ptr(), n, M, ctypes.byref(o), _stream(stream)), "lpq_paged_plan")
+    o = lpq_page_plan(new_counters.data_ptr(), cu_q.data_ptr(), kv_lens.data_ptr(), slots.data_ptr(), positions.data_ptr(), info.data_ptr())
+    _check(load_library().lpq_paged_plan(p, past.data_ptr(), q_lens.data_ptr(), n, M, o, _stream_on(stream, dev)), "lpq_paged_plan")
     return plan
 
 
 def lpq_paged_append(qkv, k_pages, v_pages, slots, stream=None):
     """K and V of the rows of qkv ([M][(heads + 2 kv heads) * d], fp16 or bf16) into their slots of the pages ([n_pages][kv heads][page_size][d])."""
     import torch
-    cfg, page_size, n_pages = _paged_cfg(qkv, k_pages, v_pages)
-    _on(qkv.device, slots=(slots, torch.int32, 1))
-    if slots.shape[0] != qkv.shape[0]:
+    dev, cfg, page_size, n_pages = _paged_cfg(qkv, k_pages, v_pages)
+    _check_tensor("slots", slots, torch.int32, 1, dev)
+    M = qkv.shape[0]
+    if slots.shape[0] != M:
         raise ValueError("slots must have a value per row")
     p = lpq_page_pool(page_size, n_pages, 0, None, None, None)
-    _check(load_library().lpq_paged_append(qkv.data_ptr(), ctypes.byref(cfg), ctypes.byref(p), k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr(),
-                                           qkv.shape[0], _stream(stream)), "lpq_paged_append")
+    _check(load_library().lpq_paged_append(qkv.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr(), M, _stream_on(stream, dev)),
+           "lpq_paged_append")
 
 
 def lpq_paged_attention(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None, max_kv=None, alibi_slopes=None, out=None, stream=None):
@@ -434,29 +451,32 @@ def lpq_paged_attention(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None,
     [n_seqs] (new tokens included).  max_q, max_kv: the most to expect (None: the batch, the table).  -> out [M][heads * d]."""
     import torch
     i32 = torch.int32
-    cfg, page_size, n_pages = _paged_cfg(qkv, k_pages, v_pages)
-    _on(qkv.device, table=(table, i32, 2), cu_q=(cu_q, i32, 1), kv_lens=(kv_lens, i32, 1))
-    n, M = kv_lens.shape[0], qkv.shape[0]
+    dev, cfg, page_size, n_pages = _paged_cfg(qkv, k_pages, v_pages)
+    _check_tensor("table", table, i32, 2, dev)
+    _check_tensor("cu_q", cu_q, i32, 1, dev)
+    _check_tensor("kv_lens", kv_lens, i32, 1, dev)
+    n, M, width = kv_lens.shape[0], qkv.shape[0], table.shape[1]
     if cu_q.shape[0] != n + 1 or table.shape[0] != n:
         raise ValueError("table, cu_q and kv_lens do not have the same number of sequences")
-    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes)
-    p = lpq_page_pool(page_size, n_pages, table.shape[1], table.data_ptr(), None, None)
-    _check(load_library().lpq_paged_attention(qkv.data_ptr(), ctypes.byref(cfg), ctypes.byref(p), k_pages.data_ptr(), v_pages.data_ptr(), slopes, cu_q.data_ptr(),
-                                              kv_lens.data_ptr(), n, M, M if max_q is None else int(max_q),
-                                              table.shape[1] * page_size if max_kv is None else int(max_kv), out.data_ptr(), _stream(stream)),
-           "lpq_paged_attention")
+    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes, dev)
+    p = lpq_page_pool(page_size, n_pages, width, table.data_ptr(), None, None)
+    _check(load_library().lpq_paged_attention(qkv.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), slopes, cu_q.data_ptr(), kv_lens.data_ptr(), n, M,
+                                              M if max_q is None else max_q, width * page_size if max_kv is None else max_kv, out.data_ptr(),
+                                              _stream_on(stream, dev)), "lpq_paged_attention")
     return out
 
 
 def lpq_packed_attention(qkv, cu_q, n_heads, n_kv_heads, max_q=None, alibi_slopes=None, out=None, stream=None):
     """Causal attention of whole prompts, packed in the rows of qkv, over themselves; cu_q int32 [n_seqs + 1].  -> out [M][heads * d]."""
     import torch
+    dev = _device_of(qkv)
+    _check_tensor("qkv", qkv, qkv.dtype, 2, dev)
     cfg = _attn_cfg(qkv, n_heads, n_kv_heads)
-    _on(qkv.device, qkv=(qkv, qkv.dtype, 2), cu_q=(cu_q, torch.int32, 1))
-    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes)
+    _check_tensor("cu_q", cu_q, torch.int32, 1, dev)
+    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes, dev)
     M = qkv.shape[0]
-    _check(load_library().lpq_packed_attention(qkv.data_ptr(), ctypes.byref(cfg), slopes, cu_q.data_ptr(), cu_q.shape[0] - 1, M,
-                                               M if max_q is None else int(max_q), out.data_ptr(), _stream(stream)), "lpq_packed_attention")
+    _check(load_library().lpq_packed_attention(qkv.data_ptr(), cfg, slopes, cu_q.data_ptr(), cu_q.shape[0] - 1, M, M if max_q is None else max_q, out.data_ptr(),
+                                               _stream_on(stream, dev)), "lpq_packed_attention")
     return out
 
 
