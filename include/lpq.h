@@ -322,8 +322,8 @@ typedef struct {
  * positions behind max_pages * page_size, or its and its predecessors' needs exceed the free pages: it gets no page, its rows no slots, its kv_lens stays
  * at `past`, and the caller may plan it again later.  Negative past counts as 0, counters are taken into their range.
  * With in-place counters and kv_lens a step is the same call every time and can be replayed from a graph.  The other outputs must not overlap the
- * inputs.  n_seqs <= 2048.  M > 6144 uses n_seqs words of the library's workspace.
- * Errors: NULL, SHAPE (page_size, counts, limits above), ALIGN (4 bytes), BUFSIZE, DEVICE. */
+ * inputs.  n_seqs <= 2048.  M > 6144 uses n_seqs words of the library's workspace, if a reservation leaves room for them.
+ * Errors: NULL, SHAPE (page_size, counts, limits above), ALIGN (4 bytes), DEVICE. */
 lpq_status lpq_paged_plan(const lpq_page_pool *pool, const int32_t *past, const int32_t *q_lens, int32_t n_seqs, int32_t M,
                           const lpq_page_plan *plan, void *hip_stream);
 
@@ -339,7 +339,7 @@ lpq_status lpq_paged_append(const void *qkv, const lpq_attn_cfg *cfg, const lpq_
  * nothing (or only scores of minus infinity) gives zero.  Values at masked places, infinite or NaN, do not touch the result.
  * alibi_slopes: fp32 [n_heads] or NULL.  q_s may be 1 (decode), a chunk, a whole prompt, 0, and differ from sequence to sequence.
  * max_q, max_kv: the largest q_s and kv_lens the caller expects; they choose kernels and splits, and larger ones than that are only slower.
- * Partial results are kept in the library's workspace; where a reservation leaves no room the work is not split.
+ * Partial results are kept in the library's workspace; where a reservation leaves no room the work is not split.  out must not overlap qkv.
  * Errors: NULL, SHAPE (as above, n_seqs in 1 .. 2048, max_q, max_kv < 1), UNSUPPORTED (dtype), ALIGN, DEVICE. */
 lpq_status lpq_paged_attention(const void *qkv, const lpq_attn_cfg *cfg, const lpq_page_pool *pool, const void *k_pages, const void *v_pages,
                                const float *alibi_slopes, const int32_t *cu_q, const int32_t *kv_lens, int32_t n_seqs, int32_t M,

@@ -135,6 +135,10 @@ __device__ __forceinline__ void row_walk(const AttnArgs& a, const Seq& q, int h,
 #pragma unroll
             for (int i = 0; i < D / 64; ++i) acc[i] = __builtin_fmaf(wu, (float)__builtin_bit_cast(T, vr[64 * i + lane]), acc[i]);
         }
+        bool rest = false;                             // a NaN in every feature stays: inputs that are NaN throughout are not walked to their end
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) rest |= acc[i] == acc[i];
+        if (!__any(rest)) break;
     }
     l = group_reduce<64>(l, OpAdd());
 }
@@ -917,6 +921,9 @@ __global__ __launch_bounds__(256) void tile_combine_kernel(AttnArgs a)
 
 // ---- host ------------------------------------------------------------------------------------------
 
+// Room that the tile kernel's parts may take: its list has a place for each sequence, also for those that the streaming kernel does.
+constexpr size_t MAX_PART_BYTES = (size_t)256 << 20;
+
 // What a call launches: the streaming kernel, the tile kernel or, where a batch may have sequences of both kinds, both.
 AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int M, int max_q, int max_kv, int cus)
 {
@@ -938,6 +945,8 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
         const int64_t key_tiles = ((int64_t)max_kv + TILE_KEYS - 1) / TILE_KEYS;
         const int64_t fill = std::max<int64_t>(slots / wgs, std::min<int64_t>(2 * slots / wgs, key_tiles / LONG_KEY_TILES));
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({fill, 16, key_tiles / LEAST_KEY_TILES}));
+        const size_t split_bytes = (size_t)p.tiles * c.n_kv_heads * TILE_ROWS_Q * (c.head_dim + 2) * sizeof(float);
+        p.splits = (int)std::max<size_t>(1, std::min<size_t>(p.splits, MAX_PART_BYTES / split_bytes));
         p.least = (int)std::max<int64_t>(LEAST_KEY_TILES, (key_tiles + p.splits - 1) / p.splits);
     }
     const size_t d2 = (size_t)c.head_dim + 2;

@@ -467,6 +467,19 @@ def test_later_tokens_do_not_matter(q, val):
     assert not bool(torch.isfinite(out[q - 1]).any())
 
 
+def test_nan_throughout():
+    """A batch whose values, or queries, are NaN everywhere: NaN everywhere, and no row is walked to its end on the way."""
+    import torch
+    for where in ("v", "qkv"):
+        p = Paged([(2000, 900), (700, 3), (50, 1)], 8, 2, 128, 64, "bf16")
+        getattr(p, where).fill_(math.nan)
+        out = torch.zeros((p.M, 8 * 128), dtype=torch.bfloat16, device="cuda")
+        lpq.lpq_paged_attention(p.qkv, p.k, p.v, ints(p.table), ints(p.cu), ints([a + b for a, b in p.seqs]), max_q=900, out=out)
+        assert bool(torch.isnan(out).all())
+    out = lpq.lpq_packed_attention(torch.full((2500, 12 * 64), math.nan, dtype=torch.float16, device="cuda"), ints([0, 2400, 2500]), 8, 2)
+    assert bool(torch.isnan(out).all())
+
+
 def test_large_scores():
     """Scores in the thousands: one key takes all; and all scores equal."""
     import torch

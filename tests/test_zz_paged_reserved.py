@@ -1,0 +1,35 @@
+"""The paged operators where a reservation leaves no room for parts: nothing is split, the results are as exact.  A process of its own, because a
+reservation holds until the process ends."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+CHILD = r'''
+import random
+import sys
+sys.path.insert(0, %r), sys.path.insert(0, %r)
+import paper_2403_01136_amd as lpq
+import test_gpu_paged as t
+lpq.load_library()
+lpq.lpq_workspace_reserve(1024)
+size = lpq.lpq_workspace_bytes()
+t.check_attention(*t.Paged([(5000, 1), (30, 1), (0, 1), (777, 1)], 8, 2, 128, 16, "fp16", 2).run(max_q=1), what="decode")
+t.check_attention(*t.Paged([(2000, 3), (31, 4)], 10, 2, 64, 32, "bf16").run(True, max_q=4), what="two column tiles")
+t.check_attention(*t.Paged([(3000, 100)], 8, 2, 128, 64, "fp16").run(max_q=100), what="chunk")
+t.check_attention(*t.Paged([(900, 1), (2100, 200), (17, 1)], 8, 8, 64, 16, "bf16", 5).run(max_q=200), what="mixed")
+t.check_attention(*t.packed_run([1100, 60], 2, 1, 128, "fp16", True), what="packed")
+r = random.Random(1)
+t.check_plan(t.plan_case(5, 300, 32, lambda r: r.choice((1, 80)), 300, 4), 32)
+assert lpq.lpq_workspace_bytes() == size, "the workspace has grown"
+print("RESERVED OK")
+'''
+
+
+def test_no_room_for_parts():
+    out = subprocess.run([sys.executable, "-c", CHILD % (os.path.dirname(HERE), HERE)], capture_output=True, text=True, timeout=110)
+    assert out.returncode == 0 and "RESERVED OK" in out.stdout, out.stdout[-2000:] + out.stderr[-4000:]
