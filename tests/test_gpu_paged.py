@@ -3,7 +3,9 @@ plain 64-bit implementations, at the sizes, layouts and masks where they can go 
 
 Tolerance of an attention output, element by element.  With weights w_j (summing to 1), A = sum w_j |v_j| and u half a step of the output's type
 (2^-11 fp16, 2^-8 bf16):
-  * the weights are rounded to that type ahead of their product:                          u A
+  * the weights are rounded to that type, in the products and in the sum that divides them: w_j (1 + d_j) with |d_j| <= u gives
+    sum w_j (1 + d_j) v_j / sum w_j (1 + d_j) = (out + sum w_j d_j v_j) / (1 + sum w_j d_j), off by                             u A + u |out|
+    to first order; a weight below fp16's normal range by half its smallest step instead, beside a sum of at least 1:       n 2^-25 max |v|
   * a weight exp2(s) has the error of its exponent: the score is a 32-bit sum of D products of 16-bit numbers ((D + 4) 2^-24 sum |q_i k_i|),
     scaled, biased and shifted by the row's maximum in 32 bits (3 roundings of at most 2^-24 (|s| + |max|)), and exp2 itself 2^-22;
     the error counts for the weight and for the sum it is divided by:                     2 (ln 2 * that + 2^-22) A
@@ -204,8 +206,8 @@ def test_append_bit_exact(H, KV, d, P, M, dt):
 # ---- attention --------------------------------------------------------------------------------------------------------
 
 def attention_ref(q, k, v, ok, pos, slopes):
-    """q [T][H][d], k, v [L][KV][d] (any values where ok is false), ok [L], pos [T] -> (out [T][H][d], bound without the output's rounding and the weights')
-    in 64 bits; per head."""
+    """q [T][H][d], k, v [L][KV][d] (any values where ok is false), ok [L], pos [T] -> (out [T][H][d], A, bound without the output's rounding and the weights'
+    relative one) in 64 bits; per head."""
     import torch
     T, H, d = q.shape
     L, KV = k.shape[0], k.shape[1]
@@ -242,6 +244,8 @@ def attention_ref(q, k, v, ok, pos, slopes):
         fin = lambda x: torch.where(torch.isfinite(x), x, torch.zeros_like(x))
         arg = ((d + 4) * mag * lg + 3 * (fin(s).abs() * lg + fin(top).abs() * lg)) * 2.0**-24
         E[:, h] = (w * (2 * (math.log(2) * torch.where(vis, arg, torch.zeros_like(arg)).amax(1, keepdim=True) + 2.0**-22) + 2 * L * 2.0**-24)) @ vz.abs()
+        if q.dtype == torch.float16:
+            E[:, h] += L * 2.0**-25 * vz.abs().amax()
     return out, A, E
 
 
@@ -257,7 +261,7 @@ def check_attention(got, parts, what=""):
         g = got[r0:r1].double().view(out.shape)
         nan = torch.isnan(out)
         assert torch.equal(torch.isnan(g), nan), what + ": NaN at other places"
-        tol = u * A + E + u * (out.abs() + u * A + E) + 2.0**-25
+        tol = u * (A + out.abs()) + E + u * (out.abs() + u * A + E) + 2.0**-25
         far = torch.where(nan, torch.zeros_like(out), (g - out).abs() / tol)
         assert float(far.max()) <= 1.0, "%s: rows %d..%d, %.2f of the bound at %s" % (what, r0, r1, float(far.max()), np.unravel_index(int(far.argmax()), far.shape))
     assert bool((got[left] == 77).all()), what + ": rows behind the last sequence"
