@@ -66,19 +66,20 @@ struct Seq {
     int s, first, len, rows;             // rows of the batch [first, first + len); rows = len * group
     int pos0, ctx;                       // position of its first new token; keys that exist
 };
-__device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s)
+__device__ __forceinline__ Seq make_seq(const AttnArgs& a, int s, int cu0, int cu1, int kv_len)
 {
-    const RowSpan r = row_span(a.cu_q[s], a.cu_q[s + 1], a.M);
+    const RowSpan r = row_span(cu0, cu1, a.M);
     Seq q;
     q.s = s;
     q.first = r.first;
     q.len = r.end - r.first;
     q.rows = q.len * a.group;
-    const int kv = a.kv_lens ? a.kv_lens[s] : q.len;
+    const int kv = a.kv_lens ? kv_len : q.len;
     q.pos0 = token_position(kv, q.len, 0);
     q.ctx = a.kv_lens ? keys_of(kv, a.max_pages, a.shift) : q.len;
     return q;
 }
+__device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s) { return make_seq(a, s, a.cu_q[s], a.cu_q[s + 1], a.kv_lens ? a.kv_lens[s] : 0); }
 __device__ __forceinline__ bool takes(const AttnArgs& a, int rows) { return rows > 0 && rows >= a.rows_from && rows < a.rows_to; }
 
 __device__ __forceinline__ int page_of_group(const AttnArgs& a, int s, int g)
@@ -566,24 +567,33 @@ template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D ==
 constexpr float LAZY = 8.0f;
 constexpr int LEAST_KEY_TILES = 4, LONG_KEY_TILES = 48;      // of a split
 
-// The sequence of virtual tile v, or -1.  Every wave for itself: two rounds of 64 candidates.
-__device__ __forceinline__ int tile_sequence(const AttnArgs& a, int v)
+// The sequence of virtual tile v: false if it is nobody's.  Every wave for itself.  Up to 63 sequences: one load of every lane's has all that is needed.
+// More: two rounds of 64 candidates, then the one found.
+__device__ __forceinline__ bool tile_sequence(const AttnArgs& a, int v, Seq* q)
 {
-    const int lane = threadIdx.x & 63, stride = (a.n_seqs + 63) / 64;
-    auto begins = [&](int s) { return s < a.n_seqs && tile_start(clamp_int(a.cu_q[s], 0, a.M), a.group, s, TILE_ROWS_Q) <= v; };
-    const int block = __popcll(__ballot(begins(lane * stride))) - 1;
-    if (block < 0 || stride == 1) return block;
-    return block * stride + __popcll(__ballot(lane < stride && begins(block * stride + lane))) - 1;
+    const int lane = threadIdx.x & 63;
+    auto begins = [&](int cu, int s) { return s < a.n_seqs && tile_start(clamp_int(cu, 0, a.M), a.group, s, TILE_ROWS_Q) <= v; };
+    if (a.n_seqs < 64) {
+        const int cu = a.cu_q[min(lane, a.n_seqs)], kv = a.kv_lens ? a.kv_lens[min(lane, a.n_seqs - 1)] : 0;
+        const int s = __popcll(__ballot(begins(cu, lane))) - 1;
+        if (s >= 0) *q = make_seq(a, s, __builtin_amdgcn_readlane(cu, s), __builtin_amdgcn_readlane(cu, s + 1), __builtin_amdgcn_readlane(kv, s));
+        return s >= 0;
+    }
+    auto begins_at = [&](int s) { return s < a.n_seqs && begins(a.cu_q[s], s); };
+    const int stride = (a.n_seqs + 63) / 64, block = __popcll(__ballot(begins_at(lane * stride))) - 1;
+    if (block < 0) return false;
+    const int s = block * stride + __popcll(__ballot(lane < stride && begins_at(block * stride + lane))) - 1;
+    if (s < 0) return false;
+    *q = load_seq(a, __builtin_amdgcn_readfirstlane(s));
+    return true;
 }
 
 // What a workgroup of the tile kernel, or of its combining kernel, is about.
 struct Tile { Seq q; int row0, n_rows, key_end, key_tiles; };
 __device__ __forceinline__ bool tile_of(const AttnArgs& a, int v, Tile* t)
 {
-    const int s = __builtin_amdgcn_readfirstlane(tile_sequence(a, v));
-    if (s < 0) return false;
-    t->q = load_seq(a, s);
-    t->row0 = TILE_ROWS_Q * (v - tile_start(t->q.first, a.group, s, TILE_ROWS_Q));
+    if (!tile_sequence(a, v, &t->q)) return false;
+    t->row0 = TILE_ROWS_Q * (v - tile_start(t->q.first, a.group, t->q.s, TILE_ROWS_Q));
     if (!takes(a, t->q.rows) || t->row0 < 0 || t->row0 >= t->q.rows) return false;
     t->n_rows = min((int)TILE_ROWS_Q, t->q.rows - t->row0);
     t->key_end = max(0, min(t->q.ctx, t->q.pos0 + (t->row0 + t->n_rows - 1) / a.group + 1));
@@ -664,6 +674,7 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
     typedef typename Elem<DT>::v8 V8;
     constexpr int CH = D / 8, KS = D / 16, DTL = D / 32, ROWS = 512 / D, FILLS = 16 / ROWS;       // chunks of a row; feature steps; feature tiles; keys per load; loads of a wave's 16 keys
     constexpr int TILE_BYTES = TILE_KEYS * D * 2;
+    constexpr bool BACKWARD = ALIBI;                   // biases grow towards the diagonal: from there on the first tiles have the maximum
     extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];          // K, K, V, V (dynamic: ahead of a read of a named array the compiler waits for every load into it)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     // (head, split, row tile) of this workgroup: the last row tiles, with the longest walks, first
@@ -686,11 +697,11 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
     const int my_end = active ? min(ks.end, (max(0, min(q.ctx, q.pos0 + (tl.row0 + min(wr0 + 31, tl.n_rows - 1)) / a.group + 1)) + TILE_KEYS - 1) / TILE_KEYS) : 0;
 
     // fills: this wave brings keys 16 wave .. 16 wave + 15 of a tile, of one page
-    int ids = 0, ids_from = ks.begin;
+    int ids = 0, ids_from = 0;
     uint64_t bad_ids = 0;
-    auto load_ids = [&](int j) {
-        ids_from = j;
-        const int g = 4 * j + lane;
+    auto load_ids = [&](int j) {                       // of 16 tiles, j and those that come behind it
+        ids_from = BACKWARD ? max(j - 15, 0) : j;
+        const int g = 4 * ids_from + lane;
         ids = 16 * g < tl.key_end ? page_of_group(a, q.s, g) : -1;
         bad_ids = __ballot(ids < 0);
     };
@@ -701,7 +712,7 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
         uint8_t *ks_ = smem_raw + buf * TILE_BYTES + 16 * wave * D * 2, *vs_ = ks_ + 2 * TILE_BYTES;
         uint32_t bad = 0;
         if constexpr (PAGED) {
-            if (j - ids_from >= 16) load_ids(j);
+            if ((uint32_t)(j - ids_from) >= 16u) load_ids(j);
             const int id = max(__builtin_amdgcn_readlane(ids, 4 * (j - ids_from) + wave), 0);
             bad = (uint32_t)(bad_ids >> (4 * (j - ids_from))) & 15u;
             const size_t at = (size_t)page_element(id, h, a.kv_heads, a.shift, D) + (size_t)((TILE_KEYS * j + 16 * wave) & ((1 << a.shift) - 1)) * D;
@@ -764,10 +775,11 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) near[i] = slope * (float)(8 * (i / 4) + i % 4);
 
-    if constexpr (PAGED) load_ids(ks.begin);
-    uint32_t bad = 0, bad_next = fill(ks.begin, 0);
-    for (int j = ks.begin; j < ks.end; ++j) {
-        const int buf = (j - ks.begin) & 1, j0 = TILE_KEYS * j;
+    const int tiles = ks.end - ks.begin, j_first = BACKWARD ? ks.end - 1 : ks.begin;
+    if constexpr (PAGED) load_ids(j_first);
+    uint32_t bad = 0, bad_next = fill(j_first, 0);
+    for (int n = 0; n < tiles; ++n) {
+        const int j = BACKWARD ? j_first - n : j_first + n, buf = n & 1, j0 = TILE_KEYS * j;
         bad = bad_next;
         __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): this wave's part of tile j has landed
         if (bad != 0 || j0 + TILE_KEYS > tl.key_end) { // values of keys that no row sees: zero, like their weights
@@ -777,8 +789,8 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
                 if ((bad >> wave & 1) || j0 + row >= tl.key_end) *reinterpret_cast<u32x4*>(smem_raw + 2 * TILE_BYTES + buf * TILE_BYTES + (16 * wave + ROWS * i) * D * 2 + 16 * lane) = u32x4{};
             }
         }
-        __syncthreads();                               // everybody's part has landed, and tile j - 1 is no longer read
-        if (j + 1 < ks.end) bad_next = fill(j + 1, buf ^ 1);
+        __syncthreads();                               // everybody's part has landed, and the tile before is no longer read
+        if (n + 1 < tiles) bad_next = fill(BACKWARD ? j - 1 : j + 1, buf ^ 1);
         if (j >= my_end) continue;
         // Operands are read a batch ahead of the matrix instructions that take them, and the wait for a batch stands ahead of the next batch's issue:
         // with global-to-LDS loads under way the compiler waits for every LDS read at each use.
