@@ -279,7 +279,7 @@ lpq_status lpq_decoder_layer(const lpq_layer *layer, const lpq_layer_cfg *cfg, c
 
 /* ---- Batches of sequences of different lengths: paged caches and packed rows ---------------------------------
  * A server's step has n_seqs sequences, sequence s with q_s >= 0 new tokens behind the positions it has cached.  The rows of all of
- * them are packed: rows cu_q[s] .. cu_q[s + 1] - 1 of a batch of M rows are sequence s's; rows from cu_q[n_seqs] on belong to nobody (a
+ * them are packed: rows cu_q[s] .. cu_q[s + 1] - 1 of a batch of M rows are sequence s's (cu_q does not decrease); rows from cu_q[n_seqs] on belong to nobody (a
  * batch may be padded to a fixed M, as a captured graph needs it) and their outputs are left as they were.  All lengths, offsets, slots and tables are
  * int32 DEVICE arrays: a step can be planned, appended and attended to without the host knowing a length.
  * K and V live in a pool of pages that a layer's two buffers hold: k_pages, v_pages [n_pages][n_kv_heads][page_size][head_dim], 16-bit
