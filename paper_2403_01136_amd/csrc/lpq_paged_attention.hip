@@ -268,9 +268,17 @@ __global__ __launch_bounds__(256, STREAM_WAVES) void stream_attention_kernel(Att
     int64_t s_units = u < share.end ? seq_units(a, s, TILE_ROWS) : 0;
 
     while (u < share.end) {
-        while (u >= s_begin + s_units) {               // the next sequence with units: there is one, u is below the total
+        if (u >= s_begin + s_units) {                  // the next sequence with units, 64 looked at together: there is one, u is below the total
             s_begin += s_units;
-            s_units = seq_units(a, ++s, TILE_ROWS);
+            uint64_t found = 0;
+            int64_t mine = 0;
+            for (++s; !found; s += found ? 0 : 64) {
+                mine = seq_units(a, s + lane, TILE_ROWS);
+                found = __ballot(mine > 0);
+            }
+            const int k = __builtin_ctzll(found);
+            s = __builtin_amdgcn_readfirstlane(s + k);
+            s_units = uniform64(shfl64(mine, k));
         }
         const Seq q = load_seq(a, s);
         const int steps = stream_key_steps(q.ctx), tiles = stream_row_tiles(q.rows, TILE_ROWS);
@@ -565,7 +573,8 @@ template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D ==
 // log2 of what a row's maximum may lag behind its largest score: sums are then at most 2^8 larger.  Renewed with every larger score there is hardly a
 // tile without 32 rows' sums being multiplied: one prompt of 5801 tokens 684 us, so 655; its error in bf16 1.9e-3, so 2.1e-3; in fp16 2.2e-4 and 2.3e-4.
 constexpr float LAZY = 8.0f;
-constexpr int LEAST_KEY_TILES = 4, LONG_KEY_TILES = 48;      // of a split
+// Of a split.  At least 4 / 8 key tiles, us: 64 tokens behind 6000 positions 23 + 9 / 22 + 7, 512 tokens of 16 heads over 2 behind 4000 32 + 9 / 30 + 7; 16: 33 + 5 both.
+constexpr int LEAST_KEY_TILES = 8, LONG_KEY_TILES = 48;
 
 // The sequence of virtual tile v: false if it is nobody's.  Every wave for itself.  Up to 63 sequences: one load of every lane's has all that is needed.
 // More: two rounds of 64 candidates, then the one found.
@@ -959,7 +968,8 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
     }
     const size_t d2 = (size_t)c.head_dim + 2;
     if (p.stream_tiles) p.stream_floats = (size_t)p.workers * (2 * STREAM_ROWS * p.stream_tiles * d2 + sizeof(Cut) / sizeof(float));
-    p.long_lists = (int64_t)n_seqs * c.n_kv_heads * 32 <= p.workers;
+    // lists of 32 parts and more, where the walks are long enough to be cut that often (4 sequences of up to 800 positions: long lists' form 7.2 us, the other's 4.0)
+    p.long_lists = (int64_t)n_seqs * c.n_kv_heads * 32 <= p.workers && max_kv >= 64 * STREAM_KEYS;
     p.stream_rows = (int)std::min<int64_t>(STREAM_ROWS * p.stream_tiles, p.tile ? 2 * STREAM_ROWS : most);
     if (p.splits > 1) p.tile_floats = (size_t)p.tiles * c.n_kv_heads * p.splits * TILE_ROWS_Q * d2;
     return p;

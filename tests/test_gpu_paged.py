@@ -398,6 +398,15 @@ def test_paged_decode_many_sequences(n):
     check_attention(*Paged([(r.choice((0, 3, r.randint(0, top))), r.choice((1, 1, 1, 0))) for _ in range(n)], 4, 2, 64, 16, "bf16", 3).run(max_q=1), what="many")
 
 
+def test_paged_mostly_idle_slots():
+    """As many sequences as a call takes, nearly all of them without rows: far between two that have some, at the front and at the end; chunks among them."""
+    for live, q in (((0, 1, 700, 2047), 1), ((64, 1500), 1), ((3, 900, 901, 2000), 50)):
+        seqs = [(0, 0)] * 2048
+        for i, s in enumerate(live):
+            seqs[s] = (300 + 100 * i, q if i % 2 == 0 else 1)
+        check_attention(*Paged(seqs, 4, 2, 64, 64, "fp16", 3).run(max_q=q, max_kv=800), what="idle")
+
+
 def test_paged_long_context():
     """Many parts of one row tile, ids reloaded many times, small pages."""
     check_attention(*Paged([(40000, 1)], 4, 1, 128, 16, "fp16").run(max_q=1), what="long")
