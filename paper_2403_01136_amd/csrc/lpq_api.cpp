@@ -868,7 +868,7 @@ lpq_status run_batch_attention(const void* qkv, const lpq_attn_cfg* cfg, const l
     if (cst != LPQ_OK) return cst;
     AttentionPlan plan = attention_plan(*cfg, kp != nullptr, n_seqs, M, max_q, max_kv, cus);
     float* part = nullptr;
-    const size_t floats = std::max(plan.stream_floats, plan.tile_floats);
+    const size_t floats = plan.stream_floats + plan.tile_floats;
     if (floats) {
         const lpq_status s = workspace(false, floats * sizeof(float), &part);
         if (s == LPQ_ERR_BUFSIZE) plan.splits = 1, plan.stream_floats = plan.tile_floats = 0;      // no room for parts: nothing is split

@@ -197,7 +197,7 @@ __device__ __forceinline__ int64_t seq_units(const AttnArgs& a, int s, int tile_
 // A wave's share: units [u, end), the sequence that has unit u and the units before that sequence.
 struct Share { int64_t u, end, units, seq_begin; int workers, s; };
 struct ShareSmem { int64_t scan[4], begin[4]; int seq[4]; };
-__device__ __forceinline__ Share find_share(const AttnArgs& a, int tile_rows, ShareSmem& sm)
+__device__ __forceinline__ Share find_share(const AttnArgs& a, int block, int tile_rows, ShareSmem& sm)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t first = seq_units(a, tid, tile_rows);                          // the usual batch has no more than 256 sequences: one pass
@@ -209,7 +209,7 @@ __device__ __forceinline__ Share find_share(const AttnArgs& a, int tile_rows, Sh
     Share r;
     r.units = uniform64(sm.scan[0] + sm.scan[1] + sm.scan[2] + sm.scan[3]);
     r.workers = (int)min<int64_t>(a.workers, r.units);
-    const int w0 = 4 * (int)blockIdx.x;
+    const int w0 = 4 * block;
     int64_t carry = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 256) {
         if (a.n_seqs > 256) {
@@ -248,20 +248,19 @@ __device__ __forceinline__ Share find_share(const AttnArgs& a, int tile_rows, Sh
 constexpr int STREAM_WAVES = 1, DEPTH = 2;
 
 template <int DT, int D, int NT, bool ALIBI>
-__global__ __launch_bounds__(256, STREAM_WAVES) void stream_attention_kernel(AttnArgs a)
+__device__ __forceinline__ void stream_block(const AttnArgs& a, int block, ShareSmem& sm)
 {
     typedef typename Elem<DT>::v8 V8;
     constexpr int KJ = D / 32, F = D / 16, TILE_ROWS = STREAM_ROWS * NT;         // feature steps of S^T; features of a lane's V chunk
     constexpr int SLOT = TILE_ROWS * (D + 2);
     typedef uint32_t vchunk __attribute__((ext_vector_type(F / 2)));
-    __shared__ ShareSmem sm;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const float c = LOG2E / sqrtf((float)D);
     const int cols = (a.heads + 2 * a.kv_heads) * D, page_mask = (1 << a.shift) - 1;
 
-    const Share share = find_share(a, TILE_ROWS, sm);
-    const int w = 4 * (int)blockIdx.x + wave;
+    const Share share = find_share(a, block, TILE_ROWS, sm);
+    const int w = 4 * block + wave;
     int64_t u = share.u, s_begin = share.seq_begin;
     int s = share.s;
     Cut cut{0, 0, 0, 0};
@@ -272,10 +271,11 @@ __global__ __launch_bounds__(256, STREAM_WAVES) void stream_attention_kernel(Att
             s_begin += s_units;
             uint64_t found = 0;
             int64_t mine = 0;
-            for (++s; !found; s += found ? 0 : 64) {
+            for (++s; !found && s < a.n_seqs; s += found ? 0 : 64) {
                 mine = seq_units(a, s + lane, TILE_ROWS);
                 found = __ballot(mine > 0);
             }
+            if (!found) break;                         // lengths that change under the kernel
             const int k = __builtin_ctzll(found);
             s = __builtin_amdgcn_readfirstlane(s + k);
             s_units = uniform64(shfl64(mine, k));
@@ -499,6 +499,13 @@ __global__ __launch_bounds__(256, STREAM_WAVES) void stream_attention_kernel(Att
     if (a.part && lane == 0) reinterpret_cast<Cut*>(a.part + (size_t)2 * a.workers * SLOT)[w] = cut;
 }
 
+template <int DT, int D, int NT, bool ALIBI>
+__global__ __launch_bounds__(256, STREAM_WAVES) void stream_attention_kernel(AttnArgs a)
+{
+    __shared__ ShareSmem sm;
+    stream_block<DT, D, NT, ALIBI>(a, (int)blockIdx.x, sm);
+}
+
 // Adds up the parts of the row tiles that the entries of `cuts` name, 16 entries a workgroup; blockIdx.y: rows and, if LONG, slices of 32 features.  Many
 // short lists of parts: a wave takes a row of a cut, D / 4 lanes of four features each for every (256 / D)-th part.  LONG, for few lists of hundreds of parts:
 // the workgroup takes a slice, 8 lanes for every 32nd part, the sums added through LDS.  Either is right for any list.
@@ -677,19 +684,20 @@ __device__ __forceinline__ void store_rows(const AttnArgs& a, const Tile& tl, in
     }
 }
 
+extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];              // K, K, V, V (dynamic: ahead of a read of a named array the compiler waits for every load into it)
+
 template <int DT, int D, bool ALIBI, bool PAGED>
-__global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
+__device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 {
     typedef typename Elem<DT>::v8 V8;
     constexpr int CH = D / 8, KS = D / 16, DTL = D / 32, ROWS = 512 / D, FILLS = 16 / ROWS;       // chunks of a row; feature steps; feature tiles; keys per load; loads of a wave's 16 keys
     constexpr int TILE_BYTES = TILE_KEYS * D * 2;
     constexpr bool BACKWARD = ALIBI;                   // biases grow towards the diagonal: from there on the first tiles have the maximum
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];          // K, K, V, V (dynamic: ahead of a read of a named array the compiler waits for every load into it)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     // (head, split, row tile) of this workgroup: the last row tiles, with the longest walks, first
     const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
     const int per_xcd = a.kv_heads * classes / 8, per_class = (a.tiles + classes - 1) / classes;
-    const int slot = (int)(blockIdx.x >> 3), combo = (int)(blockIdx.x & 7) + 8 * (slot % per_xcd), rest = slot / per_xcd;
+    const int slot = block >> 3, combo = (block & 7) + 8 * (slot % per_xcd), rest = slot / per_xcd;
     const int h = combo % a.kv_heads, split = rest / per_class, v = a.tiles - 1 - ((rest % per_class) * classes + combo / a.kv_heads);
     Tile tl;
     if (v < 0 || !tile_of(a, v, &tl)) return;
@@ -894,6 +902,21 @@ __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a)
     store_rows<DT, D>(a, tl, h, ks, tile_part<D>(a, ks, h, v, split), o, m, l2[0] + l2[1], wr0, tok, head);
 }
 
+template <int DT, int D, bool ALIBI, bool PAGED>
+__global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a) { tile_block<DT, D, ALIBI, PAGED>(a, (int)blockIdx.x); }
+
+// Both for a batch that may have sequences of either kind: the streaming kernel's workgroups, then the tile kernel's, which multiply while the others read.
+// Against a launch of each, us: two chunks of 512 beside 9 sequences that decode, 56 heads (8 K/V heads), biases, 77 so, 71 now; 250 and one chunk, 64 heads (8), 148 / 145;
+// 60 and one chunk, 40 heads (40), 110 / 100; 4 and a chunk of 200, 32 heads (8), 22 / 16.  The tile kernel's first: 62, 210, 144, 15; by turns: 69, 193, 134, 15: streams
+// that begin late end last.  With two column tiles the streaming kernel has more registers than two workgroups a compute unit leave: a launch of each.
+template <int DT, int D, bool ALIBI>
+__global__ __launch_bounds__(256, 2) void mixed_attention_kernel(AttnArgs stream, AttnArgs tile)
+{
+    const int streams = stream.workers / 4;
+    if ((int)blockIdx.x < streams) stream_block<DT, D, 1, ALIBI>(stream, (int)blockIdx.x, *reinterpret_cast<ShareSmem*>(smem_raw));
+    else tile_block<DT, D, ALIBI, true>(tile, (int)blockIdx.x - streams);
+}
+
 // Adds up the splits of a row tile and head (blockIdx.x), in order: a thread has four features of a row, a workgroup 1024 / D rows (blockIdx.y).  The loads of four
 // splits are under way together.
 template <int DT, int D>
@@ -976,46 +999,49 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
 }
 
 template <int DT, int D>
-static hipError_t launch_attention(const AttentionPlan& p, AttnArgs a, float* part, hipStream_t s)
+static hipError_t launch_attention(const AttentionPlan& p, const AttnArgs& a, float* part, hipStream_t s)
 {
-    const bool alibi = a.slopes != nullptr;
-    const bool both = p.stream_tiles && p.tile;
-    if (p.stream_tiles) {
-        a.rows_from = 1;
-        a.rows_to = both ? 2 * STREAM_ROWS + 1 : INT32_MAX;
-        a.workers = p.workers;
-        a.part = p.stream_floats ? part : nullptr;
-        const unsigned grid = (unsigned)p.workers / 4, cuts = (unsigned)((p.workers + CUTS_PER_WG - 1) / CUTS_PER_WG);
-#define LPQ_STREAM(NT)                                                                                                  \
-        do {                                                                                                            \
-            if (alibi) stream_attention_kernel<DT, D, NT, true><<<grid, 256, 0, s>>>(a);                                \
-            else       stream_attention_kernel<DT, D, NT, false><<<grid, 256, 0, s>>>(a);                               \
-            if (a.part && p.long_lists) stream_combine_kernel<DT, D, NT, true><<<dim3(cuts, (unsigned)p.stream_rows * (D / 32)), 256, 0, s>>>(a); \
-            else if (a.part) stream_combine_kernel<DT, D, NT, false><<<dim3(cuts, (unsigned)p.stream_rows), 256, 0, s>>>(a);             \
-        } while (0)
-        if (p.stream_tiles == 1) LPQ_STREAM(1);
-        else LPQ_STREAM(2);
-#undef LPQ_STREAM
+    const bool alibi = a.slopes != nullptr, both = p.stream_tiles && p.tile, mixed = both && p.stream_tiles == 1;
+    const unsigned streams = (unsigned)p.workers / 4;
+    AttnArgs st = a, tl = a;
+    st.rows_from = 1;
+    st.rows_to = both ? 2 * STREAM_ROWS + 1 : INT32_MAX;
+    st.workers = p.workers;
+    st.part = p.stream_floats ? part : nullptr;
+    tl.rows_from = both ? 2 * STREAM_ROWS + 1 : 1;
+    tl.rows_to = INT32_MAX;
+    tl.tiles = p.tiles;
+    tl.splits = p.splits;
+    tl.least = p.least;
+    tl.part = part + p.stream_floats;
+    const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
+    const unsigned grid = (unsigned)(a.kv_heads * classes) * (unsigned)((p.tiles + classes - 1) / classes) * (unsigned)p.splits;
+    constexpr size_t smem = 4 * TILE_KEYS * D * 2;
+#define LPQ_ALIBI(KERNEL, GRID, SMEM, ...)                                                                              \
+    do {                                                                                                                \
+        if (alibi) KERNEL(true)<<<GRID, 256, SMEM, s>>>(__VA_ARGS__);                                                   \
+        else       KERNEL(false)<<<GRID, 256, SMEM, s>>>(__VA_ARGS__);                                                  \
+    } while (0)
+#define LPQ_MIXED(A) mixed_attention_kernel<DT, D, A>
+#define LPQ_STREAM1(A) stream_attention_kernel<DT, D, 1, A>
+#define LPQ_STREAM2(A) stream_attention_kernel<DT, D, 2, A>
+#define LPQ_TILE_PAGED(A) tile_attention_kernel<DT, D, A, true>
+#define LPQ_TILE_PACKED(A) tile_attention_kernel<DT, D, A, false>
+    if (mixed) LPQ_ALIBI(LPQ_MIXED, streams + grid, smem, st, tl);
+    else {
+        if (p.stream_tiles == 1) LPQ_ALIBI(LPQ_STREAM1, streams, 0, st);
+        else if (p.stream_tiles == 2) LPQ_ALIBI(LPQ_STREAM2, streams, 0, st);
+        if (p.tile && a.kp) LPQ_ALIBI(LPQ_TILE_PAGED, grid, smem, tl);
+        else if (p.tile) LPQ_ALIBI(LPQ_TILE_PACKED, grid, smem, tl);
     }
-    if (p.tile) {
-        a.rows_from = both ? 2 * STREAM_ROWS + 1 : 1;
-        a.rows_to = INT32_MAX;
-        a.tiles = p.tiles;
-        a.splits = p.splits;
-        a.least = p.least;
-        a.part = part;
-        const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
-        const unsigned grid = (unsigned)(a.kv_heads * classes) * (unsigned)((p.tiles + classes - 1) / classes) * (unsigned)p.splits;
-        constexpr size_t smem = 4 * TILE_KEYS * D * 2;
-        if (a.kp) {
-            if (alibi) tile_attention_kernel<DT, D, true, true><<<grid, 256, smem, s>>>(a);
-            else       tile_attention_kernel<DT, D, false, true><<<grid, 256, smem, s>>>(a);
-        } else {
-            if (alibi) tile_attention_kernel<DT, D, true, false><<<grid, 256, smem, s>>>(a);
-            else       tile_attention_kernel<DT, D, false, false><<<grid, 256, smem, s>>>(a);
-        }
-        if (p.splits > 1) tile_combine_kernel<DT, D><<<dim3((unsigned)(p.tiles * a.kv_heads), TILE_ROWS_Q * D / 1024), 256, 0, s>>>(a);
+    if (st.part && p.stream_tiles) {
+        const unsigned cuts = (unsigned)((p.workers + CUTS_PER_WG - 1) / CUTS_PER_WG), rows = (unsigned)p.stream_rows;
+        if (p.stream_tiles == 1 && p.long_lists) stream_combine_kernel<DT, D, 1, true><<<dim3(cuts, rows * (D / 32)), 256, 0, s>>>(st);
+        else if (p.stream_tiles == 1) stream_combine_kernel<DT, D, 1, false><<<dim3(cuts, rows), 256, 0, s>>>(st);
+        else if (p.long_lists) stream_combine_kernel<DT, D, 2, true><<<dim3(cuts, rows * (D / 32)), 256, 0, s>>>(st);
+        else stream_combine_kernel<DT, D, 2, false><<<dim3(cuts, rows), 256, 0, s>>>(st);
     }
+    if (p.tile && p.splits > 1) tile_combine_kernel<DT, D><<<dim3((unsigned)(p.tiles * a.kv_heads), TILE_ROWS_Q * D / 1024), 256, 0, s>>>(tl);
     return hipGetLastError();
 }
 

@@ -398,6 +398,13 @@ def test_paged_decode_many_sequences(n):
     check_attention(*Paged([(r.choice((0, 3, r.randint(0, top))), r.choice((1, 1, 1, 0))) for _ in range(n)], 4, 2, 64, 16, "bf16", 3).run(max_q=1), what="many")
 
 
+@pytest.mark.parametrize("H,KV,d,dt,alibi", [(8, 1, 128, "fp16", False), (8, 2, 64, "bf16", True), (40, 2, 64, "fp16", False)])
+def test_paged_parts_of_both_kernels(H, KV, d, dt, alibi):
+    """Long contexts of few heads: single tokens' walks are cut among waves and a chunk's into key splits, each with its own part of the workspace; group 20: launched
+    one after the other."""
+    check_attention(*Paged([(9000, 1), (4000, 300), (0, 0), (7001, 2), (2500, 40)], H, KV, d, 16, dt, 5).run(alibi, max_q=300), what="parts of both")
+
+
 def test_paged_mostly_idle_slots():
     """As many sequences as a call takes, nearly all of them without rows: far between two that have some, at the front and at the end; chunks among them."""
     for live, q in (((0, 1, 700, 2047), 1), ((64, 1500), 1), ((3, 900, 901, 2000), 50)):
