@@ -964,7 +964,7 @@ __global__ __launch_bounds__(256) void tile_combine_kernel(AttnArgs a)
 // Room that the tile kernel's parts may take: its list has a place for each sequence, also for those that the streaming kernel does.
 constexpr size_t MAX_PART_BYTES = (size_t)256 << 20;
 
-// What a call launches: the streaming kernel, the tile kernel or, where a batch may have sequences of both kinds, both.
+// What a call launches: the streaming kernel, the tile kernel or, where a batch may have sequences of both kinds, both, in one launch if column tiles are single.
 AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int M, int max_q, int max_kv, int cus)
 {
     AttentionPlan p{};
