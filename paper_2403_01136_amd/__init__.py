@@ -368,6 +368,21 @@ def _stream_on(stream, dev):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
+def _new_tensors(make, stream, dev):
+    """make() -> tensors, allocated and filled on the stream of the call: a fill on another one, or memory that another one's queued work still uses, is
+    not ordered with the kernel.  The allocator learns that the current stream will use them too."""
+    import torch
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        made = make()
+    current = torch.cuda.current_stream(dev)
+    if current != stream:
+        for t in made:
+            t.record_stream(current)
+    return made
+
+
 def _attn_cfg(qkv, n_heads, n_kv_heads):
     import torch
     if qkv.dtype is not torch.float16 and qkv.dtype is not torch.bfloat16:
@@ -393,21 +408,22 @@ def _paged_cfg(qkv, k_pages, v_pages):
     return dev, cfg, page_size, n_pages
 
 
-def _out_and_slopes(qkv, cfg, out, alibi_slopes, dev):
+def _out_and_slopes(qkv, cfg, out, alibi_slopes, stream, dev):
     import torch
     M, cols = qkv.shape[0], cfg.n_heads * cfg.head_dim
-    if out is None:
-        out = torch.zeros((M, cols), dtype=qkv.dtype, device=qkv.device)      # rows that no sequence has stay as they are: zero
-    else:
+    if out is not None:
         _check_tensor("out", out, qkv.dtype, 2, dev)
         if out.shape[0] != M or out.shape[1] != cols:
             raise ValueError("out must be [%d][%d]" % (M, cols))
-    if alibi_slopes is None:
-        return out, None
-    _check_tensor("alibi_slopes", alibi_slopes, torch.float32, 1, dev)
-    if alibi_slopes.shape[0] != cfg.n_heads:
-        raise ValueError("alibi_slopes must have a value per head")
-    return out, alibi_slopes.data_ptr()
+    slopes = None
+    if alibi_slopes is not None:
+        _check_tensor("alibi_slopes", alibi_slopes, torch.float32, 1, dev)
+        if alibi_slopes.shape[0] != cfg.n_heads:
+            raise ValueError("alibi_slopes must have a value per head")
+        slopes = alibi_slopes.data_ptr()
+    if out is None:                                    # rows that no sequence has stay as they are: zero
+        out, = _new_tensors(lambda: [torch.zeros((M, cols), dtype=qkv.dtype, device=qkv.device)], stream, dev)
+    return out, slopes
 
 
 def lpq_paged_plan(past, q_lens, table, ring, counters, page_size, M, plan=None, stream=None):
@@ -417,7 +433,7 @@ def lpq_paged_plan(past, q_lens, table, ring, counters, page_size, M, plan=None,
     import torch
     i32, n, dev = torch.int32, past.shape[0], _device_of(past)
     if plan is None:
-        plan = [torch.empty(m, dtype=i32, device=past.device) for m in (n + 1, n, M, M, 2, 4)]
+        plan = _new_tensors(lambda: [torch.empty(m, dtype=i32, device=past.device) for m in (n + 1, n, M, M, 2, 4)], stream, dev)
     plan = cu_q, kv_lens, slots, positions, new_counters, info = PagePlan(*plan)
     _check_tensor("table", table, i32, 2, dev)
     for name, t, size in (("past", past, n), ("q_lens", q_lens, n), ("ring", ring, None), ("counters", counters, 2), ("cu_q", cu_q, n + 1), ("kv_lens", kv_lens, n),
@@ -458,7 +474,7 @@ def lpq_paged_attention(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None,
     n, M, width = kv_lens.shape[0], qkv.shape[0], table.shape[1]
     if cu_q.shape[0] != n + 1 or table.shape[0] != n:
         raise ValueError("table, cu_q and kv_lens do not have the same number of sequences")
-    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes, dev)
+    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes, stream, dev)
     p = lpq_page_pool(page_size, n_pages, width, table.data_ptr(), None, None)
     _check(load_library().lpq_paged_attention(qkv.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), slopes, cu_q.data_ptr(), kv_lens.data_ptr(), n, M,
                                               M if max_q is None else max_q, width * page_size if max_kv is None else max_kv, out.data_ptr(),
@@ -473,7 +489,7 @@ def lpq_packed_attention(qkv, cu_q, n_heads, n_kv_heads, max_q=None, alibi_slope
     _check_tensor("qkv", qkv, qkv.dtype, 2, dev)
     cfg = _attn_cfg(qkv, n_heads, n_kv_heads)
     _check_tensor("cu_q", cu_q, torch.int32, 1, dev)
-    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes, dev)
+    out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes, stream, dev)
     M = qkv.shape[0]
     _check(load_library().lpq_packed_attention(qkv.data_ptr(), cfg, slopes, cu_q.data_ptr(), cu_q.shape[0] - 1, M, M if max_q is None else max_q, out.data_ptr(),
                                                _stream_on(stream, dev)), "lpq_packed_attention")

@@ -645,6 +645,38 @@ def test_on_another_stream():
     assert torch.equal(out, want)
 
 
+def test_on_another_stream_with_new_outputs():
+    """Outputs that the binding makes, on a stream of the caller's while the current one is busy: what is filled or still in use on the current one must not
+    reach them, neither while it works nor afterwards."""
+    import torch
+    p = Paged([(900, 1), (40, 30)], 8, 2, 64, 16, "fp16", 3)
+    want, _ = p.run(max_q=30)
+    want[31:] = 0
+    t, cu, kv = ints(p.table), ints(p.cu), ints([901, 70])
+    packed = lpq.lpq_packed_attention(p.qkv, ints([0, 34]), 8, 2)
+    case = plan_case(3, 40, 32, MIXED, 300, 5)
+    past, q, table, ring, counters, M = ints(case[0]), ints(case[1]), ints(case[2]), ints(case[3]), ints(case[4:6]), case[6]
+    plan = lpq.lpq_paged_plan(past, q, table.clone(), ring.clone(), counters, 32, M)
+    s, cu2 = torch.cuda.Stream(), ints([0, 34])
+    torch.cuda.synchronize()
+    calls = [(lambda: [lpq.lpq_paged_attention(p.qkv, p.k, p.v, t, cu, kv, max_q=30, stream=s)], [want]),
+             (lambda: [lpq.lpq_packed_attention(p.qkv, cu2, 8, 2, stream=s)], [packed]),
+             (lambda: list(lpq.lpq_paged_plan(past, q, table, ring, counters, 32, M, stream=s)), list(plan))]
+    for call, expected in calls:
+        freed = [torch.empty_like(e) for e in expected]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        for f in freed:
+            f.fill_(-9)                                # queued behind the sleep, in memory that is free for the current stream's next tensors
+        del freed, f
+        got = call()
+        s.synchronize()
+        with torch.cuda.stream(s):
+            assert all(torch.equal(g, e) for g, e in zip(got, expected))
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, e) for g, e in zip(got, expected))
+
+
 def test_captured_decode_loop():
     """A decode step (plan in place, append, attention) captured once and replayed: each replay is the next step, as the eager loop has it; eager work of other
     sizes, with its own use of the workspace, runs between the replays."""
