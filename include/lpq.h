@@ -322,7 +322,7 @@ typedef struct {
  * positions behind max_pages * page_size, or its and its predecessors' needs exceed the free pages: it gets no page, its rows no slots, its kv_lens stays
  * at `past`, and the caller may plan it again later.  Negative past counts as 0, counters are taken into their range.
  * With in-place counters and kv_lens a step is the same call every time and can be replayed from a graph.  The other outputs must not overlap the
- * inputs.  n_seqs <= 2048.  M > 6144 uses n_seqs words of the library's workspace, if a reservation leaves room for them.
+ * inputs.  n_seqs <= 2048.  Uses none of the library's workspace: plans may overlap other calls that do not touch their buffers.
  * Errors: NULL, SHAPE (page_size, counts, limits above), ALIGN (4 bytes), DEVICE. */
 lpq_status lpq_paged_plan(const lpq_page_pool *pool, const int32_t *past, const int32_t *q_lens, int32_t n_seqs, int32_t M,
                           const lpq_page_plan *plan, void *hip_stream);

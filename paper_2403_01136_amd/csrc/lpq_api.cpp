@@ -986,10 +986,7 @@ lpq_status lpq_paged_plan(const lpq_page_pool* pool, const int32_t* past, const 
                           (const void*)plan->counters, (const void*)plan->cu_q, (const void*)plan->kv_lens, (const void*)plan->slots,
                           (const void*)plan->positions, (const void*)plan->info})
         if (misaligned4(p)) return LPQ_ERR_ALIGN;
-    float* ws = nullptr;
-    const size_t need = paged_plan_workspace_bytes(n_seqs, M);
-    if (need && (s = workspace(false, need, &ws)) != LPQ_OK && s != LPQ_ERR_BUFSIZE) return s;       // no room: one launch does the rows too
-    return launch_paged_plan(*pool, page_shift_of(pool->page_size), past, q_lens, n_seqs, M, *plan, ws, static_cast<hipStream_t>(hip_stream)) == hipSuccess
+    return launch_paged_plan(*pool, page_shift_of(pool->page_size), past, q_lens, n_seqs, M, *plan, static_cast<hipStream_t>(hip_stream)) == hipSuccess
                ? LPQ_OK : LPQ_ERR_DEVICE;
 }
 

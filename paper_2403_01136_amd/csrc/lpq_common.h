@@ -206,9 +206,8 @@ hipError_t launch_attention_decode(const void* qkv, void* kc, void* vtc, const f
 hipError_t launch_attention_prefill(const void* qkv, const void* kc, const void* vtc, const float* slopes, int n_seqs, int T, int pos0, int H, int d,
                                     int S, void* out, hipStream_t s);
 // paged caches and packed batches (lpq_paged.hip, lpq_paged_attention.hip); shift: log2 of the page size
-size_t paged_plan_workspace_bytes(int n_seqs, int M);
 hipError_t launch_paged_plan(const lpq_page_pool& pool, int shift, const int32_t* past, const int32_t* q_lens, int n_seqs, int M, const lpq_page_plan& out,
-                             void* ws, hipStream_t s);
+                             hipStream_t s);
 hipError_t launch_paged_append(const void* qkv, const lpq_attn_cfg& c, int shift, int n_pages, void* k_pages, void* v_pages, const int32_t* slots, int M,
                                hipStream_t s);
 struct AttentionPlan {

@@ -74,7 +74,6 @@ __device__ __forceinline__ int ring_at(uint32_t at, int n_pages) { return at >= 
 struct PlanArgs {
     const int32_t *past, *q_lens, *counters;
     int32_t *table, *ring, *counters_out, *cu_q, *kv_lens, *slots, *positions, *info;
-    int32_t* base;                                     // [n] cached positions of a served sequence, -1 of a starved one; null: this launch does the rows
     int32_t n, M, shift, n_pages, width;
 };
 
@@ -85,6 +84,12 @@ __device__ __forceinline__ void write_row(const PlanArgs& a, int r, int page, in
     a.positions[r] = pos;
 }
 
+// The rows of a long batch have a launch of their own behind the rest, whose workgroups need to know which sequences are starved and the others' cached
+// positions, and the lengths may have been updated in place.  Each finds that (-1: starved) in its own rows' slots: in the first row that a sequence has of
+// them.  Nothing is kept outside of the caller's buffers, so plans may overlap any call that leaves those alone.
+constexpr int PLAN_ROWS_PER_WG = 256 * ROWS_AHEAD;
+
+template <bool ROWS_APART>
 __global__ __launch_bounds__(PLAN_THREADS) void paged_plan_kernel(PlanArgs a)
 {
     __shared__ uint32_t cu[PAGED_MAX_SEQS], need_before[PAGED_MAX_SEQS], back_before[PAGED_MAX_SEQS];
@@ -140,7 +145,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_plan_kernel(PlanArgs a)
         if (need[i] > 0 && !starved) most = sum;
         n_starved += starved;
         base[s] = starved ? -1 : past[i];
-        if (a.base) a.base[s] = base[s];
+        if (ROWS_APART && q[i] > 0 && cu[s] < (uint32_t)a.M) a.slots[cu[s]] = base[s];
         a.kv_lens[s] = done[i] ? 0 : starved ? past[i] : past[i] + q[i];
     }
     if (most) atomicMax(&taken_s, most);
@@ -156,7 +161,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_plan_kernel(PlanArgs a)
         a.info[2] = returned;
         a.info[3] = (int)starved_s;
     }
-    const int top = n > 1 ? 1 << (31 - __builtin_clz(n - 1)) : 0, threads = blockDim.x;
+    const int top = n > 1 ? 1 << (31 - __builtin_clz(n - 1)) : 0, threads = (int)blockDim.x - (ROWS_APART ? 64 : 0);
+    if (ROWS_APART && tid >= threads) {                // the last wave, beside the others
+        for (int r = (tid - threads) * PLAN_ROWS_PER_WG; r < total_rows; r += 64 * PLAN_ROWS_PER_WG) {
+            int s[1];
+            last_at_most<1>(cu, n, top, {(uint32_t)r}, s);
+            a.slots[r] = base[s[0]];
+        }
+        return;
+    }
     for (int i = tid; i < taken; i += threads) {
         int s[1];
         last_at_most<1>(need_before, n, top, {(uint32_t)i}, s);
@@ -170,7 +183,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_plan_kernel(PlanArgs a)
         const uint32_t at = (uint32_t)head + (uint32_t)free_pages;
         a.ring[ring_at((uint32_t)ring_at(at, a.n_pages) + (uint32_t)i, a.n_pages)] = a.table[(size_t)s[0] * a.width + (i - (int)back_before[s[0]])];
     }
-    if (a.base) return;
+    if constexpr (ROWS_APART) return;
     for (int r0 = tid; r0 < a.M; r0 += ROWS_AHEAD * threads) {
         uint32_t r[ROWS_AHEAD];
         int s[ROWS_AHEAD], pos[ROWS_AHEAD], page[ROWS_AHEAD];
@@ -194,27 +207,28 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_plan_kernel(PlanArgs a)
 }
 
 // The rows of a long batch, behind the kernel above: the table is complete.
-constexpr int PLAN_ROWS_PER_WG = 256 * ROWS_AHEAD;
 __global__ __launch_bounds__(256) void paged_plan_rows_kernel(PlanArgs a)
 {
     __shared__ uint32_t cu[PAGED_MAX_SEQS];
-    __shared__ int32_t base[PAGED_MAX_SEQS];
-    for (int s = threadIdx.x; s < a.n; s += 256) cu[s] = (uint32_t)a.cu_q[s], base[s] = a.base[s];
-    const uint32_t total = (uint32_t)a.cu_q[a.n];
+    for (int s = threadIdx.x; s < a.n; s += 256) cu[s] = (uint32_t)a.cu_q[s];
+    const uint32_t total = (uint32_t)a.cu_q[a.n], from = blockIdx.x * (uint32_t)PLAN_ROWS_PER_WG;
     __syncthreads();
     const int top = a.n > 1 ? 1 << (31 - __builtin_clz(a.n - 1)) : 0;
     uint32_t r[ROWS_AHEAD];
-    int s[ROWS_AHEAD], pos[ROWS_AHEAD], page[ROWS_AHEAD];
+    int s[ROWS_AHEAD], base[ROWS_AHEAD], pos[ROWS_AHEAD], page[ROWS_AHEAD];
 #pragma unroll
-    for (int k = 0; k < ROWS_AHEAD; ++k) r[k] = blockIdx.x * (uint32_t)PLAN_ROWS_PER_WG + 256u * k + threadIdx.x;
+    for (int k = 0; k < ROWS_AHEAD; ++k) r[k] = from + 256u * k + threadIdx.x;
     last_at_most<ROWS_AHEAD>(cu, a.n, top, r, s);
+#pragma unroll
+    for (int k = 0; k < ROWS_AHEAD; ++k) base[k] = r[k] < total ? a.slots[max(cu[s[k]], from)] : -1;
+    __syncthreads();                                   // they have been read: the slots can be written
 #pragma unroll
     for (int k = 0; k < ROWS_AHEAD; ++k) {
         page[k] = -1;
         pos[k] = 0;
-        if (r[k] >= total || base[s[k]] < 0) continue;
-        pos[k] = base[s[k]] + (int)(r[k] - cu[s[k]]);
-        page[k] = a.table[(size_t)s[k] * a.width + (pos[k] >> a.shift)];
+        if (base[k] < 0) continue;
+        pos[k] = base[k] + (int)(r[k] - cu[s[k]]);
+        page[k] = a.table[(size_t)s[k] * a.width + min(pos[k] >> a.shift, a.width - 1)];
     }
 #pragma unroll
     for (int k = 0; k < ROWS_AHEAD; ++k)
@@ -243,20 +257,22 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const uint16_t* __res
 
 }  // namespace
 
-// One launch / the rows in one of their own, us: 16 sequences, 4096 rows 8.0 / 8.4, 6400 rows 9.7 / 9.8; one sequence of 8000 8.4 / 7.2.
+// One launch / the rows in one of their own, us: 16 sequences, 4096 rows 8.1 / 8.7, 6144 rows 9.6 / 8.8; one sequence, 4096 rows 7.0 / 7.2, 8000 8.5 / 7.4; 300, 3900
+// rows 10.2 / 10.8, 6000 13.1 / 11.4; 2000, 6000 rows 13.6 / 14.3, 12000 18.5 / 14.9.
 constexpr int PLAN_ONE_LAUNCH_ROWS = 6144;
 
-size_t paged_plan_workspace_bytes(int n_seqs, int M) { return M > PLAN_ONE_LAUNCH_ROWS ? (size_t)n_seqs * sizeof(int32_t) : 0; }
-
 hipError_t launch_paged_plan(const lpq_page_pool& pool, int shift, const int32_t* past, const int32_t* q_lens, int n_seqs, int M, const lpq_page_plan& out,
-                             void* ws, hipStream_t s)
+                             hipStream_t s)
 {
     const PlanArgs a{past, q_lens, pool.counters, pool.table, pool.ring, out.counters, out.cu_q, out.kv_lens, out.slots, out.positions, out.info,
-                     static_cast<int32_t*>(ws), n_seqs, M, shift, pool.n_pages, pool.max_pages};
+                     n_seqs, M, shift, pool.n_pages, pool.max_pages};
     // threads for the sequences (two each) and, up to sixteen waves, for the rows (with a launch of their own: for the new pages)
-    const int want = std::max((n_seqs + 1) / 2, ws ? 512 : M);
-    paged_plan_kernel<<<1, std::min(PLAN_THREADS, (want + 63) / 64 * 64), 0, s>>>(a);
-    if (ws) paged_plan_rows_kernel<<<(unsigned)((M + PLAN_ROWS_PER_WG - 1) / PLAN_ROWS_PER_WG), 256, 0, s>>>(a);
+    const bool apart = M > PLAN_ONE_LAUNCH_ROWS;
+    const int want = std::max((n_seqs + 1) / 2, apart ? 512 + 64 : M), threads = std::min(PLAN_THREADS, (want + 63) / 64 * 64);
+    if (apart) {
+        paged_plan_kernel<true><<<1, threads, 0, s>>>(a);
+        paged_plan_rows_kernel<<<(unsigned)((M + PLAN_ROWS_PER_WG - 1) / PLAN_ROWS_PER_WG), 256, 0, s>>>(a);
+    } else paged_plan_kernel<false><<<1, threads, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -148,6 +148,17 @@ def test_plan_many_rows(n, lo, hi):
     check_plan(case, 32, in_place=True)
 
 
+@pytest.mark.parametrize("n", [2, 30, 600, 2048])
+def test_plan_many_rows_starved(n):
+    """The same without the pages, the rows or the table entries that all of them would need; rows near the line between one launch and two."""
+    for rows in (6144, 6145, 12000):
+        case = plan_case(n + rows, n, 16, lambda r: r.choice((0, -1, r.randint(0, 2 * rows // n + 1), 2 * rows // n)), 90, 0)
+        past, q, table, ring, head, free, M = case
+        for f, m in ((free, rows), (free // 2, rows + 900), (0, rows), (max(free - 1, 0), M)):
+            check_plan((past, q, table, ring, head, f, m), 16, in_place=f == free // 2)
+        check_plan((past, q, [t[:max(1, len(t) - 3)] for t in table], ring, head, free, rows), 16)
+
+
 @pytest.mark.parametrize("n", [5, 40, 257])
 def test_plan_starved(n):
     """Too few pages, rows behind the batch, positions behind the table, an empty pool; finished sequences return theirs all the same."""
@@ -675,6 +686,31 @@ def test_on_another_stream_with_new_outputs():
             assert all(torch.equal(g, e) for g, e in zip(got, expected))
         torch.cuda.synchronize()
         assert all(torch.equal(g, e) for g, e in zip(got, expected))
+
+
+def test_long_plan_beside_attention():
+    """Plans of more rows than one launch takes on a stream of their own, while attention with partial results runs on another: both as by themselves."""
+    import torch
+    p = Paged([(5000, 1), (2000, 40), (700, 1)], 8, 2, 128, 16, "fp16")
+    want, _ = p.run(max_q=40)
+    t, cu, kv, out = ints(p.table), ints(p.cu), ints([5001, 2040, 701]), torch.full_like(want, 77.0)
+    case = plan_case(6, 40, 32, lambda r: r.randint(300, 600), 400, 9)
+    ref = plan_ref(*case[:6], 32, case[6])
+    past, q, M = ints(case[0]), ints(case[1]), case[6]
+    assert M > 10000
+    inputs = [(ints(case[2]), ints(case[3]), ints(case[4:6])) for _ in range(20)]
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    plans = []
+    for table, ring, counters in inputs:
+        lpq.lpq_paged_attention(p.qkv, p.k, p.v, t, cu, kv, max_q=40, out=out, stream=a)
+        plans.append(lpq.lpq_paged_plan(past, q, table, ring, counters, 32, M, stream=b))
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    for plan, (table, ring, _) in zip(plans, inputs):
+        got = dict({k: getattr(plan, k).tolist() for k in plan._fields}, table=table.tolist(), ring=ring.tolist())
+        for name in ref:
+            assert got[name] == ref[name], name
 
 
 def test_captured_decode_loop():

@@ -33,3 +33,22 @@ print("RESERVED OK")
 def test_no_room_for_parts():
     out = subprocess.run([sys.executable, "-c", CHILD % (os.path.dirname(HERE), HERE)], capture_output=True, text=True, timeout=110)
     assert out.returncode == 0 and "RESERVED OK" in out.stdout, out.stdout[-2000:] + out.stderr[-4000:]
+
+
+CHILD_PLAN = r'''
+import sys
+sys.path.insert(0, %r), sys.path.insert(0, %r)
+import paper_2403_01136_amd as lpq
+import test_gpu_paged as t
+lpq.load_library()
+case = t.plan_case(5, 30, 32, lambda r: r.choice((300, 800)), 300, 4)
+assert case[-1] > 10000
+t.check_plan(case, 32)
+assert lpq.lpq_workspace_bytes() == 0, "a plan has made a workspace"
+print("PLAN OK")
+'''
+
+
+def test_plans_use_no_workspace():
+    out = subprocess.run([sys.executable, "-c", CHILD_PLAN % (os.path.dirname(HERE), HERE)], capture_output=True, text=True, timeout=110)
+    assert out.returncode == 0 and "PLAN OK" in out.stdout, out.stdout[-2000:] + out.stderr[-4000:]
