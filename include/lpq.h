@@ -336,7 +336,8 @@ lpq_status lpq_paged_append(const void *qkv, const lpq_attn_cfg *cfg, const lpq_
 /* Causal attention of the new tokens over the pages, after their append: token t of sequence s stands at position kv_lens[s] - q_s + t and sees
  * positions up to its own; out = softmax(q . k / sqrt(head_dim) + slope * (key position - query position)) . v per head, heads
  * concatenated, [M][n_heads * head_dim].  Positions whose table entry is not a page of the pool, or lies behind the table, count as masked; a row that sees
- * nothing (or only scores of minus infinity) gives zero.  Values at masked places, infinite or NaN, do not touch the result.
+ * nothing (or only scores of minus infinity) gives zero.  Values at masked places, infinite or NaN, do not touch the result; at a place that a row sees they make
+ * their feature infinite or NaN for that row (NaN also where an infinity's weight rounds to zero).
  * alibi_slopes: fp32 [n_heads] or NULL.  q_s may be 1 (decode), a chunk, a whole prompt, 0, and differ from sequence to sequence.
  * max_q, max_kv: the largest q_s and kv_lens the caller expects; they choose kernels and splits, and larger ones than that are only slower.
  * Partial results are kept in the library's workspace; where a reservation leaves no room the work is not split.  out must not overlap qkv.

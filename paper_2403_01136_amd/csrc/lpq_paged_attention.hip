@@ -11,9 +11,12 @@
 // others then cancels.  (One prompt of 5801 tokens in bf16 with sums of unrounded weights: 2.2e-3 from 64 bits; so 2.1e-3; the output's rounding alone 1.6e-3.)
 //
 // Keys that no row may see (behind the sequence's end, pages that are not in the pool) are read from page 0 or a stale page, their scores are replaced and
-// their values set to zero.  A later token's value row stays in the products at weight zero, and is finite; where it is not, the sums that it has
-// spoilt are formed again by row_walk, over the visible keys and no others.
+// their values set to zero.  A value that only some rows of a tile see stays in the products, at weight zero for the others, and must be finite: what is not is
+// set to zero too and added afterwards to the rows that see it (any weight of an infinity is one, of a NaN is one).  Such keys lie within the tokens of a tile,
+// at the diagonal, so only the tiles there are looked through (by v_dot2 with zeros: NaN if anything is not finite), at up to 1 % of a call's time.  A prompt of 3000
+// tokens, 8 heads over 2, one feature infinite in the first value row 58 us, in every row 91, without 58.
 #include <algorithm>
+#include <mutex>
 #include <type_traits>
 
 #include "lpq_common.h"
@@ -37,6 +40,8 @@ template <> struct Elem<LPQ_DT_FP16> {
     static __device__ __forceinline__ f4 mfma16(v8 a, v8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { const h2 p = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, p); }
     static __device__ __forceinline__ float add_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, p), h2{1, 1}, c, false); }
+    static __device__ __forceinline__ float probe_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, p), h2{0, 0}, c, false); }
+    enum { EXPONENT_STEP = 0x04000400 };                                        // one in the exponents' last places
 };
 template <> struct Elem<LPQ_DT_BF16> {
     typedef __bf16 t;
@@ -45,6 +50,8 @@ template <> struct Elem<LPQ_DT_BF16> {
     static __device__ __forceinline__ f4 mfma16(v8 a, v8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { const bf2 p = {(__bf16)a, (__bf16)b}; return __builtin_bit_cast(uint32_t, p); }
     static __device__ __forceinline__ float add_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, p), bf2{1.0f, 1.0f}, c, false); }
+    static __device__ __forceinline__ float probe_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, p), bf2{0.0f, 0.0f}, c, false); }
+    enum { EXPONENT_STEP = 0x00800080 };
 };
 
 // What a launch is about.  Pointers are to 16-bit elements.
@@ -88,63 +95,28 @@ __device__ __forceinline__ int page_of_group(const AttnArgs& a, int s, int g)
     return e < 0 ? -1 : page_checked(a.table[(size_t)s * a.max_pages + e], a.n_pages);
 }
 
-// One row by one wave, on the vector units, over the visible keys of [k0, k1) and no others: lanes along the keys for the scores, along the features for
-// the sums.  For rows whose sums came out not finite (see above); the same scaling, exponents and rounding of the weights.
-template <int DT, int D>
-__device__ __forceinline__ void row_walk(const AttnArgs& a, const Seq& q, int h, const uint16_t* qp, int p, float slope, int k0, int k1,
-                                         float& m, float& l, float (&acc)[D / 64])
+// Which of a pair of elements are infinite or NaN: bit 15 and bit 31.  An exponent of all ones carries into the sign's place.
+template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t pair) { return ((pair & 0x7fff7fffu) + (uint32_t)Elem<DT>::EXPONENT_STEP) & 0x80008000u; }
+// The pair without the elements that `odd`, the above, names.
+__device__ __forceinline__ uint32_t without(uint32_t pair, uint32_t odd) { return pair & ~(odd | (odd - (odd >> 15))); }
+// Element e of a pair if it is infinite or NaN and `seen`, else zero.
+template <int DT> __device__ __forceinline__ float odd_element(uint32_t pair, int e, bool seen)
 {
-    typedef typename Elem<DT>::t T;
-    typedef typename Elem<DT>::v8 V8;
-    const int lane = threadIdx.x & 63, cols = (a.heads + 2 * a.kv_heads) * D;
-    const float c = LOG2E / sqrtf((float)D);
-    m = -INFINITY;
-    l = 0.0f;
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) acc[i] = 0.0f;
-    k1 = min(k1, min(p + 1, q.ctx));
-    auto key_row = [&](int j, bool v) -> const uint16_t* {                       // null: not there
-        if (!a.kp) return a.qkv + (size_t)(q.first + j) * cols + (a.heads + (v ? a.kv_heads : 0) + h) * D;
-        const int page = page_of_group(a, q.s, j >> 4);
+    const float v = (float)__builtin_bit_cast(typename Elem<DT>::t, (uint16_t)(pair >> (16 * e)));
+    return seen && !__builtin_isfinite(v) ? v : 0.0f;
+}
+// The value row of key j of a sequence and K/V head (the same for the whole wave): null if it has no page, or if all of it is finite.
+template <int DT, int D>
+__device__ __forceinline__ const uint16_t* odd_value_row(const AttnArgs& a, const Seq& q, int h, int j)
+{
+    const uint16_t* row;
+    if (a.kp) {
+        const int page = __builtin_amdgcn_readfirstlane(page_of_group(a, q.s, j >> 4));
         if (page < 0) return nullptr;
-        return (v ? a.vp : a.kp) + page_element(page, h, a.kv_heads, a.shift, D) + (size_t)(j & ((1 << a.shift) - 1)) * D;
-    };
-#pragma unroll 1
-    for (int j0 = k0; j0 < k1; j0 += 64) {
-        const int j = j0 + lane;
-        const uint16_t* kr = j < k1 ? key_row(j, false) : nullptr;
-        float sc = -INFINITY;
-        if (kr) {
-            float d = 0.0f;
-#pragma unroll 1
-            for (int f = 0; f < D; f += 8) {
-                const V8 x = *reinterpret_cast<const V8*>(qp + f), k = *reinterpret_cast<const V8*>(kr + f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d += (float)x[e] * (float)k[e];
-            }
-            sc = __builtin_fmaf(d, c, slope * (float)(j - p));
-        }
-        const float mn = fmaxf(m, group_reduce<64>(sc, OpMax())), ms = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(m - ms), w = kr ? (float)(T)__builtin_amdgcn_exp2f(sc - ms) : 0.0f;
-        m = mn;
-        l = l * alpha + w;
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) acc[i] *= alpha;
-        const int n = min(64, k1 - j0);
-#pragma unroll 1
-        for (int u = 0; u < n; ++u) {
-            const uint16_t* vr = key_row(j0 + u, true);
-            const float wu = __shfl(w, u);
-            if (!vr) continue;
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) acc[i] = __builtin_fmaf(wu, (float)__builtin_bit_cast(T, vr[64 * i + lane]), acc[i]);
-        }
-        bool rest = false;                             // a NaN in every feature stays: inputs that are NaN throughout are not walked to their end
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) rest |= acc[i] == acc[i];
-        if (!__any(rest)) break;
-    }
-    l = group_reduce<64>(l, OpAdd());
+        row = a.vp + page_element(page, h, a.kv_heads, a.shift, D) + (size_t)(j & ((1 << a.shift) - 1)) * D;
+    } else row = a.qkv + (size_t)(q.first + j) * ((a.heads + 2 * a.kv_heads) * D) + (a.heads + a.kv_heads + h) * D;
+    const uint32_t pair = reinterpret_cast<const uint32_t*>(row)[threadIdx.x % (D / 2)];
+    return __any(not_finite<DT>(pair) != 0) ? row : nullptr;
 }
 
 // ---- streaming kernel ---------------------------------------------------------------------------
@@ -327,6 +299,7 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
         vchunk vf[DEPTH][2][4];
         uint32_t bad_of[DEPTH];                        // of the buffers' steps: bit i: 16-key group i has no page
         uint64_t bad_ids = 0;                          // bit l: lane l's group has none
+        bool odd = false;                              // a step that not every row sees had values that are not finite
         int ids_from = n0;
         // step n's loads from the pages `from`: an address is a scalar base and a 32-bit lane offset
         auto page_bytes = [&](const uint16_t* pages, int n, int i) {
@@ -420,6 +393,24 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if ((bad >> i & 1) || key0 + 16 * i + 4 * quarter + r >= key_end) vf[x][i][r] = vchunk{};
+            if (all_see < key_end && key0 + STREAM_KEYS > all_see) {             // the diagonal of more than one token
+                float probe = 0.0f;                    // NaN once a value has been infinite or NaN
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int e = 0; e < F / 2; ++e) probe = Elem<DT>::probe_pair(vf[x][i][r][e], probe);
+                if (__builtin_expect(__any(probe != probe), 0)) {
+                    odd = true;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int e = 0; e < F / 2; ++e) vf[x][i][r][e] = without(vf[x][i][r][e], not_finite<DT>(vf[x][i][r][e]));
+                }
+            }
 #pragma unroll
             for (int e = 0; e < F; ++e) {
                 u32x4 vt;                              // element e of the lane's chunks of the quarter's eight keys
@@ -440,6 +431,21 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
             for (int x = 0; x < DEPTH; ++x)            // buffers by name
                 if (n + x < n_last) step(n + x, x);
 
+        if (__builtin_expect(odd, 0))
+#pragma unroll 1
+            for (int j = max(STREAM_KEYS * n0, all_see / STREAM_KEYS * STREAM_KEYS); j < min(STREAM_KEYS * n_last, key_end); ++j) {
+                const uint16_t* row = odd_value_row<DT, D>(a, q, h, j);
+                if (!row) continue;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const vchunk x = *reinterpret_cast<const vchunk*>(row + F * (4 * quarter + g));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < F; ++e) o[t][e][g] += odd_element<DT>(x[e / 2], e % 2, j <= p[t]);
+                }
+            }
+
         // a whole row tile's results, or a part's sums
         const bool whole = n0 == 0 && n1 == steps;
         float* const slot = a.part + (size_t)(2 * w + (first < share.u ? 0 : 1)) * SLOT;
@@ -449,16 +455,7 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
             f2 z = both_rows(l[t]);
             z = both_halves(z[0] + z[1]);
             const float L = z[0] + z[1];
-            uint32_t again = 0;                        // rows whose sums a later token's values have spoilt: a bit per column
-            if (q.len > 1) {
-                float total = 0.0f;
-#pragma unroll
-                for (int e = 0; e < F; ++e) total += (o[t][e][0] + o[t][e][1]) + (o[t][e][2] + o[t][e][3]);
-                uint64_t odd = __ballot(!__builtin_isfinite(total) && ri < n_rows);
-                odd |= odd >> 32;
-                again = (uint32_t)(odd | odd >> 16) & 0xffffu;
-            }
-            if (ri < n_rows && !(again >> col & 1)) {
+            if (ri < n_rows) {
                 if (whole) {
                     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
                     uint16_t* op = a.out + (size_t)(q.first + tok) * a.heads * D + head * D;
@@ -477,19 +474,6 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
                             *reinterpret_cast<f4*>(slot + ri * D + F * (4 * quarter + g) + e) = f4{o[t][e][g], o[t][e + 1][g], o[t][e + 2][g], o[t][e + 3][g]};
                     if (quarter == 0) *reinterpret_cast<f2*>(slot + TILE_ROWS * D + 2 * ri) = f2{m[t], L};
                 }
-            }
-            while (__builtin_expect(again != 0, 0)) {
-                const int k = __builtin_ctz(again), rk = row0 + STREAM_ROWS * t + k, tk = rk / a.group, hk = h * a.group + rk % a.group;
-                again &= again - 1;
-                float wm, wl, acc[D / 64];
-                row_walk<DT, D>(a, q, h, a.qkv + (size_t)(q.first + tk) * cols + hk * D, q.pos0 + tk, ALIBI ? a.slopes[hk] * LOG2E : 0.0f, STREAM_KEYS * n0,
-                                STREAM_KEYS * n1, wm, wl, acc);
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    if (whole) a.out[(size_t)(q.first + tk) * a.heads * D + hk * D + 64 * i + lane] = (uint16_t)Elem<DT>::pack(acc[i] * (wl == 0.0f ? 0.0f : 1.0f / wl), 0.0f);
-                    else slot[(STREAM_ROWS * t + k) * D + 64 * i + lane] = acc[i];
-                }
-                if (!whole && lane == 0) *reinterpret_cast<f2*>(slot + TILE_ROWS * D + 2 * (STREAM_ROWS * t + k)) = f2{wm, wl};
             }
         }
         if (!whole && first >= share.u)                // it begins here and ends in another worker's share
@@ -631,16 +615,8 @@ __device__ __forceinline__ void store_rows(const AttnArgs& a, const Tile& tl, in
                                            int wr, int tok, int head)
 {
     constexpr int DTL = D / 32;
-    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, cols = (a.heads + 2 * a.kv_heads) * D;
-    const bool mine = wr + col < tl.n_rows;
-    float total[4] = {0.0f, 0.0f, 0.0f, 0.0f};         // finite if all the lane's sums are
-#pragma unroll
-    for (int d = 0; d < DTL; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) total[i % 4] += o[d][i];
-    uint64_t again = __ballot(!__builtin_isfinite((total[0] + total[1]) + (total[2] + total[3])) && mine);
-    again = (again | again >> 32) & 0xffffffffu;       // rows to be done again: a bit per column, of either half
-    const bool store = mine && !(again >> col & 1);
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const bool store = wr + col < tl.n_rows;
     float* const ml = part + (size_t)TILE_ROWS_Q * D;
     if (part) {
         if (store) {
@@ -669,22 +645,9 @@ __device__ __forceinline__ void store_rows(const AttnArgs& a, const Tile& tl, in
                 if (store) *reinterpret_cast<u32x4*>(orow + 8 * half + 32 * d + 8 * b) = x;
             }
     }
-    while (__builtin_expect(again != 0, 0)) {
-        const int k = __builtin_ctzll(again), rk = tl.row0 + wr + k, tk = rk / a.group, hk = h * a.group + rk % a.group;
-        again &= again - 1;
-        float wm, wl, acc[D / 64];
-        row_walk<DT, D>(a, tl.q, h, a.qkv + (size_t)(tl.q.first + tk) * cols + hk * D, tl.q.pos0 + tk, a.slopes ? a.slopes[hk] * LOG2E : 0.0f, TILE_KEYS * ks.begin,
-                        TILE_KEYS * ks.end, wm, wl, acc);
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            if (part) part[(size_t)(wr + k) * D + 64 * i + lane] = acc[i];
-            else a.out[(size_t)(tl.q.first + tk) * a.heads * D + hk * D + 64 * i + lane] = (uint16_t)Elem<DT>::pack(acc[i] * (wl == 0.0f ? 0.0f : 1.0f / wl), 0.0f);
-        }
-        if (part && lane == 0) *reinterpret_cast<f2*>(ml + 2 * (wr + k)) = f2{wm, wl};
-    }
 }
 
-extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];              // K, K, V, V (dynamic: ahead of a read of a named array the compiler waits for every load into it)
+extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];              // K, K, V, V, a word per wave (dynamic: ahead of a read of a named array the compiler waits for every load into it)
 
 template <int DT, int D, bool ALIBI, bool PAGED>
 __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
@@ -787,6 +750,11 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         va[d] = (uint32_t)(2 * TILE_BYTES + row * D * 2 + 16 * (chunk ^ v_swizzle<D>(row)) + 8 * (lane & 1));
     }
 
+    // keys from here on are not seen by every row of the tile; and whether a wave has set values of theirs to zero, in LDS behind the tiles
+    const int first_hidden = min(tl.key_end, q.pos0 + tl.row0 / a.group + 1);
+    uint32_t* const odd_values = reinterpret_cast<uint32_t*>(smem_raw + 4 * TILE_BYTES);
+    if (lane == 0) odd_values[wave] = 0;
+
     float near[ALIBI ? 16 : 1];                        // bias of a register's key within its 32
     if constexpr (ALIBI)
 #pragma unroll
@@ -804,6 +772,24 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
             for (int i = 0; i < FILLS; ++i) {
                 const int row = 16 * wave + ROWS * i + lane / CH;
                 if ((bad >> wave & 1) || j0 + row >= tl.key_end) *reinterpret_cast<u32x4*>(smem_raw + 2 * TILE_BYTES + buf * TILE_BYTES + (16 * wave + ROWS * i) * D * 2 + 16 * lane) = u32x4{};
+            }
+        }
+        if (j0 + 16 * wave + 16 > first_hidden && first_hidden < tl.key_end) {      // the wave's keys are not seen by every row: none of their values may be infinite or NaN
+            u32x4* const at = reinterpret_cast<u32x4*>(smem_raw + (2 + buf) * TILE_BYTES + 16 * wave * D * 2 + 16 * lane);
+            float probe = 0.0f;
+#pragma unroll
+            for (int i = 0; i < FILLS; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) probe = Elem<DT>::probe_pair(at[64 * i][e], probe);
+            if (__builtin_expect(__any(probe != probe), 0)) {
+#pragma unroll 1
+                for (int i = 0; i < FILLS; ++i) {
+                    u32x4 x = at[64 * i];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = without(x[e], not_finite<DT>(x[e]));
+                    at[64 * i] = x;
+                }
+                odd_values[wave] = 1;
             }
         }
         __syncthreads();                               // everybody's part has landed, and the tile before is no longer read
@@ -898,6 +884,20 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         }
     }
     if (!active) return;
+    if (__builtin_expect((odd_values[0] | odd_values[1] | odd_values[2] | odd_values[3]) != 0, 0))      // all written ahead of the last tile's barrier
+#pragma unroll 1
+        for (int j = max(TILE_KEYS * ks.begin, first_hidden & ~15); j < min(TILE_KEYS * ks.end, tl.key_end); ++j) {
+            const uint16_t* row = odd_value_row<DT, D>(a, q, h, j);
+            if (!row) continue;
+#pragma unroll
+            for (int d = 0; d < DTL; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const u32x2 x = *reinterpret_cast<const u32x2*>(row + 32 * d + 2 * i + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[d][i + e] += odd_element<DT>(x[e / 2], e % 2, j <= p);
+                }
+        }
     const f2 l2 = both_halves(l);
     store_rows<DT, D>(a, tl, h, ks, tile_part<D>(a, ks, h, v, split), o, m, l2[0] + l2[1], wr0, tok, head);
 }
@@ -998,6 +998,22 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
     return p;
 }
 
+// LDS of a workgroup of the tile kernel: its tiles and a word per wave.  Allowed once per kernel and device where it is more than 64 KB.
+constexpr size_t tile_lds(int d) { return (size_t)4 * TILE_KEYS * d * 2 + 4 * sizeof(uint32_t); }
+template <auto KERNEL>
+static hipError_t allow_lds(size_t bytes)
+{
+    static std::once_flag flags[64];
+    static hipError_t results[64];
+    int dev = 0;
+    if (bytes <= 65536) return hipSuccess;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+    std::call_once(flags[dev], [&] { results[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); });
+    return results[dev];
+}
+
 template <int DT, int D>
 static hipError_t launch_attention(const AttentionPlan& p, const AttnArgs& a, float* part, hipStream_t s)
 {
@@ -1016,7 +1032,7 @@ static hipError_t launch_attention(const AttentionPlan& p, const AttnArgs& a, fl
     tl.part = part + p.stream_floats;
     const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
     const unsigned grid = (unsigned)(a.kv_heads * classes) * (unsigned)((p.tiles + classes - 1) / classes) * (unsigned)p.splits;
-    constexpr size_t smem = 4 * TILE_KEYS * D * 2;
+    constexpr size_t smem = tile_lds(D);
 #define LPQ_ALIBI(KERNEL, GRID, SMEM, ...)                                                                              \
     do {                                                                                                                \
         if (alibi) KERNEL(true)<<<GRID, 256, SMEM, s>>>(__VA_ARGS__);                                                   \
@@ -1027,6 +1043,9 @@ static hipError_t launch_attention(const AttentionPlan& p, const AttnArgs& a, fl
 #define LPQ_STREAM2(A) stream_attention_kernel<DT, D, 2, A>
 #define LPQ_TILE_PAGED(A) tile_attention_kernel<DT, D, A, true>
 #define LPQ_TILE_PACKED(A) tile_attention_kernel<DT, D, A, false>
+#define LPQ_ALLOW(KERNEL) (alibi ? allow_lds<&KERNEL(true)>(smem) : allow_lds<&KERNEL(false)>(smem))
+    const hipError_t allowed = !p.tile ? hipSuccess : mixed ? LPQ_ALLOW(LPQ_MIXED) : a.kp ? LPQ_ALLOW(LPQ_TILE_PAGED) : LPQ_ALLOW(LPQ_TILE_PACKED);
+    if (allowed != hipSuccess) return allowed;
     if (mixed) LPQ_ALIBI(LPQ_MIXED, streams + grid, smem, st, tl);
     else {
         if (p.stream_tiles == 1) LPQ_ALIBI(LPQ_STREAM1, streams, 0, st);

@@ -498,6 +498,117 @@ def test_later_tokens_do_not_matter(q, val):
     assert not bool(torch.isfinite(out[q - 1]).any())
 
 
+def odd_reference_of(plain):
+    """attention_ref where values may be infinite or NaN: every weight is positive, so such a value makes its feature what it is itself, for the rows that see
+    it and no others.  A weight that rounds to zero makes an infinity NaN in a product; beside a largest weight of 1 or more (E is then infinite) that is one of at
+    most half of fp16's smallest step, 2^-25, or, in bf16, whose steps are smaller, one below 2^-126: the hardware's exponential has no subnormal results."""
+    import torch
+
+    def ref(q, k, v, ok, pos, slopes):
+        fin, group, zero = torch.isfinite(v), q.shape[1] // k.shape[1], {torch.float16: 2.0**-25, torch.bfloat16: 2.0**-126}[q.dtype]
+        out, A, E = plain(q, k, torch.where(fin, v, torch.zeros_like(v)), ok, pos, slopes)
+        for j in torch.nonzero(~fin.all(2).all(1) & ok).flatten().tolist():
+            sees = pos >= j
+            rest = torch.where(fin[j], torch.zeros_like(v[j]), v[j]).double().repeat_interleave(group, 0)
+            out[sees] += rest
+            for t in torch.nonzero(sees).flatten().tolist():
+                kt = k[:int(pos[t]) + 1].double().repeat_interleave(group, 1)
+                s = (q[t].double()[None] * kt).sum(2) / math.sqrt(q.shape[2])
+                if slopes is not None:
+                    s = s + slopes.double()[None] * (torch.arange(len(kt), device="cuda") - pos[t]).double()[:, None]
+                s[~ok[:len(kt)]] = -math.inf
+                small = torch.exp(s[j] - s.amax(0)) <= 1.01 * zero
+                E[t] = torch.where(small[:, None] & torch.isinf(rest), torch.full_like(E[t], math.inf), E[t])
+        return out, A, E
+
+    return ref
+
+
+def check_odd(got, parts, what=""):
+    import torch
+    u = {torch.float16: 2.0**-11, torch.bfloat16: 2.0**-8}[got.dtype]
+    for (r0, r1), (out, A, E) in parts:
+        if r1 == r0:
+            continue
+        g, fin = got[r0:r1].double().view(out.shape), torch.isfinite(out)
+        same = (g == out) | (torch.isnan(g) & (torch.isnan(out) | torch.isinf(E)))
+        tol = u * (A + out.abs()) + E + u * (out.abs() + u * A + E) + 2.0**-25
+        bad = torch.nonzero(~torch.where(fin, (g - out).abs() <= tol, same))
+        assert bad.shape[0] == 0, "%s: rows %d..%d, %d elements, the first at %s" % (what, r0, r1, bad.shape[0], bad[0].tolist())
+
+
+INF, NAN = math.inf, math.nan
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("past,q,H,KV,d,P,alibi", [
+    (200, 1, 8, 2, 64, 16, False), (70, 3, 8, 2, 128, 16, True), (0, 4, 4, 4, 64, 64, False), (900, 16, 4, 2, 128, 32, False), (31, 12, 34, 17, 64, 16, True),
+    (40, 33, 2, 2, 128, 16, False), (100, 140, 8, 2, 64, 64, True), (2000, 60, 4, 1, 128, 32, False), (0, 300, 3, 3, 128, 16, True), (250, 270, 2, 1, 64, 256, False),
+])
+def test_infinite_values_reach_the_rows_that_see_them(past, q, H, KV, d, P, alibi, dt, monkeypatch):
+    """Single infinite and NaN elements of values: in the first position, in cached ones, in the new tokens' own from the first to the last."""
+    import torch
+    p = Paged([(past, q), (past // 2, q), (5, 1)], H, KV, d, P, dt, 2)
+    p.qkv[:, :H * d] *= 0.125
+    r = random.Random(past + q)
+    new = sorted({past, past + q // 2, past + q // 3, past + q - 1, past + r.randrange(q)})
+    for n, j in enumerate([0, past // 3] + new):
+        for val in (INF, -INF, NAN)[n % 3:][:2]:
+            p.v[p.table[0][j // P], r.randrange(KV), j % P, r.randrange(d)] = val
+    monkeypatch.setitem(globals(), "attention_ref", odd_reference_of(attention_ref))
+    check_odd(*p.run(alibi, max_q=q), what="paged")
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("lens,H,KV,d,alibi", [([5, 40], 4, 2, 64, False), ([130, 64, 1], 4, 4, 128, True), ([300, 17], 6, 2, 128, False), ([513], 20, 4, 64, True), ([90, 200], 40, 1, 64, False)])
+def test_infinite_values_of_packed_rows(lens, H, KV, d, alibi, dt, monkeypatch):
+    import torch
+    r = random.Random(sum(lens))
+
+    def edit(x):
+        x[:, :H * d] *= 0.125
+        cu = np.concatenate([[0], np.cumsum(lens)])
+        for s, n in enumerate(lens):
+            for i, j in enumerate(sorted({0, n // 2, n - 1, r.randrange(n), r.randrange(n)})):
+                x[cu[s] + j, (H + KV) * d + r.randrange(KV * d)] = (INF, -INF, NAN)[i % 3]
+
+    monkeypatch.setitem(globals(), "attention_ref", odd_reference_of(attention_ref))
+    check_odd(*packed_run(lens, H, KV, d, dt, alibi, 1, edit=edit), what="packed %s" % lens)
+
+
+def test_an_infinite_value_costs_little():
+    """One infinite element in the first value row, which every row sees; and one in every value row, so that some are at every diagonal."""
+    import torch
+    H, KV, d, n = 8, 2, 128, 3000
+
+    def time_of(call):
+        for _ in range(2):
+            call()
+        torch.cuda.synchronize()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(3):
+            call()
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b) / 3
+
+    qkv = torch.randn((n, (H + 2 * KV) * d), generator=gen(1), device="cuda").half()
+    k, v = (torch.randn((n // 16 + 1, KV, 16, d), generator=gen(2 + i), device="cuda").half() for i in range(2))
+    table, cu = ints([list(range(n // 16 + 1))]), ints([0, n])
+    few, cu_few, kv = qkv[:4].contiguous(), ints([0, 4]), ints([n])
+    calls = (lambda: lpq.lpq_packed_attention(qkv, cu, H, KV), lambda: lpq.lpq_paged_attention(qkv, k, v, table, cu, kv),
+             lambda: lpq.lpq_paged_attention(few, k, v, table, cu_few, kv))
+    plain = [time_of(c) for c in calls]
+    qkv[0, (H + KV) * d + 3] = v[0, :, 0, 3] = INF
+    first = [time_of(c) for c in calls]
+    qkv[:, (H + KV) * d + 3] = v[:, :, :, 3] = INF
+    every = [time_of(c) for c in calls]
+    print("ms without, one, in every row:", plain, first, every)
+    assert all(b <= 5 * a for a, b in zip(plain, first)), (plain, first)
+    assert all(b <= 50 * a for a, b in zip(plain, every)), (plain, every)
+
+
 def test_nan_throughout():
     """A batch whose values, or queries, are NaN everywhere: NaN everywhere, and no row is walked to its end on the way."""
     import torch
