@@ -336,6 +336,7 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
                 load_v(n0 + x, x);
             }
         auto step = [&](int n, int x) {
+#pragma clang fp contract(off)                         // an exponent is a rounded score less the largest rounded score: at most zero, whatever their size
             const int key0 = STREAM_KEYS * n;
             const uint32_t bad = bad_of[x];
             const bool plain = bad == 0 && key0 + STREAM_KEYS <= all_see, more = n + DEPTH < n_last;
@@ -564,6 +565,7 @@ template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D ==
 // log2 of what a row's maximum may lag behind its largest score: sums are then at most 2^8 larger.  Renewed with every larger score there is hardly a
 // tile without 32 rows' sums being multiplied: one prompt of 5801 tokens 684 us, so 655; its error in bf16 1.9e-3, so 2.1e-3; in fp16 2.2e-4 and 2.3e-4.
 constexpr float LAZY = 8.0f;
+constexpr float LARGE_SCORE = 0x1p22f;                 // half of the last place of scores below: at most a quarter
 // Of a split.  At least 4 / 8 key tiles, us: 64 tokens behind 6000 positions 23 + 9 / 22 + 7, 512 tokens of 16 heads over 2 behind 4000 32 + 9 / 30 + 7; 16: 33 + 5 both.
 constexpr int LEAST_KEY_TILES = 8, LONG_KEY_TILES = 48;
 
@@ -740,6 +742,7 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;                     // the maximum in use of the lane's row; this lane's part of its sum
+    bool large = false;                                // the maximum of some row of the wave is
     // operand reads, bytes within a buffer
     uint32_t ka[KS], va[DTL];
 #pragma unroll
@@ -849,7 +852,10 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         float mx = ALIBI ? fmaxf(mk[0] + base[0], mk[1] + base[1]) : fmaxf(mk[0], mk[1]) * c;
         const f2 m2 = both_halves(mx);
         mx = fmaxf(m2[0], m2[1]);
-        if (__any(mx > m + LAZY)) {
+        // An exponent is c s - m by one FMA, m the rounded product of a largest s (or s + base - m, likewise): up to half of m's last place off.  Where that is much,
+        // products are rounded first (0 to 1.5 % of a call's time for asking).
+        if (__builtin_expect(__any(mx > m + LAZY) || large, 0)) {
+#pragma clang fp contract(off)
             const float mn = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
             m = mn;
             l *= alpha;
@@ -857,8 +863,15 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
             for (int d = 0; d < DTL; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+            large = __any(__builtin_fabsf(m) >= LARGE_SCORE && m != -INFINITY);
+            if (__builtin_expect(large, 0))
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[kt][i] = (ALIBI ? s[kt][i] + base[kt] : s[kt][i] * c) - (m == -INFINITY ? 0.0f : m);
         }
-        const float ms = m == -INFINITY ? 0.0f : m;
+        const float ms = m == -INFINITY ? 0.0f : m, by = large ? 1.0f : c;
+        const float from[2] = {large ? 0.0f : ms - base[0], large ? 0.0f : ms - base[1]};
         V8 pf[4];                                      // P^T operands of the four 16-key steps
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -867,8 +880,8 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
                 u32x4 x;
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e] + (base[kt] - ms) : __builtin_fmaf(s[kt][i + e], c, -ms));
-                    const float e1 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e + 1] + (base[kt] - ms) : __builtin_fmaf(s[kt][i + e + 1], c, -ms));
+                    const float e0 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e] - from[kt] : __builtin_fmaf(s[kt][i + e], by, -from[kt]));
+                    const float e1 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e + 1] - from[kt] : __builtin_fmaf(s[kt][i + e + 1], by, -from[kt]));
                     x[e / 2] = Elem<DT>::pack(e0, e1);
                     l = Elem<DT>::add_pair(x[e / 2], l);
                 }

@@ -632,6 +632,38 @@ def test_large_scores():
     check_attention(*p.run(max_q=30), what="equal")
 
 
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_beyond_24_bits(d, dt, biases):
+    """Scores so large that neighbours in 32 bits are tens or hundreds apart, each of them exact: the visible keys with the largest share the weight equally, the
+    others have none.  Off by the output's rounding, and 2^-20 for 32-bit sums and the division; the weights are equal, so their rounding is gone.  (With biases
+    of zero: the kernels' other form.)"""
+    import torch
+    u, r = {"fp16": 2.0**-11, "bf16": 2.0**-8}[dt], random.Random(d)
+    seqs, H, KV = [(300, 1), (0, 300), (70, 90), (500, 6), (0, 1), (64, 17)], 4, 2
+    for max_q, step in ((300, 2048.0), (300, 4.0), (6, 2048.0)):
+        p = Paged([(a, min(b, max_q)) for a, b in seqs], H, KV, d, 32, dt, 1)
+        p.qkv[:, :H * d] = 16384.0
+        levels = [torch.tensor([r.randint(-7, 7) for _ in range(a + b)], device="cuda") for a, b in p.seqs]
+        for s, lv in enumerate(levels):
+            for i in range(0, len(lv), 32):
+                n = min(32, len(lv) - i)
+                p.k[p.table[s][i // 32], :, :n] = (lv[i:i + n] * step).to(p.k.dtype)[None, :, None]
+        out = torch.full((p.M, H * d), 77.0, dtype=p.qkv.dtype, device="cuda")
+        slopes = torch.zeros(H, device="cuda") if biases else None
+        lpq.lpq_paged_attention(p.qkv, p.k, p.v, ints(p.table), ints(p.cu), ints([a + b for a, b in p.seqs]), max_q=max_q, alibi_slopes=slopes, out=out)
+        for s, (past, n) in enumerate(p.seqs):
+            L = past + n
+            v = p.v[torch.tensor([p.table[s][j // 32] for j in range(L)], device="cuda"), :, torch.arange(L, device="cuda") % 32].double()
+            for t in range(n):
+                seen = levels[s][:past + t + 1]
+                rows = v[:past + t + 1][seen == seen.max()].repeat_interleave(H // KV, 1)
+                want, size = rows.mean(0), rows.abs().mean(0)
+                err = (out[p.cu[s] + t].double().view(H, d) - want).abs()
+                assert bool((err <= u * want.abs() + 2.0**-20 * size + 2.0**-25).all()), (max_q, step, s, t, float(err.max()))
+
+
 def test_pool_past_32_bits():
     """Pages more than 2^31 elements into the pool."""
     import torch
