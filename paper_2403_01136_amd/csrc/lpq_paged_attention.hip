@@ -6,9 +6,12 @@
 //
 // Two kernels.  The streaming kernel (few rows per sequence: decode) reads the pages once, straight into registers, as fast as the memory gives them.
 // The tile kernel (prompts and chunks) shares tiles of keys through LDS between 128 rows and is bound by the matrix and vector units.
-// Both keep a running maximum and sum per row in fp32 and take exponents to base 2.  Weights are rounded to the inputs' type for the matrix units, and the sum
+// Both keep a running reference (about the largest score) and sum per row in fp32 and take exponents to base 2.  Weights are rounded to the inputs' type for the matrix units, and the sum
 // that divides is of the rounded ones (pairs of them by one v_dot2, exact for subnormal weights too): what rounding does to a weight that outweighs the
 // others then cancels.  (One prompt of 5801 tokens in bf16 with sums of unrounded weights: 2.2e-3 from 64 bits; so 2.1e-3; the output's rounding alone 1.6e-3.)
+//
+// In fp16 a weight of 2^-25 beside 1 would be zero, and lost the tens of thousands of them that a long context may have: there a row's largest weight is 2^15 (tile
+// kernel: 2^7 to 2^15) beside a smallest one of 2^-24.
 //
 // Keys that no row may see (behind the sequence's end, pages that are not in the pool) are read from page 0 or a stale page, their scores are replaced and
 // their values set to zero.  A value that only some rows of a tile see stays in the products, at weight zero for the others, and must be finite: what is not is
@@ -42,6 +45,7 @@ template <> struct Elem<LPQ_DT_FP16> {
     static __device__ __forceinline__ float add_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, p), h2{1, 1}, c, false); }
     static __device__ __forceinline__ float probe_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, p), h2{0, 0}, c, false); }
     enum { EXPONENT_STEP = 0x04000400 };                                        // one in the exponents' last places
+    enum { TOP = 15 };                                                          // log2 of the largest weight
 };
 template <> struct Elem<LPQ_DT_BF16> {
     typedef __bf16 t;
@@ -52,6 +56,7 @@ template <> struct Elem<LPQ_DT_BF16> {
     static __device__ __forceinline__ float add_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, p), bf2{1.0f, 1.0f}, c, false); }
     static __device__ __forceinline__ float probe_pair(uint32_t p, float c) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, p), bf2{0.0f, 0.0f}, c, false); }
     enum { EXPONENT_STEP = 0x00800080 };
+    enum { TOP = 0 };
 };
 
 // What a launch is about.  Pointers are to 16-bit elements.
@@ -97,6 +102,8 @@ __device__ __forceinline__ int page_of_group(const AttnArgs& a, int s, int g)
 
 // Which of a pair of elements are infinite or NaN: bit 15 and bit 31.  An exponent of all ones carries into the sign's place.
 template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t pair) { return ((pair & 0x7fff7fffu) + (uint32_t)Elem<DT>::EXPONENT_STEP) & 0x80008000u; }
+// What scores are taken from so that the largest, mx, has weight 2^top; without that factor where it would be lost beside the score.
+__device__ __forceinline__ float reference(float mx, int top) { return top == 0 || !(__builtin_fabsf(mx) < 0x1p20f) ? mx : mx - (float)top; }
 // The pair without the elements that `odd`, the above, names.
 __device__ __forceinline__ uint32_t without(uint32_t pair, uint32_t odd) { return pair & ~(odd | (odd - (odd >> 15))); }
 // Element e of a pair if it is infinite or NaN and `seen`, else zero.
@@ -370,8 +377,8 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
                 f2 z = both_rows(mx);
                 z = both_halves(fmaxf(z[0], z[1]));
                 mx = fmaxf(z[0], z[1]);
-                if (__any(mx > m[t])) {
-                    const float mn = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - (mn == -INFINITY ? 0.0f : mn));
+                if (__any(mx - m[t] > (float)Elem<DT>::TOP)) {
+                    const float mn = fmaxf(m[t], reference(mx, Elem<DT>::TOP)), alpha = __builtin_amdgcn_exp2f(m[t] - (mn == -INFINITY ? 0.0f : mn));
                     l[t] *= alpha;
 #pragma unroll
                     for (int e = 0; e < F; ++e) o[t][e] *= alpha;
@@ -564,7 +571,7 @@ template <int D> __device__ __forceinline__ int v_swizzle(int row) { return D ==
 
 // log2 of what a row's maximum may lag behind its largest score: sums are then at most 2^8 larger.  Renewed with every larger score there is hardly a
 // tile without 32 rows' sums being multiplied: one prompt of 5801 tokens 684 us, so 655; its error in bf16 1.9e-3, so 2.1e-3; in fp16 2.2e-4 and 2.3e-4.
-constexpr float LAZY = 8.0f;
+constexpr int LAZY = 8;
 constexpr float LARGE_SCORE = 0x1p22f;                 // half of the last place of scores below: at most a quarter
 // Of a split.  At least 4 / 8 key tiles, us: 64 tokens behind 6000 positions 23 + 9 / 22 + 7, 512 tokens of 16 heads over 2 behind 4000 32 + 9 / 30 + 7; 16: 33 + 5 both.
 constexpr int LEAST_KEY_TILES = 8, LONG_KEY_TILES = 48;
@@ -742,6 +749,7 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;                     // the maximum in use of the lane's row; this lane's part of its sum
+    constexpr int TOP = Elem<DT>::TOP ? Elem<DT>::TOP - LAZY : 0;
     bool large = false;                                // the maximum of some row of the wave is
     // operand reads, bytes within a buffer
     uint32_t ka[KS], va[DTL];
@@ -854,9 +862,9 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         mx = fmaxf(m2[0], m2[1]);
         // An exponent is c s - m by one FMA, m the rounded product of a largest s (or s + base - m, likewise): up to half of m's last place off.  Where that is much,
         // products are rounded first (0 to 1.5 % of a call's time for asking).
-        if (__builtin_expect(__any(mx > m + LAZY) || large, 0)) {
+        if (__builtin_expect(__any(mx - m > TOP + LAZY) || large, 0)) {
 #pragma clang fp contract(off)
-            const float mn = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+            const float mn = fmaxf(m, reference(mx, TOP)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
             m = mn;
             l *= alpha;
 #pragma unroll

@@ -664,6 +664,27 @@ def test_scores_beyond_24_bits(d, dt, biases):
                 assert bool((err <= u * want.abs() + 2.0**-20 * size + 2.0**-25).all()), (max_q, step, s, t, float(err.max()))
 
 
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_many_small_weights(dt, biases):
+    """One key that outweighs each of the others by 2^25.5, which is less than fp16's smallest step beside it, with a value of zero, and thousands of others, with
+    ones.  Off by the weights' and the output's rounding (2 u of the result), exponents of 25.5 from exact 32-bit products (2^-12) and 32-bit sums (2 n 2^-24)."""
+    import torch
+    u, H, KV, d = {"fp16": 2.0**-11, "bf16": 2.0**-8}[dt], 4, 2, 64
+    for past, n in ((60000, 1), (30000, 3), (9000, 64), (3000, 300)):
+        p = Paged([(past, n)], H, KV, d, 64, dt)
+        p.qkv.zero_(), p.k.zero_(), p.v.fill_(1.0)
+        p.qkv[:, :H * d:d] = 16.0
+        at = past // 3
+        p.k[p.table[0][at // 64], :, at % 64, 0] = 8.84375                      # a score of 17.6875, in bf16 of 17.75
+        p.v[p.table[0][at // 64], :, at % 64] = 0.0
+        out = torch.full((p.M, H * d), 77.0, dtype=p.qkv.dtype, device="cuda")
+        lpq.lpq_paged_attention(p.qkv, p.k, p.v, ints(p.table), ints(p.cu), ints([past + n]), max_q=n, alibi_slopes=torch.zeros(H, device="cuda") if biases else None, out=out)
+        rest = (past + torch.arange(n, device="cuda").double()) * math.exp(-2 * float(p.k[p.table[0][at // 64], 0, at % 64, 0]))
+        want = (rest / (1 + rest))[:, None]
+        assert bool(((out.double() - want).abs() <= (2 * u + 2.0**-12 + 2 * (past + n) * 2.0**-24) * want + 2.0**-25).all()), (past, n, float(out.min()), float(want.min()))
+
+
 def test_pool_past_32_bits():
     """Pages more than 2^31 elements into the pool."""
     import torch
