@@ -868,12 +868,13 @@ lpq_status run_batch_attention(const void* qkv, const lpq_attn_cfg* cfg, const l
     if (cst != LPQ_OK) return cst;
     AttentionPlan plan = attention_plan(*cfg, kp != nullptr, n_seqs, M, max_q, max_kv, cus);
     float* part = nullptr;
-    const size_t floats = plan.stream_floats + plan.tile_floats;
-    if (floats) {
-        const lpq_status s = workspace(false, floats * sizeof(float), &part);
-        if (s == LPQ_ERR_BUFSIZE) plan.splits = 1, plan.stream_floats = plan.tile_floats = 0;      // no room for parts: nothing is split
-        else if (s != LPQ_OK) return s;
+    auto floats = [&] { return plan.stream_floats + plan.tile_floats; };
+    lpq_status s = floats() ? workspace(false, floats() * sizeof(float), &part) : LPQ_OK;
+    if (s == LPQ_ERR_BUFSIZE) {                        // it cannot grow: what it has room for
+        plan = attention_plan_within(plan, lpq_workspace_bytes() / sizeof(float));
+        s = floats() ? workspace(false, floats() * sizeof(float), &part) : LPQ_OK;
     }
+    if (s != LPQ_OK) return s;
     return launch_batch_attention(plan, *cfg, qkv, kp, vp, pool ? pool->table : nullptr, pool ? page_shift_of(pool->page_size) : 4, pool ? pool->n_pages : 0,
                                   pool ? pool->max_pages : 0, cu_q, kv_lens, slopes, n_seqs, M, out, part, stream) == hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
 }

@@ -214,9 +214,10 @@ struct AttentionPlan {
     int stream_tiles, stream_rows, workers;      // streaming kernel: column tiles of 16 rows (0: not launched), rows that a tile is expected to have, waves
     bool long_lists;                     // few row tiles, cut into many parts each
     bool tile;                           // tile kernel launched
-    int tiles, splits, least;            // its virtual row tiles, K splits at most and key tiles of one at least
-    size_t stream_floats, tile_floats;   // partial results of either (0: whole row tiles only)
+    int tiles, splits, least, key_tiles; // its virtual row tiles, K splits at most and key tiles of one at least; key tiles to expect
+    size_t stream_floats, tile_floats, split_floats;    // partial results of either (0: whole row tiles only), and of one split
 };
+AttentionPlan attention_plan_within(AttentionPlan p, size_t floats);
 AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int M, int max_q, int max_kv, int cus);
 hipError_t launch_batch_attention(const AttentionPlan& p, const lpq_attn_cfg& c, const void* qkv, const void* kp, const void* vp, const int32_t* table,
                                   int shift, int n_pages, int max_pages, const int32_t* cu_q, const int32_t* kv_lens, const float* slopes, int n_seqs, int M,

@@ -1008,14 +1008,26 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int 
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({fill, 16, key_tiles / LEAST_KEY_TILES}));
         const size_t split_bytes = (size_t)p.tiles * c.n_kv_heads * TILE_ROWS_Q * (c.head_dim + 2) * sizeof(float);
         p.splits = (int)std::max<size_t>(1, std::min<size_t>(p.splits, MAX_PART_BYTES / split_bytes));
-        p.least = (int)std::max<int64_t>(LEAST_KEY_TILES, (key_tiles + p.splits - 1) / p.splits);
+        p.key_tiles = (int)key_tiles;
     }
     const size_t d2 = (size_t)c.head_dim + 2;
     if (p.stream_tiles) p.stream_floats = (size_t)p.workers * (2 * STREAM_ROWS * p.stream_tiles * d2 + sizeof(Cut) / sizeof(float));
     // lists of 32 parts and more, where the walks are long enough to be cut that often (4 sequences of up to 800 positions: long lists' form 7.2 us, the other's 4.0)
     p.long_lists = (int64_t)n_seqs * c.n_kv_heads * 32 <= p.workers && max_kv >= 64 * STREAM_KEYS;
     p.stream_rows = (int)std::min<int64_t>(STREAM_ROWS * p.stream_tiles, p.tile ? 2 * STREAM_ROWS : most);
-    if (p.splits > 1) p.tile_floats = (size_t)p.tiles * c.n_kv_heads * p.splits * TILE_ROWS_Q * d2;
+    p.split_floats = (size_t)p.tiles * c.n_kv_heads * TILE_ROWS_Q * d2;
+    return attention_plan_within(p, SIZE_MAX);
+}
+
+// The plan with partial results of at most `floats`: the streaming kernel's, whose room does not depend on the batch, go first, as a long walk that is not cut takes a
+// hundred times as long there; the tile kernel makes as many splits as the rest has room for.
+AttentionPlan attention_plan_within(AttentionPlan p, size_t floats)
+{
+    if (p.stream_floats > floats) p.stream_floats = 0;
+    floats -= p.stream_floats;
+    if (p.tile) p.splits = (int)std::max<size_t>(1, std::min<size_t>(p.splits, floats / p.split_floats));
+    p.tile_floats = p.splits > 1 ? p.split_floats * p.splits : 0;
+    p.least = std::max<int>(LEAST_KEY_TILES, (p.key_tiles + p.splits - 1) / p.splits);
     return p;
 }
 
