@@ -311,7 +311,7 @@ typedef struct {
     int32_t *cu_q;                   /* [n_seqs + 1] first rows (at most M)                                */
     int32_t *kv_lens;                /* [n_seqs] cached positions afterwards; may be `past`                */
     int32_t *slots;                  /* [M] page * page_size + offset of a row's position, -1: none        */
-    int32_t *positions;              /* [M] a row's position, 0 where it has no slot                       */
+    int32_t *positions;              /* [M] a row's position; 0 for rows of starved sequences and of nobody */
     int32_t *info;                   /* [4] rows, pages taken, pages returned, sequences starved           */
 } lpq_page_plan;
 

@@ -190,6 +190,15 @@ def test_plan_odd_integers():
             assert got[name] == want[name], name
 
 
+def test_plan_positions_of_rows_without_a_slot():
+    """A served row has its position also where its table entry is no page of the pool (slot -1); a starved one and one of nobody have 0."""
+    got = run_plan([20, 5, 40], [2, 30, 1], [[3, -1, -1], [9, -1, -1], [0, 1, 99]], [4, 5, 6, 7, 8, 2, -9, -9, -9, -9], 0, 1, 16, 35)
+    assert got["slots"][:2] == [-1, -1] and got["positions"][:2] == [20, 21]        # entry 1 of the first sequence is no page
+    assert got["slots"][2:32] == [-1] * 30 and got["positions"][2:32] == [0] * 30   # two pages wanted, one free
+    assert got["slots"][32] == -1 and got["positions"][32] == 40                    # page 99 of a pool of 10
+    assert got["slots"][33:] == [-1, -1] and got["positions"][33:] == [0, 0] and got["info"][3] == 1
+
+
 # ---- the append -------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dt", ["fp16", "bf16"])
