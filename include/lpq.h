@@ -320,7 +320,8 @@ typedef struct {
  * has; nothing else of the table changes.  A finished sequence's pages go behind the ring's last free page (as far as the ring has
  * room) and can be taken from the next call on; its kv_lens is 0.  A sequence is starved if its rows end behind M, its
  * positions behind max_pages * page_size, or its and its predecessors' needs exceed the free pages: it gets no page, its rows no slots, its kv_lens stays
- * at `past`, and the caller may plan it again later.  Negative past counts as 0, counters are taken into their range.
+ * at `past`, and the caller may plan it again later.  Its rows stay where they are in the batch: attention takes them for its last cached positions (zero, in front of
+ * the first), so their outputs mean nothing and must not be used; they are the rows below cu_q[n_seqs] with slot -1, and info[3] is 0 if there are none.  Negative past counts as 0, counters are taken into their range.
  * With in-place counters and kv_lens a step is the same call every time and can be replayed from a graph.  The other outputs must not overlap the
  * inputs.  n_seqs <= 2048.  Uses none of the library's workspace: plans may overlap other calls that do not touch their buffers.
  * Errors: NULL, SHAPE (page_size, counts, limits above), ALIGN (4 bytes), DEVICE. */

@@ -429,7 +429,7 @@ def _out_and_slopes(qkv, cfg, out, alibi_slopes, stream, dev):
 def lpq_paged_plan(past, q_lens, table, ring, counters, page_size, M, plan=None, stream=None):
     """Where a step's M rows go: past, q_lens int32 [n_seqs]; table int32 [n_seqs][max_pages], ring int32 [n_pages] and counters int32 {head, free} are the
     pool's, the first two updated in place.  plan: the outputs (PagePlan or a tuple in its order), of which kv_lens may be `past` and counters the pool's
-    own; None allocates them.  -> PagePlan."""
+    own; None allocates them.  Outputs of attention for rows of starved sequences (slot -1; info[3] of them) mean nothing.  -> PagePlan."""
     import torch
     i32, n, dev = torch.int32, past.shape[0], _device_of(past)
     if plan is None:

@@ -795,6 +795,67 @@ def test_serving_run(alibi):
     assert sorted(owned + [ring[(head + i) % n_pages].item() for i in range(free)]) == list(range(n_pages))
 
 
+@pytest.mark.parametrize("q", [1, 5, 40])
+def test_starved_sequences_beside_served_ones(q):
+    """A step with too few pages: served sequences are exact, nothing of a starved one is written anywhere but in its own output rows, which are its queries' over
+    the cached positions; with pages returned the same step is exact for it too."""
+    import torch
+    H, KV, d, P, n_pages = 8, 2, 64, 16, 30
+    past, lens = [80, 64, 0, 70], [0, q, q, q]                      # the second and third need pages, the fourth (one token) may not
+    held = [-(-p // P) for p in past]
+    need = [-(-(p + n) // P) - h for p, n, h in zip(past, lens, held)]
+    g = gen(q)
+    k, v = (torch.randn((n_pages, KV, P, d), generator=g, device="cuda").half() for _ in range(2))
+    ids = torch.randperm(n_pages, generator=g, device="cuda").tolist()
+    table, at = [], 0
+    for h in held:
+        table.append(ids[at:at + h] + [-1] * (10 - h))
+        at += h
+    free = need[1]                                                  # the second's
+    ring = ids[at:] + [-1] * at
+    table_d, ring_d, counters, M = ints(table), ints(ring), ints([0, free]), 3 * q + 2
+    qkv = torch.randn((M, (H + 2 * KV) * d), generator=g, device="cuda").half()
+    k0, v0 = k.clone(), v.clone()
+    plan = lpq.lpq_paged_plan(ints(past), ints(lens), table_d, ring_d, counters, P, M)
+    starved = [s for s in range(4) if lens[s] and need[s] and s > 1]
+    assert 2 in starved and plan.info.tolist()[3] == len(starved)
+    cu, kv, slots = plan.cu_q.tolist(), plan.kv_lens.tolist(), plan.slots.tolist()
+    for s in range(4):
+        assert (kv[s] == past[s]) == (s in starved or not lens[s]) and all((x == -1) == (s in starved) for x in slots[cu[s]:cu[s + 1]])
+    lpq.lpq_paged_append(qkv, k, v, plan.slots)
+    mine = torch.zeros((n_pages, P), dtype=torch.bool, device="cuda")
+    for x in slots:
+        if x >= 0:
+            mine[x // P, x % P] = True
+    assert torch.equal(torch.where(mine[:, None, :, None], k0, k), k0) and torch.equal(torch.where(mine[:, None, :, None], v0, v), v0)
+
+    def check(out, kv, cu):
+        rows = table_d.tolist()
+        parts = []
+        for s in range(4):
+            L, r0, r1 = kv[s], cu[s], cu[s + 1]
+            page = torch.tensor([rows[s][j // P] for j in range(L)], dtype=torch.long, device="cuda")
+            off = torch.arange(L, device="cuda") % P
+            parts.append(((r0, r1), attention_ref(qkv[r0:r1, :H * d].view(r1 - r0, H, d), k[page, :, off], v[page, :, off], page >= 0, L - (r1 - r0) + torch.arange(r1 - r0, device="cuda"), None)))
+        check_attention(out, parts, what="starved")
+
+    out = torch.full((M, H * d), 77.0, dtype=torch.float16, device="cuda")
+    lpq.lpq_paged_attention(qkv, k, v, table_d, plan.cu_q, plan.kv_lens, max_q=q, out=out)
+    check(out, kv, cu)
+    assert bool((out[cu[2]:cu[3]] == 0).all())                      # nothing cached
+    # the first sequence has finished: its pages serve the starved in the step after
+    back = lpq.lpq_paged_plan(plan.kv_lens, ints([-1, 0, 0, 0]), table_d, ring_d, plan.counters, P, M)
+    assert back.info.tolist() == [0, 0, held[0], 0]
+    again = [0, 0] + [lens[s] if s in starved else 0 for s in (2, 3)]
+    plan = lpq.lpq_paged_plan(back.kv_lens, ints(again), table_d, ring_d, back.counters, P, M)
+    assert plan.info.tolist()[3] == 0
+    cu, kv = plan.cu_q.tolist(), plan.kv_lens.tolist()
+    lpq.lpq_paged_append(qkv, k, v, plan.slots)
+    out = torch.full((M, H * d), 77.0, dtype=torch.float16, device="cuda")
+    lpq.lpq_paged_attention(qkv, k, v, table_d, plan.cu_q, plan.kv_lens, max_q=q, out=out)
+    check(out, kv, cu)
+
+
 def test_paged_against_packed_and_contiguous():
     """The same prompts through the packed rows, through pages, and (one length, as many K/V heads as heads) through the contiguous cache."""
     import torch
