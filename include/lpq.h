@@ -343,7 +343,7 @@ lpq_status lpq_paged_append(const void *qkv, const lpq_attn_cfg *cfg, const lpq_
  * max_q, max_kv: the largest q_s and kv_lens the caller expects; they choose kernels and splits, and larger ones than that are only slower.
  * Partial results are kept in the library's workspace, up to 290 MiB of them; where a reservation has room for less the work is split less: first the tiles of
  * chunks and prompts, then, below 17 MiB (34 with 17 to 32 rows of a sequence and K/V head), decoding sequences too.  out must not overlap qkv.
- * Errors: NULL, SHAPE (as above, n_seqs in 1 .. 2048, max_q, max_kv < 1), UNSUPPORTED (dtype), ALIGN, DEVICE. */
+ * Errors: NULL, SHAPE (as above, n_seqs in 1 .. 2048, n_seqs * n_kv_heads <= 2^23, max_q, max_kv < 1), UNSUPPORTED (dtype), ALIGN, DEVICE. */
 lpq_status lpq_paged_attention(const void *qkv, const lpq_attn_cfg *cfg, const lpq_page_pool *pool, const void *k_pages, const void *v_pages,
                                const float *alibi_slopes, const int32_t *cu_q, const int32_t *kv_lens, int32_t n_seqs, int32_t M,
                                int32_t max_q, int32_t max_kv, void *out, void *hip_stream);

@@ -858,6 +858,9 @@ lpq_status check_table(const lpq_page_pool* p, int32_t n_seqs)
     return LPQ_OK;
 }
 
+// A place of the tile kernel's list per sequence, tile of rows and K/V head, each a workgroup of 256 threads: fewer than 2^32 threads.
+bool too_many_tiles(const lpq_attn_cfg* c, int32_t n_seqs) { return (int64_t)n_seqs * c->n_kv_heads > (int64_t)1 << 23; }
+
 // kp null: packed rows
 lpq_status run_batch_attention(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* kp, const void* vp, const float* slopes,
                                const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M, int32_t max_q, int32_t max_kv, void* out,
@@ -1012,7 +1015,7 @@ lpq_status lpq_paged_attention(const void* qkv, const lpq_attn_cfg* cfg, const l
     if (s == LPQ_OK) s = check_pool(pool);
     if (s == LPQ_OK) s = check_table(pool, n_seqs);
     if (s != LPQ_OK) return s;
-    if (max_q < 1 || max_kv < 1) return LPQ_ERR_SHAPE;
+    if (max_q < 1 || max_kv < 1 || too_many_tiles(cfg, n_seqs)) return LPQ_ERR_SHAPE;
     if (misaligned(qkv) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out) || misaligned4(alibi_slopes) || misaligned4(cu_q) ||
         misaligned4(kv_lens) || misaligned4(pool->table))
         return LPQ_ERR_ALIGN;
@@ -1026,7 +1029,7 @@ lpq_status lpq_packed_attention(const void* qkv, const lpq_attn_cfg* cfg, const 
     if (!qkv || !cfg || !cu_q || !out) return LPQ_ERR_NULL;
     const lpq_status s = check_heads(cfg, M);
     if (s != LPQ_OK) return s;
-    if (n_seqs < 1 || n_seqs > PAGED_MAX_SEQS || max_q < 1) return LPQ_ERR_SHAPE;
+    if (n_seqs < 1 || n_seqs > PAGED_MAX_SEQS || max_q < 1 || too_many_tiles(cfg, n_seqs)) return LPQ_ERR_SHAPE;
     if (misaligned(qkv) || misaligned(out) || misaligned4(alibi_slopes) || misaligned4(cu_q)) return LPQ_ERR_ALIGN;
     return run_batch_attention(qkv, cfg, nullptr, nullptr, nullptr, alibi_slopes, cu_q, nullptr, n_seqs, M, max_q, std::min(max_q, M), out,
                                static_cast<hipStream_t>(hip_stream));

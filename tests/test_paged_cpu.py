@@ -192,6 +192,13 @@ def test_attention_refusals():
     assert paged(k=FAKE + 8) == paged(v=FAKE + 8) == paged(kv=FAKE + 2) == paged(p=pool(table=FAKE + 2)) == ALIGN
 
 
+def test_more_tiles_than_a_launch_has_threads_for_are_refused():
+    L = lpq.load_library()
+    many = cfg(heads=8192, kv=8192)                                   # M * heads is 2^24 and allowed; 2048 sequences of 8192 K/V heads are not
+    assert L.lpq_paged_attention(FAKE, many, pool(), FAKE, FAKE, None, FAKE, FAKE, 2048, 2048, 1, 1, FAKE, None) == SHAPE
+    assert L.lpq_packed_attention(FAKE, many, None, FAKE, 2048, 2048, 1, FAKE, None) == SHAPE
+
+
 def test_binding_refuses_host_tensors():
     import torch
     x, pages, i = torch.zeros((1, 256), dtype=torch.float16), torch.zeros((1, 1, 16, 64), dtype=torch.float16), torch.zeros(2, dtype=torch.int32)
