@@ -993,3 +993,48 @@ def test_captured_decode_loop():
         assert torch.equal(other.run(max_q=40)[0], other_want)
     for name in ("k", "v", "table", "ring", "counters", "lens"):
         assert torch.equal(s[name], eager[name]), name
+
+
+def test_captured_steps_of_all_kinds():
+    """Plan of more rows than one launch takes, append, mixed paged and packed attention, captured once: replays with other lengths (sequences that decode become
+    chunks and the other way round), eager calls with workspace between them, against the same calls made eagerly."""
+    import torch
+    H, KV, d, P, N, M, n_pages = 8, 2, 128, 16, 4, 7000, 400
+    x = torch.randn((M, (H + 2 * KV) * d), generator=gen(1), device="cuda").half()
+    base_k, base_v = (torch.randn((n_pages, KV, P, d), generator=gen(2 + i), device="cuda").half() for i in range(2))
+    ring = torch.randperm(n_pages, generator=gen(4), device="cuda").to(torch.int32)
+    slopes = slopes_of(H, True)
+
+    def fresh():
+        return dict(k=base_k.clone(), v=base_v.clone(), table=torch.full((N, 140), -1, dtype=torch.int32, device="cuda"), ring=ring.clone(), counters=ints([0, n_pages]),
+                    lens=ints([0] * N), q=ints([0] * N), plan=[torch.zeros(m, dtype=torch.int32, device="cuda") for m in (N + 1, N, M, M, 2, 4)],
+                    out=torch.zeros((M, H * d), dtype=torch.float16, device="cuda"), packed=torch.zeros((M, H * d), dtype=torch.float16, device="cuda"))
+
+    def step(s):
+        plan = (s["plan"][0], s["lens"], s["plan"][2], s["plan"][3], s["counters"], s["plan"][5])
+        lpq.lpq_paged_plan(s["lens"], s["q"], s["table"], s["ring"], s["counters"], P, M, plan=plan)
+        lpq.lpq_paged_append(x, s["k"], s["v"], s["plan"][2])
+        lpq.lpq_paged_attention(x, s["k"], s["v"], s["table"], s["plan"][0], s["lens"], max_q=1500, max_kv=2000, alibi_slopes=slopes, out=s["out"])
+        lpq.lpq_packed_attention(x, s["plan"][0], H, KV, max_q=1500, out=s["packed"])
+
+    steps = [[1500, 20, 0, 300], [1, 1, 900, 1], [1, 200, 40, 1], [-1, 1, 1, 500], [600, 1, -1, 1], [1, 1, 5, 1]]
+    eager, want = fresh(), []
+    for q in steps:
+        eager["q"].copy_(ints(q))
+        step(eager)
+        want.append([eager[n].clone() for n in ("out", "packed", "lens", "counters", "table", "ring")] + [t.clone() for t in (eager["plan"][0], eager["plan"][2], eager["plan"][3], eager["plan"][5])])
+    assert all(w[-1][3].item() == 0 for w in want)
+    s = fresh()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(s)
+    other = Paged([(3000, 1), (100, 40)], 8, 2, 128, 32, "fp16")
+    other_want, _ = other.run(max_q=40)
+    for q, w in zip(steps, want):
+        s["q"].copy_(ints(q))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [s[n] for n in ("out", "packed", "lens", "counters", "table", "ring")] + [s["plan"][i] for i in (0, 2, 3, 5)]
+        assert all(torch.equal(a, b) for a, b in zip(got, w)), q
+        assert torch.equal(other.run(max_q=40)[0], other_want)
