@@ -15,7 +15,7 @@ namespace {
 //   offsets    cu[s] = sum of q before s, at most M
 //   owned      min(ceil(past / P), W);  need = ceil(n / P) - owned if q > 0
 //   starved    rows end behind M, n > W P, or need > 0 and the sum of the needs up to s exceeds the free pages
-// 3.3 us for one sequence, 4.0 for 64 that decode, 8.1 for 1000: kernel start and end and a chain of loads (lengths, scan, table, store).
+// 2.9 us for one sequence, 4.3 for 64 that decode, 8.1 for 1000: kernel start and end and a chain of loads (lengths, scan, table, store).
 // One workgroup: all of it hangs on three prefix sums over the sequences, which are a handful of numbers per thread; what is left is
 // a search (in LDS) per new page, returned page and row.  The lengths and the pool's counters may be updated in place: every thread has read what
 // it needs of them ahead of the first barrier.

@@ -927,9 +927,9 @@ template <int DT, int D, bool ALIBI, bool PAGED>
 __global__ __launch_bounds__(256, 2) void tile_attention_kernel(AttnArgs a) { tile_block<DT, D, ALIBI, PAGED>(a, (int)blockIdx.x); }
 
 // Both for a batch that may have sequences of either kind: the streaming kernel's workgroups, then the tile kernel's, which multiply while the others read.
-// Against a launch of each, us: two chunks of 512 beside 9 sequences that decode, 56 heads (8 K/V heads), biases, 77 so, 71 now; 250 and one chunk, 64 heads (8), 148 / 145;
-// 60 and one chunk, 40 heads (40), 110 / 100; 4 and a chunk of 200, 32 heads (8), 22 / 16.  The tile kernel's first: 62, 210, 144, 15; by turns: 69, 193, 134, 15: streams
-// that begin late end last.  With two column tiles the streaming kernel has more registers than two workgroups a compute unit leave: a launch of each.
+// A launch of each / this one, us: two chunks of 512 beside 9 sequences that decode, 56 heads (8 K/V heads), biases, 74 / 67 with contexts of 100 to 6000, 125 / 117 with 900 to
+// 6000; 250 with up to 2000 and one chunk, 64 heads (8), 150 / 143; 60 with up to 1000 and one chunk, 40 heads (40), 113 / 100; 4 with up to 800 and a chunk of 200, 32 heads
+// (8), 23 / 16.  The tile kernel's workgroups first: 62 (contexts from 100), 210, 144, 15; by turns: 69, 193, 134, 15: streams that begin late end last.  With two column tiles the streaming kernel has more registers than two workgroups a compute unit leave: a launch of each.
 template <int DT, int D, bool ALIBI>
 __global__ __launch_bounds__(256, 2) void mixed_attention_kernel(AttnArgs stream, AttnArgs tile)
 {
