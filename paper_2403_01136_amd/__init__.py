@@ -19,6 +19,7 @@ LINEARS = ("qkv", "out", "fc1", "fc2")
 EXPORTS = ("lpq_packed_sizes", "lpq_quantize_pack", "lpq_quantize_pack_rows", "lpq_load_quantize_pack",
            "lpq_qlinear_prefill", "lpq_qlinear_decode", "lpq_qlinear_fused", "lpq_stage_linears", "lpq_stage_linears_noalloc", "lpq_layernorm",
            "lpq_kv_append", "lpq_attention", "lpq_paged_plan", "lpq_paged_append", "lpq_paged_attention", "lpq_packed_attention",
+           "lpq_cell_page_bytes", "lpq_qk_norm_rotary", "lpq_paged_append4", "lpq_paged_load4", "lpq_paged_attention4",
            "lpq_decoder_layer_workspace", "lpq_decoder_layer", "lpq_variance_indicator",
            "lpq_mem_embedding_bytes", "lpq_mem_layer_bytes", "lpq_mem_kv_bytes", "lpq_latency_fit", "lpq_latency_predict",
            "lpq_plan_objective", "lpq_plan_adabits", "lpq_plan_bitwidth_transfer",
@@ -63,6 +64,11 @@ class lpq_layer_state(ctypes.Structure):
 
 class lpq_attn_cfg(ctypes.Structure):
     _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class lpq_rotary(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("max_pos", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("cos_sin", ctypes.c_void_p), ("q_gamma", ctypes.c_void_p), ("k_gamma", ctypes.c_void_p)]
 
 
 class lpq_page_pool(ctypes.Structure):
@@ -136,6 +142,12 @@ def load_library():
         acfg, pool = ctypes.POINTER(lpq_attn_cfg), ctypes.POINTER(lpq_page_pool)
         L.lpq_paged_plan.argtypes = [pool, vp, vp, i32, i32, ctypes.POINTER(lpq_page_plan), vp]
         L.lpq_paged_append.argtypes = [vp, acfg, pool, vp, vp, vp, i32, vp]
+        L.lpq_cell_page_bytes.argtypes = [i32, i32]
+        L.lpq_cell_page_bytes.restype = ctypes.c_size_t
+        L.lpq_qk_norm_rotary.argtypes = [vp, acfg, ctypes.POINTER(lpq_rotary), vp, vp, i32, vp, vp]
+        L.lpq_paged_append4.argtypes = [vp, acfg, pool, vp, vp, vp, i32, vp]
+        L.lpq_paged_load4.argtypes = [vp, vp, acfg, pool, vp, i32, vp, vp]
+        L.lpq_paged_attention4.argtypes = [vp, acfg, pool, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp]
         L.lpq_paged_attention.argtypes = [vp, acfg, pool, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp]
         L.lpq_packed_attention.argtypes = [vp, acfg, vp, vp, i32, i32, i32, vp, vp]
         L.lpq_decoder_layer_workspace.argtypes = [ctypes.POINTER(lpq_layer), cfgp, i32]
@@ -465,9 +477,14 @@ def lpq_paged_append(qkv, k_pages, v_pages, slots, stream=None):
 def lpq_paged_attention(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None, max_kv=None, alibi_slopes=None, out=None, stream=None):
     """Causal attention of the packed rows over the pages of their sequences: table int32 [n_seqs][max_pages], cu_q int32 [n_seqs + 1], kv_lens int32
     [n_seqs] (new tokens included).  max_q, max_kv: the most to expect (None: the batch, the table).  -> out [M][heads * d]."""
+    return _attention_over(load_library().lpq_paged_attention, "lpq_paged_attention", _paged_cfg(qkv, k_pages, v_pages), qkv, k_pages, v_pages, table, cu_q, kv_lens,
+                           max_q, max_kv, alibi_slopes, out, stream)
+
+
+def _attention_over(call, name, cfg_of, qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q, max_kv, alibi_slopes, out, stream):
     import torch
     i32 = torch.int32
-    dev, cfg, page_size, n_pages = _paged_cfg(qkv, k_pages, v_pages)
+    dev, cfg, page_size, n_pages = cfg_of
     _check_tensor("table", table, i32, 2, dev)
     _check_tensor("cu_q", cu_q, i32, 1, dev)
     _check_tensor("kv_lens", kv_lens, i32, 1, dev)
@@ -476,9 +493,8 @@ def lpq_paged_attention(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None,
         raise ValueError("table, cu_q and kv_lens do not have the same number of sequences")
     out, slopes = _out_and_slopes(qkv, cfg, out, alibi_slopes, stream, dev)
     p = lpq_page_pool(page_size, n_pages, width, table.data_ptr(), None, None)
-    _check(load_library().lpq_paged_attention(qkv.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), slopes, cu_q.data_ptr(), kv_lens.data_ptr(), n, M,
-                                              M if max_q is None else max_q, width * page_size if max_kv is None else max_kv, out.data_ptr(),
-                                              _stream_on(stream, dev)), "lpq_paged_attention")
+    _check(call(qkv.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), slopes, cu_q.data_ptr(), kv_lens.data_ptr(), n, M,
+                M if max_q is None else max_q, width * page_size if max_kv is None else max_kv, out.data_ptr(), _stream_on(stream, dev)), name)
     return out
 
 
@@ -494,6 +510,105 @@ def lpq_packed_attention(qkv, cu_q, n_heads, n_kv_heads, max_q=None, alibi_slope
     _check(load_library().lpq_packed_attention(qkv.data_ptr(), cfg, slopes, cu_q.data_ptr(), cu_q.shape[0] - 1, M, M if max_q is None else max_q, out.data_ptr(),
                                                _stream_on(stream, dev)), "lpq_packed_attention")
     return out
+
+
+# ---- 4-bit paged caches: pages are uint8 [n_pages][kv heads][lpq_cell_page_bytes(page_size, head_dim)] ---------------
+
+LPQ_PAIRS_HALVES, LPQ_PAIRS_ADJACENT = 0, 1
+_CELL_PAGES = {p * (d // 2 + 4): (p, d) for p in (16, 32, 64, 128, 256) for d in (64, 128)}      # bytes of a head's part of a page: no two alike
+
+
+def lpq_cell_page_bytes(page_size, head_dim):
+    """Bytes of one K/V head's part of a page of 4-bit cells."""
+    n = int(load_library().lpq_cell_page_bytes(page_size, head_dim))
+    if n == 0:
+        raise ValueError("no pages of %d positions of %d features" % (page_size, head_dim))
+    return n
+
+
+def _cells_cfg(qkv, k_pages, v_pages):
+    """(device index, attention cfg, page size, pages): K and V pages are uint8 [n_pages][kv heads][bytes of a head's part of a page]."""
+    import torch
+    dev = _device_of(qkv)
+    _check_tensor("qkv", qkv, qkv.dtype, 2, dev)
+    _check_tensor("k_pages", k_pages, torch.uint8, 3, dev)
+    _check_tensor("v_pages", v_pages, torch.uint8, 3, dev)
+    n_pages, kv, size = shape = k_pages.shape
+    if v_pages.shape != shape:
+        raise ValueError("k_pages and v_pages must have the same shape")
+    if size not in _CELL_PAGES:
+        raise ValueError("%d bytes are no head's part of a page" % size)
+    page_size, d = _CELL_PAGES[size]
+    cfg = _attn_cfg(qkv, qkv.shape[1] // d - 2 * kv, kv)
+    if cfg.head_dim != d:
+        raise ValueError("qkv's columns do not match the pages' heads")
+    return dev, cfg, page_size, n_pages
+
+
+def lpq_qk_norm_rotary(qkv, positions, n_heads, n_kv_heads, cos_sin=None, interleaved=False, q_gamma=None, k_gamma=None, eps=1e-6, slots=None, out=None, stream=None):
+    """Norms (q_gamma, k_gamma [d], or None) and rotation (cos_sin fp32 [max_pos][rotary_dim], cosines then sines, or None; interleaved: neighbours are pairs, else
+    halves) of the q and k heads of qkv ([M][(heads + 2 kv heads) * d]) at int32 positions [M].  Rows with a negative entry in slots are left as they are in out.
+    out: qkv itself (None: in place) or another tensor like it, which gets V too.  -> out."""
+    import torch
+    dev = _device_of(qkv)
+    _check_tensor("qkv", qkv, qkv.dtype, 2, dev)
+    cfg, M = _attn_cfg(qkv, n_heads, n_kv_heads), qkv.shape[0]
+    rows = [(name, t) for name, t in (("positions", positions), ("slots", slots)) if t is not None]
+    for name, t in rows:
+        _check_tensor(name, t, torch.int32, 1, dev)
+        if t.shape[0] != M:
+            raise ValueError("%s must have a value per row" % name)
+    for name, t in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
+        if t is not None:
+            _check_tensor(name, t, qkv.dtype, 1, dev)
+            if t.shape[0] != cfg.head_dim:
+                raise ValueError("%s must have a value per feature of a head" % name)
+    rotary_dim = max_pos = 0
+    if cos_sin is not None:
+        _check_tensor("cos_sin", cos_sin, torch.float32, 2, dev)
+        max_pos, rotary_dim = cos_sin.shape
+    if out is None:
+        out = qkv
+    elif out is not qkv:
+        _check_tensor("out", out, qkv.dtype, 2, dev)
+        if out.shape != qkv.shape:
+            raise ValueError("out must have qkv's shape")
+    ptr = lambda t: None if t is None else t.data_ptr()
+    r = lpq_rotary(rotary_dim, LPQ_PAIRS_ADJACENT if interleaved else LPQ_PAIRS_HALVES, max_pos, eps, ptr(cos_sin), ptr(q_gamma), ptr(k_gamma))
+    _check(load_library().lpq_qk_norm_rotary(qkv.data_ptr(), cfg, r, ptr(positions), ptr(slots), M, out.data_ptr(), _stream_on(stream, dev)), "lpq_qk_norm_rotary")
+    return out
+
+
+def lpq_paged_append4(qkv, k_pages, v_pages, slots, stream=None):
+    """K and V of the rows of qkv ([M][(heads + 2 kv heads) * d], fp16 or bf16), quantised, into their slots of pages of 4-bit cells."""
+    _cells_and_slots("lpq_paged_append4", qkv, k_pages, v_pages, slots, stream)
+
+
+def lpq_paged_load4(k_pages, v_pages, slots, out, stream=None):
+    """What the slots hold to the K and V parts of the rows of out ([M][(heads + 2 kv heads) * d], fp16 or bf16: the type that was appended).  -> out."""
+    _cells_and_slots("lpq_paged_load4", out, k_pages, v_pages, slots, stream)
+    return out
+
+
+def _cells_and_slots(name, rows, k_pages, v_pages, slots, stream):
+    import torch
+    dev, cfg, page_size, n_pages = _cells_cfg(rows, k_pages, v_pages)
+    _check_tensor("slots", slots, torch.int32, 1, dev)
+    M = rows.shape[0]
+    if slots.shape[0] != M:
+        raise ValueError("slots must have a value per row")
+    p, L, on = lpq_page_pool(page_size, n_pages, 0, None, None, None), load_library(), _stream_on(stream, dev)
+    if name == "lpq_paged_append4":
+        _check(L.lpq_paged_append4(rows.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr(), M, on), name)
+    else:
+        _check(L.lpq_paged_load4(k_pages.data_ptr(), v_pages.data_ptr(), cfg, p, slots.data_ptr(), M, rows.data_ptr(), on), name)
+
+
+def lpq_paged_attention4(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None, max_kv=None, alibi_slopes=None, out=None, stream=None):
+    """lpq_paged_attention over pages of 4-bit cells.  -> out [M][heads * d]."""
+    cfg_of = _cells_cfg(qkv, k_pages, v_pages)
+    return _attention_over(load_library().lpq_paged_attention4, "lpq_paged_attention4", cfg_of, qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q, max_kv, alibi_slopes,
+                           out, stream)
 
 
 def lpq_decoder_layer(layer, state, phase, n_seqs, T, pos0, x, y=None, workspace=None, stream=None):

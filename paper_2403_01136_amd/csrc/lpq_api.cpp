@@ -861,15 +861,23 @@ lpq_status check_table(const lpq_page_pool* p, int32_t n_seqs)
 // A place of the tile kernel's list per sequence, tile of rows and K/V head, each a workgroup of 256 threads: fewer than 2^32 threads.
 bool too_many_tiles(const lpq_attn_cfg* c, int32_t n_seqs) { return (int64_t)n_seqs * c->n_kv_heads > (int64_t)1 << 23; }
 
-// kp null: packed rows
-lpq_status run_batch_attention(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* kp, const void* vp, const float* slopes,
-                               const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M, int32_t max_q, int32_t max_kv, void* out,
-                               hipStream_t stream)
+// Rows of a batch and slots of the pages, of either kind.
+lpq_status check_rows_and_slots(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* k_pages, const void* v_pages, const int32_t* slots,
+                                int32_t M)
+{
+    if (!qkv || !cfg || !pool || !k_pages || !v_pages || !slots) return LPQ_ERR_NULL;
+    lpq_status s = check_heads(cfg, M);
+    if (s == LPQ_OK) s = check_pool(pool);
+    if (s != LPQ_OK) return s;
+    return misaligned(qkv) || misaligned(k_pages) || misaligned(v_pages) || misaligned4(slots) ? LPQ_ERR_ALIGN : LPQ_OK;
+}
+
+lpq_status run_batch_attention(AttentionSource source, const lpq_attn_cfg* cfg, const AttentionBatch& b, int32_t max_q, int32_t max_kv, hipStream_t stream)
 {
     int cus = 0;
     const lpq_status cst = device_cus(&cus);
     if (cst != LPQ_OK) return cst;
-    AttentionPlan plan = attention_plan(*cfg, kp != nullptr, n_seqs, M, max_q, max_kv, cus);
+    AttentionPlan plan = attention_plan(*cfg, source, b.n_seqs, b.M, max_q, max_kv, cus);
     float* part = nullptr;
     auto floats = [&] { return plan.stream_floats + plan.tile_floats; };
     lpq_status s = floats() ? workspace(false, floats() * sizeof(float), &part) : LPQ_OK;
@@ -878,8 +886,25 @@ lpq_status run_batch_attention(const void* qkv, const lpq_attn_cfg* cfg, const l
         s = floats() ? workspace(false, floats() * sizeof(float), &part) : LPQ_OK;
     }
     if (s != LPQ_OK) return s;
-    return launch_batch_attention(plan, *cfg, qkv, kp, vp, pool ? pool->table : nullptr, pool ? page_shift_of(pool->page_size) : 4, pool ? pool->n_pages : 0,
-                                  pool ? pool->max_pages : 0, cu_q, kv_lens, slopes, n_seqs, M, out, part, stream) == hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
+    return (source == SRC_CELLS ? launch_cell_attention : launch_batch_attention)(plan, *cfg, b, part, stream) == hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
+}
+
+// Attention over pages of either kind.
+lpq_status paged_attention(AttentionSource source, const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* k_pages, const void* v_pages,
+                           const float* alibi_slopes, const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M, int32_t max_q, int32_t max_kv,
+                           void* out, void* hip_stream)
+{
+    if (!qkv || !cfg || !pool || !pool->table || !k_pages || !v_pages || !cu_q || !kv_lens || !out) return LPQ_ERR_NULL;
+    lpq_status s = check_heads(cfg, M);
+    if (s == LPQ_OK) s = check_pool(pool);
+    if (s == LPQ_OK) s = check_table(pool, n_seqs);
+    if (s != LPQ_OK) return s;
+    if (max_q < 1 || max_kv < 1 || too_many_tiles(cfg, n_seqs)) return LPQ_ERR_SHAPE;
+    if (misaligned(qkv) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out) || misaligned4(alibi_slopes) || misaligned4(cu_q) ||
+        misaligned4(kv_lens) || misaligned4(pool->table))
+        return LPQ_ERR_ALIGN;
+    const AttentionBatch b{qkv, k_pages, v_pages, pool->table, page_shift_of(pool->page_size), pool->n_pages, pool->max_pages, cu_q, kv_lens, alibi_slopes, n_seqs, M, out};
+    return run_batch_attention(source, cfg, b, max_q, max_kv, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // namespace
@@ -997,11 +1022,8 @@ lpq_status lpq_paged_plan(const lpq_page_pool* pool, const int32_t* past, const 
 lpq_status lpq_paged_append(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, void* k_pages, void* v_pages, const int32_t* slots,
                             int32_t M, void* hip_stream)
 {
-    if (!qkv || !cfg || !pool || !k_pages || !v_pages || !slots) return LPQ_ERR_NULL;
-    lpq_status s = check_heads(cfg, M);
-    if (s == LPQ_OK) s = check_pool(pool);
+    const lpq_status s = check_rows_and_slots(qkv, cfg, pool, k_pages, v_pages, slots, M);
     if (s != LPQ_OK) return s;
-    if (misaligned(qkv) || misaligned(k_pages) || misaligned(v_pages) || misaligned4(slots)) return LPQ_ERR_ALIGN;
     return launch_paged_append(qkv, *cfg, page_shift_of(pool->page_size), pool->n_pages, k_pages, v_pages, slots, M, static_cast<hipStream_t>(hip_stream)) ==
                    hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
 }
@@ -1010,17 +1032,7 @@ lpq_status lpq_paged_attention(const void* qkv, const lpq_attn_cfg* cfg, const l
                                const float* alibi_slopes, const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M, int32_t max_q,
                                int32_t max_kv, void* out, void* hip_stream)
 {
-    if (!qkv || !cfg || !pool || !pool->table || !k_pages || !v_pages || !cu_q || !kv_lens || !out) return LPQ_ERR_NULL;
-    lpq_status s = check_heads(cfg, M);
-    if (s == LPQ_OK) s = check_pool(pool);
-    if (s == LPQ_OK) s = check_table(pool, n_seqs);
-    if (s != LPQ_OK) return s;
-    if (max_q < 1 || max_kv < 1 || too_many_tiles(cfg, n_seqs)) return LPQ_ERR_SHAPE;
-    if (misaligned(qkv) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out) || misaligned4(alibi_slopes) || misaligned4(cu_q) ||
-        misaligned4(kv_lens) || misaligned4(pool->table))
-        return LPQ_ERR_ALIGN;
-    return run_batch_attention(qkv, cfg, pool, k_pages, v_pages, alibi_slopes, cu_q, kv_lens, n_seqs, M, max_q, max_kv, out,
-                               static_cast<hipStream_t>(hip_stream));
+    return paged_attention(SRC_PAGES, qkv, cfg, pool, k_pages, v_pages, alibi_slopes, cu_q, kv_lens, n_seqs, M, max_q, max_kv, out, hip_stream);
 }
 
 lpq_status lpq_packed_attention(const void* qkv, const lpq_attn_cfg* cfg, const float* alibi_slopes, const int32_t* cu_q, int32_t n_seqs, int32_t M,
@@ -1031,8 +1043,59 @@ lpq_status lpq_packed_attention(const void* qkv, const lpq_attn_cfg* cfg, const 
     if (s != LPQ_OK) return s;
     if (n_seqs < 1 || n_seqs > PAGED_MAX_SEQS || max_q < 1 || too_many_tiles(cfg, n_seqs)) return LPQ_ERR_SHAPE;
     if (misaligned(qkv) || misaligned(out) || misaligned4(alibi_slopes) || misaligned4(cu_q)) return LPQ_ERR_ALIGN;
-    return run_batch_attention(qkv, cfg, nullptr, nullptr, nullptr, alibi_slopes, cu_q, nullptr, n_seqs, M, max_q, std::min(max_q, M), out,
-                               static_cast<hipStream_t>(hip_stream));
+    const AttentionBatch b{qkv, nullptr, nullptr, nullptr, 4, 0, 0, cu_q, nullptr, alibi_slopes, n_seqs, M, out};
+    return run_batch_attention(SRC_ROWS, cfg, b, max_q, std::min(max_q, M), static_cast<hipStream_t>(hip_stream));
+}
+
+size_t lpq_cell_page_bytes(int32_t page_size, int32_t head_dim)
+{
+    return page_shift_of(page_size) < 0 || (head_dim != 64 && head_dim != 128) ? 0 : (size_t)(page_size / 16) * cell_group_bytes(head_dim);
+}
+
+lpq_status lpq_qk_norm_rotary(const void* qkv, const lpq_attn_cfg* cfg, const lpq_rotary* rotary, const int32_t* positions, const int32_t* slots, int32_t M,
+                              void* out, void* hip_stream)
+{
+    if (!qkv || !cfg || !rotary || !out) return LPQ_ERR_NULL;
+    lpq_status s = check_heads(cfg, M);
+    if (s != LPQ_OK) return s;
+    const int turned = rotary->rotary_dim;
+    if (turned < 0 || turned > cfg->head_dim || turned % 16 != 0) return LPQ_ERR_SHAPE;
+    if (turned > 0 && (!rotary->cos_sin || !positions)) return LPQ_ERR_NULL;
+    if (turned > 0 && (rotary->max_pos < 1 || (int64_t)rotary->max_pos * turned > (int64_t)1 << 40)) return LPQ_ERR_SHAPE;
+    if (rotary->pairs != LPQ_PAIRS_HALVES && rotary->pairs != LPQ_PAIRS_ADJACENT) return LPQ_ERR_UNSUPPORTED;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(qkv), to = reinterpret_cast<uintptr_t>(out);
+    const size_t bytes = (size_t)M * (cfg->n_heads + 2 * cfg->n_kv_heads) * cfg->head_dim * 2;
+    if (from != to && from < to + bytes && to < from + bytes) return LPQ_ERR_SHAPE;
+    if ((rotary->q_gamma || rotary->k_gamma) && !(rotary->eps > 0.0f && rotary->eps <= 3.4e38f)) return LPQ_ERR_SHAPE;
+    if (misaligned(qkv) || misaligned(out) || misaligned(rotary->cos_sin) || misaligned(rotary->q_gamma) || misaligned(rotary->k_gamma) || misaligned4(positions) ||
+        misaligned4(slots))
+        return LPQ_ERR_ALIGN;
+    return launch_qk_norm_rotary(qkv, *cfg, *rotary, positions, slots, M, out, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
+}
+
+lpq_status lpq_paged_append4(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, void* k_pages, void* v_pages, const int32_t* slots,
+                             int32_t M, void* hip_stream)
+{
+    const lpq_status s = check_rows_and_slots(qkv, cfg, pool, k_pages, v_pages, slots, M);
+    if (s != LPQ_OK) return s;
+    return launch_paged_append4(qkv, *cfg, page_shift_of(pool->page_size), pool->n_pages, k_pages, v_pages, slots, M, static_cast<hipStream_t>(hip_stream)) ==
+                   hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
+}
+
+lpq_status lpq_paged_load4(const void* k_pages, const void* v_pages, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const int32_t* slots, int32_t M,
+                           void* qkv, void* hip_stream)
+{
+    const lpq_status s = check_rows_and_slots(qkv, cfg, pool, k_pages, v_pages, slots, M);
+    if (s != LPQ_OK) return s;
+    return launch_paged_load4(k_pages, v_pages, *cfg, page_shift_of(pool->page_size), pool->n_pages, slots, M, qkv, static_cast<hipStream_t>(hip_stream)) ==
+                   hipSuccess ? LPQ_OK : LPQ_ERR_DEVICE;
+}
+
+lpq_status lpq_paged_attention4(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* k_pages, const void* v_pages,
+                                const float* alibi_slopes, const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M, int32_t max_q,
+                                int32_t max_kv, void* out, void* hip_stream)
+{
+    return paged_attention(SRC_CELLS, qkv, cfg, pool, k_pages, v_pages, alibi_slopes, cu_q, kv_lens, n_seqs, M, max_q, max_kv, out, hip_stream);
 }
 
 size_t lpq_decoder_layer_workspace(const lpq_layer* layer, const lpq_layer_cfg* cfg, int32_t M)

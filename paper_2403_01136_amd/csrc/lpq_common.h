@@ -210,6 +210,8 @@ hipError_t launch_paged_plan(const lpq_page_pool& pool, int shift, const int32_t
                              hipStream_t s);
 hipError_t launch_paged_append(const void* qkv, const lpq_attn_cfg& c, int shift, int n_pages, void* k_pages, void* v_pages, const int32_t* slots, int M,
                                hipStream_t s);
+// Where attention finds keys and values: the packed rows themselves, pages of 16-bit elements, pages of 4-bit cells.
+enum AttentionSource { SRC_ROWS, SRC_PAGES, SRC_CELLS };
 struct AttentionPlan {
     int stream_tiles, stream_rows, workers;      // streaming kernel: column tiles of 16 rows (0: not launched), rows that a tile is expected to have, waves
     bool long_lists;                     // few row tiles, cut into many parts each
@@ -218,9 +220,24 @@ struct AttentionPlan {
     size_t stream_floats, tile_floats, split_floats;    // partial results of either (0: whole row tiles only), and of one split
 };
 AttentionPlan attention_plan_within(AttentionPlan p, size_t floats);
-AttentionPlan attention_plan(const lpq_attn_cfg& c, bool paged, int n_seqs, int M, int max_q, int max_kv, int cus);
-hipError_t launch_batch_attention(const AttentionPlan& p, const lpq_attn_cfg& c, const void* qkv, const void* kp, const void* vp, const int32_t* table,
-                                  int shift, int n_pages, int max_pages, const int32_t* cu_q, const int32_t* kv_lens, const float* slopes, int n_seqs, int M,
-                                  void* out, float* part, hipStream_t s);
+AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int n_seqs, int M, int max_q, int max_kv, int cus);
+// a batch as the kernels get it
+struct AttentionBatch {
+    const void *qkv, *kp, *vp;
+    const int32_t* table;
+    int shift, n_pages, max_pages;
+    const int32_t *cu_q, *kv_lens;
+    const float* slopes;
+    int n_seqs, M;
+    void* out;
+};
+hipError_t launch_batch_attention(const AttentionPlan& p, const lpq_attn_cfg& c, const AttentionBatch& b, float* part, hipStream_t s);
+hipError_t launch_cell_attention(const AttentionPlan& p, const lpq_attn_cfg& c, const AttentionBatch& b, float* part, hipStream_t s);
+hipError_t launch_qk_norm_rotary(const void* qkv, const lpq_attn_cfg& c, const lpq_rotary& r, const int32_t* positions, const int32_t* slots, int M, void* out,
+                                 hipStream_t s);
+hipError_t launch_paged_append4(const void* qkv, const lpq_attn_cfg& c, int shift, int n_pages, void* k_pages, void* v_pages, const int32_t* slots, int M,
+                                hipStream_t s);
+hipError_t launch_paged_load4(const void* k_pages, const void* v_pages, const lpq_attn_cfg& c, int shift, int n_pages, const int32_t* slots, int M, void* qkv,
+                              hipStream_t s);
 
 }  // namespace lpq

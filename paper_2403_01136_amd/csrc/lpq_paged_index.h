@@ -35,6 +35,13 @@ LPQ_BOTH int page_checked(int id, int n_pages) { return (uint32_t)id < (uint32_t
 LPQ_BOTH int slot_checked(int slot, int n_pages, int page_shift) { return slot >= 0 && (slot >> page_shift) < n_pages ? slot : -1; }
 // First element of head h of a page (pages are [kv heads][page_size][d]).
 LPQ_BOTH int64_t page_element(int page, int h, int kv_heads, int page_shift, int d) { return (((int64_t)page * kv_heads + h) << page_shift) * d; }
+// Bytes of a group of 16 positions of a head in a 4-bit cache: their codes, then 4 bytes of parameters each.
+LPQ_BOTH int cell_group_bytes(int d) { return 16 * (d / 2 + 4); }
+// First byte of such a group, group g of head h of a page (pages are [kv heads][page_size / 16][group]).
+LPQ_BOTH int64_t cell_group(int page, int h, int kv_heads, int page_shift, int g, int d)
+{
+    return ((((int64_t)page * kv_heads + h) << (page_shift - 4)) + g) * cell_group_bytes(d);
+}
 
 // Keys that exist for a sequence: [0, ctx).  kv_len may be anything.
 LPQ_BOTH int keys_of(int kv_len, int max_pages, int page_shift)
