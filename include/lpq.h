@@ -402,8 +402,8 @@ lpq_status lpq_paged_load4(const void* k_pages, const void* v_pages, const lpq_a
 
 /* lpq_paged_attention over pages of cells, with the same arguments, masks and limits.  Where a sequence and K/V head have more than 32 rows, values of cells are rounded to
  * the type (as lpq_paged_load4 gives them) before they are multiplied; with fewer they are not rounded.  A position that is stored as NaN makes the rows that see it NaN.
- * Partial results are kept in the library's workspace, up to 324 MiB of them, split less under a smaller reservation as there: tiles of chunks and prompts first, then, below
- * 34 MiB (68 with 17 to 32 rows of a sequence and K/V head), decoding sequences too.
+ * Partial results are kept in the library's workspace, up to 290 MiB of them, split less under a smaller reservation as there: tiles of chunks and prompts first, then, below
+ * 34 MiB, decoding sequences too.
  * Errors: as lpq_paged_attention. */
 lpq_status lpq_paged_attention4(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* k_pages, const void* v_pages,
                                 const float* alibi_slopes, const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M,

@@ -1,6 +1,7 @@
 // What the attention operators for batches of sequences of different lengths share: rows, pages and work of a sequence, the list of the streaming kernels' units
 // and the kernel that adds up their parts, and the tile kernel with its combining kernel.
 #pragma once
+#include <algorithm>
 #include <mutex>
 #include <type_traits>
 
@@ -49,6 +50,7 @@ struct AttnArgs {
     const float* slopes;
     uint16_t* out;                       // [M][heads * D]
     float* part;                         // partial results, or null: nothing is split
+    uint32_t group_reciprocal;           // 2^32 / group, at most 2^32 - 1
     int32_t n_seqs, M, heads, kv_heads, group, shift, n_pages, max_pages;
     int32_t rows_from, rows_to;          // sequences with rows_from <= rows < rows_to are this launch's
     int32_t workers;                     // streaming kernel: waves
@@ -248,10 +250,10 @@ __device__ __forceinline__ Share find_share(const AttnArgs& a, int block, int ti
 // Adds up the parts of the row tiles that the entries of `cuts` name, 16 entries a workgroup; blockIdx.y: rows and, if LONG, slices of 32 features.  Many
 // short lists of parts: a wave takes a row of a cut, D / 4 lanes of four features each for every (256 / D)-th part.  LONG, for few lists of hundreds of parts:
 // the workgroup takes a slice, 8 lanes for every 32nd part, the sums added through LDS.  Either is right for any list.
-template <int DT, int D, int NT, bool LONG>
+template <int DT, int D, int TILE_ROWS, bool LONG>
 __global__ __launch_bounds__(256) void stream_combine_kernel(AttnArgs a)
 {
-    constexpr int TILE_ROWS = STREAM_ROWS * NT, SLOT = TILE_ROWS * (D + 2), SLICES = LONG ? D / 32 : 1, LANES = D / SLICES / 4, WAYS = (LONG ? 256 : 64) / LANES;
+    constexpr int SLOT = TILE_ROWS * (D + 2), SLICES = LONG ? D / 32 : 1, LANES = D / SLICES / 4, WAYS = (LONG ? 256 : 64) / LANES;
     __shared__ __attribute__((aligned(16))) float red[4][36];                    // LONG only: a wave's sums
     const Cut* cuts = reinterpret_cast<const Cut*>(a.part + (size_t)2 * a.workers * SLOT);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = LONG ? (int)threadIdx.x : lane;
@@ -844,7 +846,7 @@ static hipError_t allow_lds(size_t bytes)
 template <typename Family, int DT, int D>
 hipError_t launch_attention(const AttentionPlan& p, const AttnArgs& a, float* part, hipStream_t s)
 {
-    const bool alibi = a.slopes != nullptr, both = p.stream_tiles && p.tile, mixed = both && p.stream_tiles == 1;
+    const bool alibi = a.slopes != nullptr, both = p.stream_tile && p.tile, mixed = both && p.stream_tile <= STREAM_ROWS;
     const unsigned streams = (unsigned)p.workers / 4;
     AttnArgs st = a, tl = a;
     st.rows_from = 1;
@@ -860,40 +862,34 @@ hipError_t launch_attention(const AttentionPlan& p, const AttnArgs& a, float* pa
     const int classes = a.kv_heads % 8 == 0 ? 1 : a.kv_heads % 4 == 0 ? 2 : a.kv_heads % 2 == 0 ? 4 : 8;
     const unsigned grid = (unsigned)(a.kv_heads * classes) * (unsigned)((p.tiles + classes - 1) / classes) * (unsigned)p.splits;
     constexpr size_t smem = tile_lds(D, Family::CELLS);
-    // KERNEL<.., true or false>
-#define LPQ_ALIBI(KERNEL, GRID, SMEM, ...)                                                                              \
-    do {                                                                                                                \
-        if (alibi) KERNEL(true)<<<GRID, 256, SMEM, s>>>(__VA_ARGS__);                                                   \
-        else       KERNEL(false)<<<GRID, 256, SMEM, s>>>(__VA_ARGS__);                                                  \
-    } while (0)
-#define LPQ_MIXED(A) Family::template mixed<DT, D, A>
-#define LPQ_STREAM1(A) Family::template stream<DT, D, 1, A>
-#define LPQ_STREAM2(A) Family::template stream<DT, D, 2, A>
-#define LPQ_TILE_PAGED(A) Family::template tile<DT, D, A>
-#define LPQ_TILE_PACKED(A) Family::template tile_rows<DT, D, A>
-#define LPQ_ALLOW(KERNEL) (alibi ? allow_lds<KERNEL(true)>(smem) : allow_lds<KERNEL(false)>(smem))
-    const hipError_t allowed = !p.tile ? hipSuccess : mixed ? LPQ_ALLOW(LPQ_MIXED) : a.kp ? LPQ_ALLOW(LPQ_TILE_PAGED) : LPQ_ALLOW(LPQ_TILE_PACKED);
+    // with biases or without
+    auto launch = [&](auto plain, auto biased, unsigned blocks, size_t lds, const auto&... args) {
+        if (alibi) biased<<<blocks, 256, lds, s>>>(args...);
+        else plain<<<blocks, 256, lds, s>>>(args...);
+    };
+    const hipError_t allowed = !p.tile ? hipSuccess : alibi ? Family::template allow<DT, D, true>(mixed, p.stream_tile, a.kp != nullptr, smem)
+                                                            : Family::template allow<DT, D, false>(mixed, p.stream_tile, a.kp != nullptr, smem);
     if (allowed != hipSuccess) return allowed;
-    if (mixed) LPQ_ALIBI(LPQ_MIXED, streams + grid, smem, st, tl);
-    else {
-        if (p.stream_tiles == 1) LPQ_ALIBI(LPQ_STREAM1, streams, 0, st);
-        else if (p.stream_tiles == 2) LPQ_ALIBI(LPQ_STREAM2, streams, 0, st);
-        if (p.tile && a.kp) LPQ_ALIBI(LPQ_TILE_PAGED, grid, smem, tl);
-        else if (p.tile) LPQ_ALIBI(LPQ_TILE_PACKED, grid, smem, tl);
-    }
-#undef LPQ_ALIBI
-#undef LPQ_MIXED
-#undef LPQ_STREAM1
-#undef LPQ_STREAM2
-#undef LPQ_TILE_PAGED
-#undef LPQ_TILE_PACKED
-#undef LPQ_ALLOW
-    if (st.part && p.stream_tiles) {
-        const unsigned cuts = (unsigned)((p.workers + CUTS_PER_WG - 1) / CUTS_PER_WG), rows = (unsigned)p.stream_rows;
-        if (p.stream_tiles == 1 && p.long_lists) stream_combine_kernel<DT, D, 1, true><<<dim3(cuts, rows * (D / 32)), 256, 0, s>>>(st);
-        else if (p.stream_tiles == 1) stream_combine_kernel<DT, D, 1, false><<<dim3(cuts, rows), 256, 0, s>>>(st);
-        else if (p.long_lists) stream_combine_kernel<DT, D, 2, true><<<dim3(cuts, rows * (D / 32)), 256, 0, s>>>(st);
-        else stream_combine_kernel<DT, D, 2, false><<<dim3(cuts, rows), 256, 0, s>>>(st);
+    auto streaming = [&](auto rows) {                  // what is launched with a streaming kernel whose tiles have this many rows
+        constexpr int ROWS = decltype(rows)::value;
+        if constexpr (Family::template has<ROWS>) {
+            if constexpr (Family::template has_mixed<ROWS>)
+                if (mixed) launch(Family::template mixed<DT, D, ROWS, false>, Family::template mixed<DT, D, ROWS, true>, streams + grid, smem, st, tl);
+            if (!mixed) launch(Family::template stream<DT, D, ROWS, false>, Family::template stream<DT, D, ROWS, true>, streams, 0, st);
+            if (!st.part) return;
+            const unsigned per = Family::cuts_per_wg(p.long_lists), cuts = ((unsigned)p.workers + per - 1) / per, n = (unsigned)p.stream_rows;
+            if (p.long_lists) Family::template combine<DT, D, ROWS, true><<<Family::CELLS ? dim3(n * (D / 32), cuts) : dim3(cuts, n * (D / 32)), 256, 0, s>>>(st);
+            else Family::template combine<DT, D, ROWS, false><<<dim3(cuts, n), 256, 0, s>>>(st);
+        }
+    };
+    if (p.tile && !mixed && a.kp) launch(Family::template tile<DT, D, false>, Family::template tile<DT, D, true>, grid, smem, tl);
+    if constexpr (Family::ROWS)
+        if (p.tile && !a.kp) launch(Family::template tile_rows<DT, D, false>, Family::template tile_rows<DT, D, true>, grid, smem, tl);
+    switch (p.stream_tile) {
+    case 4: streaming(std::integral_constant<int, 4>()); break;
+    case 8: streaming(std::integral_constant<int, 8>()); break;
+    case 16: streaming(std::integral_constant<int, 16>()); break;
+    case 32: streaming(std::integral_constant<int, 32>()); break;
     }
     if (p.tile && p.splits > 1) tile_combine_kernel<DT, D><<<dim3((unsigned)(p.tiles * a.kv_heads), TILE_ROWS_Q * D / 1024), 256, 0, s>>>(tl);
     return hipGetLastError();
@@ -916,6 +912,7 @@ hipError_t launch_attention_of(const AttentionPlan& p, const lpq_attn_cfg& c, co
     a.heads = c.n_heads;
     a.kv_heads = c.n_kv_heads;
     a.group = c.n_heads / c.n_kv_heads;
+    a.group_reciprocal = (uint32_t)std::min<uint64_t>(UINT32_MAX, ((uint64_t)1 << 32) / (uint32_t)a.group);
     a.shift = b.shift;
     a.n_pages = b.n_pages;
     a.max_pages = b.max_pages;

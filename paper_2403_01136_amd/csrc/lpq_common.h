@@ -213,7 +213,7 @@ hipError_t launch_paged_append(const void* qkv, const lpq_attn_cfg& c, int shift
 // Where attention finds keys and values: the packed rows themselves, pages of 16-bit elements, pages of 4-bit cells.
 enum AttentionSource { SRC_ROWS, SRC_PAGES, SRC_CELLS };
 struct AttentionPlan {
-    int stream_tiles, stream_rows, workers;      // streaming kernel: column tiles of 16 rows (0: not launched), rows that a tile is expected to have, waves
+    int stream_tile, stream_rows, workers;       // streaming kernel: rows of a tile (0: not launched), rows that a tile is expected to have, waves
     bool long_lists;                     // few row tiles, cut into many parts each
     bool tile;                           // tile kernel launched
     int tiles, splits, least, key_tiles; // its virtual row tiles, K splits at most and key tiles of one at least; key tiles to expect

@@ -83,7 +83,7 @@ __device__ __forceinline__ void stream_block(const AttnArgs& a, int block, Share
         const Seq q = load_seq(a, s);
         const int steps = stream_key_steps(q.ctx), tiles = stream_row_tiles(q.rows, TILE_ROWS);
         const int64_t at = u - s_begin, tile = at >> 31 ? at / steps : (int64_t)((uint32_t)at / (uint32_t)steps), first = s_begin + tile * steps;
-        const int h = tiles == 1 ? (int)tile : (int)(tile / tiles), rt = tiles == 1 ? 0 : (int)(tile % tiles);
+        const int h = tiles == 1 ? (int)tile : (int)((uint32_t)tile / (uint32_t)tiles), rt = tiles == 1 ? 0 : (int)((uint32_t)tile % (uint32_t)tiles);
         if (!a.part && first < u) {                    // nowhere to leave parts: a worker takes the row tiles that begin in its share, whole
             u = first + steps;
             continue;
@@ -348,11 +348,14 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int 
     const bool paged = source != SRC_ROWS;
     const int group = c.n_heads / c.n_kv_heads;
     const int64_t most = (int64_t)std::min(max_q, M) * group;
-    p.stream_tiles = 0;
-    if (paged && most <= 2 * STREAM_ROWS) p.stream_tiles = most <= STREAM_ROWS ? 1 : 2;
-    else if (paged && n_seqs > 1 && group <= 2 * STREAM_ROWS) p.stream_tiles = group <= STREAM_ROWS ? 1 : 2;
+    // rows of the streaming kernel's tiles: those to expect where it is alone, else those of a decoding sequence; from 4 on for cells
+    auto tile_of_rows = [&](int64_t rows, int smallest) { return rows <= 4 && smallest <= 4 ? 4 : rows <= 8 && smallest <= 8 ? 8 : rows <= STREAM_ROWS ? STREAM_ROWS : 2 * STREAM_ROWS; };
+    const int smallest = source == SRC_CELLS ? 4 : STREAM_ROWS;
+    p.stream_tile = 0;
+    if (paged && most <= 2 * STREAM_ROWS) p.stream_tile = tile_of_rows(most, smallest);
+    else if (paged && n_seqs > 1 && group <= 2 * STREAM_ROWS) p.stream_tile = tile_of_rows(group, std::max(smallest, 8));
     p.tile = !(paged && most <= 2 * STREAM_ROWS);
-    p.workers = 4 * cus * (source == SRC_CELLS && p.stream_tiles == 1 && !p.tile ? CELL_WAVES : STREAM_WAVES);
+    p.workers = 4 * cus * (source == SRC_CELLS && p.stream_tile <= STREAM_ROWS && !p.tile ? CELL_WAVES : STREAM_WAVES);
     p.tiles = (int)tile_bound(M, group, n_seqs, TILE_ROWS_Q);
     p.splits = 1;
     if (p.tile) {
@@ -368,10 +371,10 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int 
         p.key_tiles = (int)key_tiles;
     }
     const size_t d2 = (size_t)c.head_dim + 2;
-    if (p.stream_tiles) p.stream_floats = (size_t)p.workers * (2 * STREAM_ROWS * p.stream_tiles * d2 + sizeof(Cut) / sizeof(float));
+    if (p.stream_tile) p.stream_floats = (size_t)p.workers * (2 * p.stream_tile * d2 + sizeof(Cut) / sizeof(float));
     // lists of 32 parts and more, where the walks are long enough to be cut that often (4 sequences of up to 800 positions: long lists' form 7.2 us, the other's 4.0)
     p.long_lists = (int64_t)n_seqs * c.n_kv_heads * 32 <= p.workers && max_kv >= 64 * STREAM_KEYS;
-    p.stream_rows = (int)std::min<int64_t>(STREAM_ROWS * p.stream_tiles, p.tile ? 2 * STREAM_ROWS : most);
+    p.stream_rows = (int)std::min<int64_t>(p.stream_tile, p.tile ? 2 * STREAM_ROWS : most);
     p.split_floats = (size_t)p.tiles * c.n_kv_heads * TILE_ROWS_Q * d2;
     return attention_plan_within(p, SIZE_MAX);
 }
@@ -389,11 +392,20 @@ AttentionPlan attention_plan_within(AttentionPlan p, size_t floats)
 }
 
 struct PageKernels {
-    static constexpr bool CELLS = false;
-    template <int DT, int D, bool ALIBI> static constexpr auto mixed = &mixed_attention_kernel<DT, D, ALIBI>;
-    template <int DT, int D, int NT, bool ALIBI> static constexpr auto stream = &stream_attention_kernel<DT, D, NT, ALIBI>;
+    static constexpr bool CELLS = false, ROWS = true;
+    template <int TILE> static constexpr bool has = TILE == STREAM_ROWS || TILE == 2 * STREAM_ROWS;
+    template <int TILE> static constexpr bool has_mixed = TILE == STREAM_ROWS;
+    template <int DT, int D, int TILE, bool ALIBI> static constexpr auto mixed = &mixed_attention_kernel<DT, D, ALIBI>;
+    template <int DT, int D, int TILE, bool ALIBI> static constexpr auto stream = &stream_attention_kernel<DT, D, TILE / STREAM_ROWS, ALIBI>;
+    template <int DT, int D, int TILE, bool LONG> static constexpr auto combine = &stream_combine_kernel<DT, D, TILE, LONG>;
+    static constexpr unsigned cuts_per_wg(bool) { return CUTS_PER_WG; }
     template <int DT, int D, bool ALIBI> static constexpr auto tile = &tile_attention_kernel<DT, D, ALIBI, SRC_PAGES>;
     template <int DT, int D, bool ALIBI> static constexpr auto tile_rows = &tile_attention_kernel<DT, D, ALIBI, SRC_ROWS>;
+    template <int DT, int D, bool ALIBI>
+    static hipError_t allow(bool mixed_launch, int, bool pages, size_t lds)
+    {
+        return mixed_launch ? allow_lds<mixed<DT, D, STREAM_ROWS, ALIBI>>(lds) : pages ? allow_lds<tile<DT, D, ALIBI>>(lds) : allow_lds<tile_rows<DT, D, ALIBI>>(lds);
+    }
 };
 
 hipError_t launch_batch_attention(const AttentionPlan& p, const lpq_attn_cfg& c, const AttentionBatch& b, float* part, hipStream_t s)

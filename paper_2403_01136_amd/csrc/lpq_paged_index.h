@@ -74,12 +74,17 @@ LPQ_BOTH KeySplit key_split(int tiles, int splits, int least, int sp)
 // row tile (its rows are set to zero).
 LPQ_BOTH int stream_row_tiles(int rows, int tile_rows) { return (rows + tile_rows - 1) / tile_rows; }
 LPQ_BOTH int stream_key_steps(int ctx) { return ctx > STREAM_KEYS ? (ctx + STREAM_KEYS - 1) / STREAM_KEYS : 1; }
-// Unit at which worker w of W begins, out of `units`.
-LPQ_BOTH int64_t stream_begin(int64_t units, int w, int W) { return units / W * w + units % W * w / W; }
+// Unit at which worker w of W begins, out of `units`: units * w / W.  (A 64-bit division is some 140 instructions one after the other, a 32-bit one 20.)
+LPQ_BOTH bool stream_small(int64_t units, int W) { return (uint64_t)units < (uint64_t)1 << 32 && (uint64_t)units * (uint32_t)W < (uint64_t)1 << 32; }
+LPQ_BOTH int64_t stream_begin(int64_t units, int w, int W)
+{
+    return stream_small(units, W) ? (int64_t)((uint32_t)units * (uint32_t)w / (uint32_t)W) : units / W * w + units % W * w / W;
+}
 // The worker that has unit u.
 LPQ_BOTH int stream_worker(int64_t units, int64_t u, int W)
 {
-    int w = (int)(u * W / units);            // begin(w) <= u * ... : at most one off either way
+    // begin(w) <= u * ... : at most one off either way
+    int w = stream_small(units, W) ? (int)((uint32_t)u * (uint32_t)W / (uint32_t)units) : (int)(u * W / units);
     while (w > 0 && stream_begin(units, w, W) > u) --w;
     while (w + 1 < W && stream_begin(units, w + 1, W) <= u) ++w;
     return w;

@@ -12,7 +12,7 @@ Up to 32 rows of a sequence and K/V head (codes are multiplied):
   * the matrix units keep a sum of eight products of codes, which are subnormal numbers in steps of 2^-20, to 2^-38 of the largest other factor: to
     2^-18 of a step.  In the score 2^-18 s sum |q_i|, in the result 2^-18 sum w_j s'_j
   * weights times scales are rounded to fp16, the codes' distance from 8 is what they multiply:   u16 sum w_j s'_j |c'_j - 8|, and 8 n 2^-39 max w_j s'_j for those
-    below its normal range beside a largest of 2^14 or more.
+    below its normal range beside a largest of 2^8 or more.
 More rows (values of cells in fp16, of a tile, or of K so far, with its largest between 2^14 and 2^15 in bf16):
   * K and V are rounded: the score by u16 sum |q_i k_i| (and 2^-39 of the largest |k| of a tile times sum |q_i|), the result by u16 A + 2^-39 max |v|
   * weights are rounded, in the products and in the sum that divides them:                u16 (A + |out|), and n 2^-25 max |v|."""
@@ -302,7 +302,7 @@ def attention_ref(q, cells, ok, pos, slopes, tile, dt):
         if tile:
             e = e + U16 * A + 2.0**-39 * vh.abs().amax() + (2.0**-25 if dt == "fp16" else 0.0) + U16 * (A + fin(o).abs()) + n * 2.0**-25 * vh.abs().amax()
         else:
-            e = e + (2.0**-18 * (w @ sv) + 8 * n * 2.0**-39 * (w * sv[None, :]).amax(1))[:, None] + U16 * (w @ (sv[:, None] * (cv - 8).abs()))
+            e = e + (2.0**-18 * (w @ sv) + 8 * n * 2.0**-33 * (w * sv[None, :]).amax(1))[:, None] + U16 * (w @ (sv[:, None] * (cv - 8).abs()))
         E[:, h] = e
     return out, E
 
