@@ -359,8 +359,8 @@ lpq_status lpq_packed_attention(const void *qkv, const lpq_attn_cfg *cfg, const 
  *   16 * head_dim / 2 bytes   codes of the positions in order, eight features to a little-endian u32: code e at bit 4 * (e / 2) + 16 * (e % 2)
  *   16 * 4 bytes              scale and zero of the positions, 16-bit numbers of the rows' type
  * and a code c stands for scale * c + zero.  Of x, the head_dim values of a head (the quantiser of lpq_quantize_pack, fp32 IEEE arithmetic, round-half-even):
- *   scale = type((max - min) / 15), 1 if that is zero, a last place less if 15 * scale + zero would round to infinity;   zero = min (+0 for -0);
- *   code = clamp(rint((x - zero) / scale), 0, 15)
+ *   scale = type((max - min) / 15), a last place less if 15 * scale + zero would round to infinity;   zero = min (+0 for -0);
+ *   code = clamp(rint((x - zero) / scale), 0, 15), 0 where scale is 0
  * A head with an infinity or NaN in it, or with max - min beyond the type's range, is stored as NaN throughout.
  * A layer's step is lpq_qk_norm_rotary (where the model has it), lpq_paged_append4, lpq_paged_attention4. */
 

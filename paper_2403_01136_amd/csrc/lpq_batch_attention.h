@@ -115,14 +115,22 @@ __device__ __forceinline__ const uint16_t* odd_value_row(const AttnArgs& a, cons
 // for each: scale, zero.
 template <int DT> __device__ __forceinline__ float param_scale(uint32_t p) { return (float)__builtin_bit_cast(typename Elem<DT>::t, (uint16_t)p); }
 template <int DT> __device__ __forceinline__ float param_zero(uint32_t p) { return (float)__builtin_bit_cast(typename Elem<DT>::t, (uint16_t)(p >> 16)); }
+__device__ __forceinline__ uint32_t and_or(uint32_t v, uint32_t mask, uint32_t bits)      // v & mask | bits, which the compiler makes two of
+{
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "s"(mask), "v"(bits));
+    return r;
+}
 // What a word of codes stands for, rounded once to the type.
 template <int DT> __device__ __forceinline__ u32x4 cell_values(uint32_t w, uint32_t param)
 {
     u32x4 x;
     if constexpr (DT == LPQ_DT_FP16) {                 // 1024 + code is an fp16 number with the code in its last bits
         const h2 p = as_h2(param), s = splat(p[0]), z = splat(p[1]), base = splat((_Float16)-1024.0f);
+        uint32_t bias = 0x64006400u;
+        asm("" : "+v"(bias));                          // in a register: of an instruction's operands one may be scalar
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = as_u32(pk_fma(as_h2((w >> (4 * e) & 0x000f000fu) | 0x64006400u) + base, s, z));
+        for (int e = 0; e < 4; ++e) x[e] = as_u32(pk_fma(as_h2(and_or(w >> (4 * e), 0x000f000fu, bias)) + base, s, z));
     } else {
         const float s = param_scale<DT>(param), z = param_zero<DT>(param);
         const uint32_t lo = w & 0x0f0f0f0fu, hi = w >> 4 & 0x0f0f0f0fu;          // bytes: features 0, 4, 1, 5 and 2, 6, 3, 7
@@ -135,25 +143,41 @@ template <int DT> __device__ __forceinline__ u32x4 cell_values(uint32_t w, uint3
     }
     return x;
 }
-// Numbers of either type as fp16 ones that a power of two is taken out of.  The exponent for a largest one of `top`: top 2^-exponent is 2^14 or more, below 2^15.
-__device__ __forceinline__ int exponent_to_14(float top)
+// The four pairs of a word's codes as fp16 numbers without exponent, code * 2^-20.
+__device__ __forceinline__ u32x4 code_pairs(uint32_t w)
 {
-    const int bits = (int)(__builtin_bit_cast(uint32_t, top) >> 23);
-    return bits == 0 || bits == 255 ? 0 : bits - 127 - 14;
+    constexpr uint32_t M = 0x00f000f0u;
+    return u32x4{w << 4 & M, w & M, w >> 4 & M, w >> 8 & M};
+}
+// Numbers of either type as fp16 ones that powers of two are taken out of.
+__device__ __forceinline__ int exponent_of(float v)
+{
+    const int bits = (int)(__builtin_bit_cast(uint32_t, v) >> 23);
+    return bits == 255 ? 0 : max(bits - 127, -100);
 }
 template <int DT> __device__ __forceinline__ float largest_of_pair(uint32_t pair, float top)
 {
     return fmaxf(top, fmaxf(__builtin_fabsf(param_scale<DT>(pair)), __builtin_fabsf(param_zero<DT>(pair))));
 }
-template <int DT> __device__ __forceinline__ uint32_t scaled_pair(uint32_t pair, int ex)
+template <int DT> __device__ __forceinline__ uint32_t scaled_pair(uint32_t pair, int ex0, int ex1)
 {
-    return Elem<LPQ_DT_FP16>::pack(__builtin_ldexpf(param_scale<DT>(pair), ex), __builtin_ldexpf(param_zero<DT>(pair), ex));
+    return Elem<LPQ_DT_FP16>::pack(__builtin_ldexpf(param_scale<DT>(pair), ex0), __builtin_ldexpf(param_zero<DT>(pair), ex1));
 }
-// The largest magnitude among a head's values.
-template <int DT> __device__ __forceinline__ float largest_value(uint32_t param)
+// A tile's values v are kept as v 2^-e in fp16, made from codes without exponent by scale * 2^(20 - e): e is the exponent of the largest of these numbers over its keys, which
+// leaves the scales below 2^16 and the zeros below 2^15.  As bits of a number >= 0; what is not finite does not count.
+template <int DT> __device__ __forceinline__ int cell_size(uint32_t param)
 {
-    const float z = param_zero<DT>(param);
-    return fmaxf(__builtin_fabsf(z), __builtin_fabsf(__builtin_fmaf(15.0f, param_scale<DT>(param), z)));
+    const int bits = __builtin_bit_cast(int, fmaxf(__builtin_fabsf(param_scale<DT>(param)) * 32.0f, __builtin_fabsf(param_zero<DT>(param)) * 0x1p-14f));
+    return not_finite<DT>(param) ? 0 : bits;
+}
+template <bool SCALED> __device__ __forceinline__ u32x4 tile_values(uint32_t w, uint32_t param)
+{
+    if constexpr (!SCALED) return cell_values<LPQ_DT_FP16>(w, param);
+    const h2 p = as_h2(param), s = splat(p[0]), z = splat(p[1]);
+    u32x4 x = code_pairs(w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = as_u32(pk_fma(as_h2(x[e]), s, z));
+    return x;
 }
 // Whether the values of key j of a sequence and K/V head are infinite or NaN (the same for the whole wave).
 template <int DT, int D>
@@ -316,7 +340,9 @@ __global__ __launch_bounds__(256) void stream_combine_kernel(AttnArgs a)
 // 16-byte chunks are swizzled: K's by the row (16 lanes read 16 rows), V's by the row modulo 4 in steps of four chunks (32 lanes read four rows x 64 bytes).
 // Workgroup ids go round-robin over the 8 XCDs; a head of keys, or a class of row tiles of it where there are fewer than eight, stays on one of them.
 template <int D> __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
-template <int D, int SRC> __device__ __forceinline__ int v_swizzle(int row) { return (SRC == SRC_CELLS ? 5 : 4) * (D == 128 ? row & 3 : (row >> 1) & 1); }
+template <int D> __device__ __forceinline__ int v_swizzle(int row) { return 4 * (D == 128 ? row & 3 : (row >> 1) & 1); }
+// Values of cells are stored by 16 lanes of 16 rows and the same chunk: V's swizzle goes by the other bits of the row too, K's as it does.
+template <int D> __device__ __forceinline__ int v_swizzle_cells(int row) { return v_swizzle<D>(row) + ((row >> 2) & 3); }
 
 // log2 of what a row's maximum may lag behind its largest score: sums are then at most 2^8 larger.  Renewed with every larger score there is hardly a
 // tile without 32 rows' sums being multiplied: one prompt of 5801 tokens 684 us, so 655; its error in bf16 1.9e-3, so 2.1e-3; in fp16 2.2e-4 and 2.3e-4.
@@ -411,8 +437,8 @@ template <int DT, int D, bool ALIBI, int SRC>
 __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 {
     // Products are of the rows' type; of cells in fp16 for either type, with tiles and queries of bf16 taken by powers of two.
-    constexpr int PT = SRC == SRC_CELLS ? (int)LPQ_DT_FP16 : DT;
     constexpr bool SCALED = SRC == SRC_CELLS && DT == LPQ_DT_BF16;
+    constexpr int PT = SRC == SRC_CELLS ? (int)LPQ_DT_FP16 : DT;
     typedef typename Elem<PT>::v8 V8;
     constexpr int CH = D / 8, KS = D / 16, DTL = D / 32, ROWS = 512 / D, FILLS = 16 / ROWS;       // chunks of a row; feature steps; feature tiles; keys per load; loads of a wave's 16 keys
     constexpr int TILE_BYTES = TILE_KEYS * D * 2;
@@ -448,8 +474,8 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         bad_ids = __ballot(ids < 0);
     };
     const uint32_t kl = (uint32_t)((lane / CH) * (PAGED ? D : cols) + 8 * ((lane % CH) ^ k_swizzle<D>(lane / CH))) * 2u;
-    const uint32_t vl = (uint32_t)((lane / CH) * (PAGED ? D : cols) + 8 * ((lane % CH) ^ v_swizzle<D, SRC>(lane / CH))) * 2u;
-    // cells: this wave's 16 keys of a tile as they lie, lane l has codes D / 4 (l % 4) .. of key l / 4, until place() puts their values in LDS
+    const uint32_t vl = (uint32_t)((lane / CH) * (PAGED ? D : cols) + 8 * ((lane % CH) ^ v_swizzle<D>(lane / CH))) * 2u;
+    // cells: this wave's 16 keys of a tile as they lie, lane l has codes D / 4 (l / 16) .. of key l % 16, until place() puts their values in LDS
     typedef uint32_t codes_t __attribute__((ext_vector_type(D / 32)));
     codes_t kcodes = {}, vcodes = {};
     uint32_t kparam = 0, vparam = 0;
@@ -459,10 +485,10 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         const int id = max(__builtin_amdgcn_readlane(ids, 4 * (j - ids_from) + wave), 0);
         const size_t at = (size_t)cell_group(id, h, a.kv_heads, a.shift, (4 * j + wave) & ((1 << (a.shift - 4)) - 1), D);
         const uint8_t *kb = reinterpret_cast<const uint8_t*>(a.kp) + at, *vb = reinterpret_cast<const uint8_t*>(a.vp) + at;
-        kcodes = *reinterpret_cast<const codes_t*>(kb + lane * (D / 8));
-        kparam = *reinterpret_cast<const uint32_t*>(kb + 8 * D + (lane & ~3));
-        vcodes = *reinterpret_cast<const codes_t*>(vb + lane * (D / 8));
-        vparam = *reinterpret_cast<const uint32_t*>(vb + 8 * D + (lane & ~3));
+        kcodes = *reinterpret_cast<const codes_t*>(kb + (lane & 15) * (D / 2) + (lane >> 4) * (D / 8));
+        kparam = *reinterpret_cast<const uint32_t*>(kb + 8 * D + 4 * (lane & 15));
+        vcodes = *reinterpret_cast<const codes_t*>(vb + (lane & 15) * (D / 2) + (lane >> 4) * (D / 8));
+        vparam = *reinterpret_cast<const uint32_t*>(vb + 8 * D + 4 * (lane & 15));
         return (uint32_t)(bad_ids >> (4 * (j - ids_from))) & 15u;
     };
     // asks for tile j; which of its 16-key groups have no page
@@ -499,7 +525,7 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
                     const int row = ROWS * i + lane / CH;
                     const uint8_t* kb = base + (size_t)min(k0 + row, q.len - 1) * cols * 2;
                     __builtin_amdgcn_global_load_lds((gptr_t)(kb + 16 * ((lane % CH) ^ k_swizzle<D>(row))), (lptr_t)(ks_ + 1024 * i), 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((gptr_t)(kb + a.kv_heads * D * 2 + 16 * ((lane % CH) ^ v_swizzle<D, SRC>(row))), (lptr_t)(vs_ + 1024 * i), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kb + a.kv_heads * D * 2 + 16 * ((lane % CH) ^ v_swizzle<D>(row))), (lptr_t)(vs_ + 1024 * i), 16, 0, 0);
                 }
             }
         }
@@ -519,10 +545,14 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 #pragma unroll
             for (int k = 0; k < 4 * KS; ++k) top = largest_of_pair<DT>(pairs[k], top);
             const f2 z = both_halves(top);
-            const int ex = exponent_to_14(fmaxf(z[0], z[1]));
+            const int ex = exponent_of(fmaxf(z[0], z[1])) - 14;
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
-                qf[k] = __builtin_bit_cast(V8, u32x4{scaled_pair<DT>(pairs[4 * k], -ex), scaled_pair<DT>(pairs[4 * k + 1], -ex), scaled_pair<DT>(pairs[4 * k + 2], -ex), scaled_pair<DT>(pairs[4 * k + 3], -ex)});
+            for (int k = 0; k < KS; ++k) {
+                u32x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = scaled_pair<DT>(pairs[4 * k + e], -ex, -ex);
+                qf[k] = __builtin_bit_cast(V8, x);
+            }
             c = __builtin_ldexpf(c, ex);
         }
     }
@@ -541,7 +571,7 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 #pragma unroll
     for (int d = 0; d < DTL; ++d) {
         const int row = 4 * half + (lane & 15) / 4, chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        va[d] = (uint32_t)(2 * TILE_BYTES + row * D * 2 + 16 * (chunk ^ v_swizzle<D, SRC>(row)) + 8 * (lane & 1));
+        va[d] = (uint32_t)(2 * TILE_BYTES + row * D * 2 + 16 * (chunk ^ (CELLS ? v_swizzle_cells<D>(row) : v_swizzle<D>(row))) + 8 * (lane & 1));
     }
 
     // keys from here on are not seen by every row of the tile; and whether a wave has set values of theirs to zero, in LDS behind the tiles
@@ -554,23 +584,30 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 #pragma unroll
         for (int i = 0; i < 16; ++i) near[i] = slope * (float)(8 * (i / 4) + i % 4);
 
-    // Cells: tile j's parameters have landed.  Keys that no row sees get none (values of zero, like their weights; K's scores are replaced); and, in bf16, the
-    // largest value of K and of V among the wave's keys for all waves.
+    // Cells: tile j's parameters have landed.  Keys that no row sees get none (values of zero, like their weights; K's scores are replaced); and, in
+    // bf16, the largest of K's and of V's among the wave's keys for all waves.
     int* const tops = reinterpret_cast<int*>(smem_raw + 4 * TILE_BYTES + 16);    // [n % 2][K, V][wave]
     auto look = [&](int j, int buf, uint32_t no_page) {
-        if ((no_page >> wave & 1) || TILE_KEYS * j + 16 * wave + lane / 4 >= tl.key_end) kparam = vparam = 0;
-        if constexpr (SCALED) {
-            const float kt = group_reduce<64>(largest_value<DT>(kparam), OpMax()), vt = group_reduce<64>(largest_value<DT>(vparam), OpMax());
-            if (lane == 0) {
-                tops[8 * buf + wave] = __builtin_bit_cast(int, kt);
-                tops[8 * buf + 4 + wave] = __builtin_bit_cast(int, vt);
-            }
+        if ((no_page >> wave & 1) || TILE_KEYS * j + 16 * wave + (lane & 15) >= tl.key_end) kparam = vparam = 0;
+        if constexpr (!SCALED) return;
+        int kt = cell_size<DT>(kparam), vt = cell_size<DT>(vparam);
+        auto step = [&](auto ctrl) {
+            kt = max(kt, __builtin_amdgcn_update_dpp(0, kt, decltype(ctrl)::value, 0xf, 0xf, true));
+            vt = max(vt, __builtin_amdgcn_update_dpp(0, vt, decltype(ctrl)::value, 0xf, 0xf, true));
+        };
+        step(std::integral_constant<int, 0xB1>());
+        step(std::integral_constant<int, 0x4E>());
+        step(std::integral_constant<int, 0x141>());
+        step(std::integral_constant<int, 0x140>());
+        if (lane == 0) {
+            tops[8 * buf + wave] = kt;
+            tops[8 * buf + 4 + wave] = vt;
         }
     };
     int k_ex = 0, v_ex = -200, k_ex_next = 0, v_ex_next = -200;                 // the tile's K is taken by 2^-k_ex, its V and the sums by 2^-v_ex
     // the values of the cells into LDS
     auto place = [&](int j, int buf) {
-        const int row = 16 * wave + lane / 4, key = TILE_KEYS * j + row;
+        const int row = 16 * wave + (lane & 15), key = TILE_KEYS * j + row;
         if (key >= first_hidden && __any(not_finite<DT>(vparam) != 0)) {         // not every row sees it: its values may not be infinite or NaN
             if (not_finite<DT>(vparam) != 0) vparam = 0;
             odd_values[wave] = 1;
@@ -578,18 +615,18 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         uint32_t kp = kparam, vp = vparam;
         if constexpr (SCALED) {
             typedef int i32x4 __attribute__((ext_vector_type(4)));
-            const i32x4 kt = *reinterpret_cast<const i32x4*>(tops + 8 * buf), vt = *reinterpret_cast<const i32x4*>(tops + 8 * buf + 4);      // bits of numbers >= 0 are ordered as they are
-            k_ex_next = exponent_to_14(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(max(max(kt[0], kt[1]), max(kt[2], kt[3])))));
-            v_ex_next = max(v_ex_next, exponent_to_14(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(max(max(vt[0], vt[1]), max(vt[2], vt[3]))))));
-            kp = scaled_pair<DT>(kp, -k_ex_next);
-            vp = scaled_pair<DT>(vp, -v_ex_next);
+            const i32x4 kt = *reinterpret_cast<const i32x4*>(tops + 8 * buf), vt = *reinterpret_cast<const i32x4*>(tops + 8 * buf + 4);
+            k_ex_next = exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(max(max(kt[0], kt[1]), max(kt[2], kt[3])))));
+            v_ex_next = max(v_ex_next, exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(max(max(vt[0], vt[1]), max(vt[2], vt[3]))))));
+            kp = scaled_pair<DT>(kparam, 20 - k_ex_next, -k_ex_next);
+            vp = scaled_pair<DT>(vparam, 20 - v_ex_next, -v_ex_next);
         }
         uint8_t *kr = smem_raw + buf * TILE_BYTES + row * D * 2, *vr = kr + 2 * TILE_BYTES;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
-            const int chunk = (D / 32) * (lane & 3) + i;
-            *reinterpret_cast<u32x4*>(kr + 16 * (chunk ^ k_swizzle<D>(row))) = cell_values<LPQ_DT_FP16>(kcodes[i], kp);
-            *reinterpret_cast<u32x4*>(vr + 16 * (chunk ^ v_swizzle<D, SRC>(row))) = cell_values<LPQ_DT_FP16>(vcodes[i], vp);
+            const int chunk = (D / 32) * (lane >> 4) + i;
+            *reinterpret_cast<u32x4*>(kr + 16 * (chunk ^ k_swizzle<D>(row))) = tile_values<SCALED>(kcodes[i], kp);
+            *reinterpret_cast<u32x4*>(vr + 16 * (chunk ^ v_swizzle_cells<D>(row))) = tile_values<SCALED>(vcodes[i], vp);
         }
     };
 
@@ -667,7 +704,8 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
             for (int i = 0; i < 8; ++i) {
                 const uint8_t* at = tile + va[d0 + i / 4] + 16 * (i % 4) * D * 2;
                 typedef __attribute__((address_space(3))) s16x4* tr_t;
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(at + 8 * D * 2));
+                const uint8_t* at8 = CELLS ? tile + (va[d0 + i / 4] ^ 32u) + 16 * (i % 4) * D * 2 : at;          // eight rows on: another swizzle
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(at8 + 8 * D * 2));
                 x[i] = __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };

@@ -131,8 +131,8 @@ template <int D> __device__ __forceinline__ Cell cell_of(const CellArgs& a)
 }
 
 // Codes and parameters of a head of which this lane has eight features:
-//     scale = type((max - min) / 15), 1 if that is zero, a last place less if 15 scales above zero would round to infinity;  zero = min;
-//     code = clamp(rint((x - zero) / scale), 0, 15)
+//     scale = type((max - min) / 15), a last place less if 15 scales above zero would round to infinity;  zero = min;
+//     code = clamp(rint((x - zero) / scale), 0, 15), 0 where scale is
 // with quotients rounded to fp32.  The division is done where a product with the reciprocal (off by less than 2^-18 below 16) is within 2^-13 of a half.
 // A head with an infinity or a NaN in it, or a range beyond the type's, is NaN throughout.
 template <int DT, int LANES>
@@ -157,8 +157,7 @@ __device__ __forceinline__ uint32_t quantise_head(const u32x4& x, uint32_t* para
     const uint16_t zb = __builtin_bit_cast(uint16_t, zero);
     const float z = (float)zero;
     const bool odd = probe != probe || !__builtin_isfinite((float)scale);
-    if (sb == 0) sb = __builtin_bit_cast(uint16_t, (T)1.0f);
-    else if (!odd && __builtin_isinf((float)(T)__builtin_fmaf(15.0f, (float)scale, z))) --sb;
+    if (!odd && __builtin_isinf((float)(T)__builtin_fmaf(15.0f, (float)scale, z))) --sb;
     const float s = (float)__builtin_bit_cast(T, sb);
     const bool fast = s >= 0x1p-100f && s <= 0x1p100f;
     float rcp = __builtin_amdgcn_rcpf(s);
@@ -173,7 +172,7 @@ __device__ __forceinline__ uint32_t quantise_head(const u32x4& x, uint32_t* para
     }
     constexpr uint32_t NOT_A_NUMBER = DT == LPQ_DT_FP16 ? 0x7e007e00u : 0x7fc07fc0u;
     *param = odd ? NOT_A_NUMBER : (uint32_t)sb | (uint32_t)zb << 16;
-    return odd ? 0u : word;
+    return odd || sb == 0 ? 0u : word;
 }
 
 template <int DT, int D>

@@ -29,13 +29,6 @@ namespace {
 // Both m and G are renewed only where t G passes 2^15: one maximum a step decides (P may be up to 2^60).
 constexpr float LARGEST_T = 0x1p15f, NEW_T = 0x1p8f, RENEW_T = 0x1p60f;
 
-// The four pairs of a word's codes as fp16 numbers, code * 2^-20.
-__device__ __forceinline__ u32x4 code_pairs(uint32_t w)
-{
-    constexpr uint32_t M = 0x00f000f0u;
-    return u32x4{w << 4 & M, w & M, w >> 4 & M, w >> 8 & M};
-}
-
 // v <- op(v, v of the lanes that have the same row): the four quarters, and where a tile has 8 or 4 rows the columns that are 8 or 4 apart.
 template <int ROWS, typename Op>
 __device__ __forceinline__ float over_row(float v, Op op)
@@ -263,14 +256,14 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     for (int e = 0; e < 4; ++e) top = largest_of_pair<DT>(qw[t][j][e], top);
                 f2 z = both_rows(top);
                 z = both_halves(fmaxf(z[0], z[1]));
-                ex = exponent_to_14(fmaxf(z[0], z[1]));
+                ex = exponent_of(fmaxf(z[0], z[1])) - 14;
             }
             float sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < W; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if constexpr (DT == LPQ_DT_BF16) qw[t][j][e] = scaled_pair<DT>(qw[t][j][e], -ex);
+                    if constexpr (DT == LPQ_DT_BF16) qw[t][j][e] = scaled_pair<DT>(qw[t][j][e], -ex, -ex);
                     sum = Elem<LPQ_DT_FP16>::add_pair(qw[t][j][e], sum);
                 }
             f2 z = both_rows(sum);

@@ -13,8 +13,9 @@ Up to 32 rows of a sequence and K/V head (codes are multiplied):
     2^-18 of a step.  In the score 2^-18 s sum |q_i|, in the result 2^-18 sum w_j s'_j
   * weights times scales are rounded to fp16, the codes' distance from 8 is what they multiply:   u16 sum w_j s'_j |c'_j - 8|, and 8 n 2^-39 max w_j s'_j for those
     below its normal range beside a largest of 2^8 or more.
-More rows (values of cells in fp16, of a tile, or of K so far, with its largest between 2^14 and 2^15 in bf16):
-  * K and V are rounded: the score by u16 sum |q_i k_i| (and 2^-39 of the largest |k| of a tile times sum |q_i|), the result by u16 A + 2^-39 max |v|
+More rows (values v are v 2^-e in fp16, with the largest of 32 s and 2^-14 |z| of a tile's keys, for V of all so far, between 2^e and 2^(e + 1); steps of at least 2^-24,
+half of which is 2^-24 of the largest of 15 s and |z|, or less):
+  * K and V are rounded: the score by u16 sum |q_i k_i| and 2^-24 max (15 s, |z|) sum |q_i|, the result by u16 A + 2^-24 max (15 s', |z'|)
   * weights are rounded, in the products and in the sum that divides them:                u16 (A + |out|), and n 2^-25 max |v|."""
 import math
 import random
@@ -64,8 +65,8 @@ def quantise(x, dt):
             return np.zeros(len(x), np.uint8), nan, nan
         zero = f(lo + f(0))
         if scale == 0:
-            scale = to_bits(f(1), dt)
-        elif np.isinf(of_bits(to_bits(f(15) * of_bits(scale, dt) + zero, dt), dt)):
+            return np.zeros(len(x), np.uint8), 0, int(to_bits(zero, dt))
+        if np.isinf(of_bits(to_bits(f(15) * of_bits(scale, dt) + zero, dt), dt)):
             scale = scale - 1
         s = f(of_bits(scale, dt))
         codes = np.clip(np.rint((x - zero).astype(f) / s), 0, 15).astype(np.uint8)
@@ -281,7 +282,7 @@ def attention_ref(q, cells, ok, pos, slopes, tile, dt):
         size = qh.abs().sum(1, keepdim=True) / math.sqrt(d)                      # sum |q_i|
         err = (d + 8) * 2.0**-24 * size * (15 * sk + zk.abs())[None, :]
         if tile:
-            err = err + U16 * (qh.abs() @ kh.abs().t().contiguous()) / math.sqrt(d) + 2.0**-39 * size * kh.abs().amax() + 2.0**-25 * size * (dt == "fp16")
+            err = err + U16 * (qh.abs() @ kh.abs().t().contiguous()) / math.sqrt(d) + 2.0**-24 * size * torch.maximum(15 * sk, zk.abs()).amax()
         else:
             err = err + 2.0**-18 * size * sk[None, :]
         if slopes is not None:
@@ -300,7 +301,7 @@ def attention_ref(q, cells, ok, pos, slopes, tile, dt):
         arg = err * lg + 3 * 2.0**-24 * (fin(s).abs() + fin(top).abs()) * lg
         e = 2 * (math.log(2) * torch.where(vis, arg, none).amax(1, keepdim=True) + 2.0**-22) * A + 2 * n * 2.0**-24 * (w @ (15 * sv + zv.abs()))[:, None]
         if tile:
-            e = e + U16 * A + 2.0**-39 * vh.abs().amax() + (2.0**-25 if dt == "fp16" else 0.0) + U16 * (A + fin(o).abs()) + n * 2.0**-25 * vh.abs().amax()
+            e = e + U16 * A + 2.0**-24 * torch.maximum(15 * sv, zv.abs()).amax() + U16 * (A + fin(o).abs()) + n * 2.0**-25 * vh.abs().amax()
         else:
             e = e + (2.0**-18 * (w @ sv) + 8 * n * 2.0**-33 * (w * sv[None, :]).amax(1))[:, None] + U16 * (w @ (sv[:, None] * (cv - 8).abs()))
         E[:, h] = e
