@@ -7,6 +7,7 @@ There is no CPU fallback: if the library is missing, loading raises.
 """
 import collections
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -364,7 +365,7 @@ def _device_of(t):
     """Index of the current CUDA device, where the kernels run and t has to be."""
     import torch
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != torch._C._cuda_getDevice():   # a CUDA tensor: the runtime is up
         raise ValueError("tensors must be on the current CUDA device")
     return dev
 
@@ -372,6 +373,13 @@ def _device_of(t):
 def _check_tensor(name, t, dtype, dims, dev):
     if t.dtype is not dtype or t.dim() != dims or t.get_device() != dev or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %d-D %s tensor on CUDA device %d" % (name, dims, dtype, dev))
+
+
+def _vector(name, t, dtype, size, dev):
+    """Address of a contiguous vector of `size` elements."""
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != size or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on CUDA device %d" % (name, dtype, size, dev))
+    return t.data_ptr()
 
 
 def _stream_on(stream, dev):
@@ -399,10 +407,15 @@ def _attn_cfg(qkv, n_heads, n_kv_heads):
     import torch
     if qkv.dtype is not torch.float16 and qkv.dtype is not torch.bfloat16:
         raise ValueError("qkv must be fp16 or bf16")
-    cols, heads = qkv.shape[1], n_heads + 2 * n_kv_heads
+    return _attn_cfg_of(qkv.shape[1], n_heads, n_kv_heads, LPQ_DT_FP16 if qkv.dtype is torch.float16 else LPQ_DT_BF16)
+
+
+@functools.lru_cache(maxsize=256)
+def _attn_cfg_of(cols, n_heads, n_kv_heads, dtype):
+    heads = n_heads + 2 * n_kv_heads
     if n_heads < 1 or n_kv_heads < 1 or cols % heads:
         raise ValueError("qkv has %d columns, not a multiple of %d heads" % (cols, heads))
-    return lpq_attn_cfg(n_heads, n_kv_heads, cols // heads, LPQ_DT_FP16 if qkv.dtype is torch.float16 else LPQ_DT_BF16)
+    return lpq_attn_cfg(n_heads, n_kv_heads, cols // heads, dtype)
 
 
 def _paged_cfg(qkv, k_pages, v_pages):
@@ -550,58 +563,51 @@ def lpq_qk_norm_rotary(qkv, positions, n_heads, n_kv_heads, cos_sin=None, interl
     halves) of the q and k heads of qkv ([M][(heads + 2 kv heads) * d]) at int32 positions [M].  Rows with a negative entry in slots are left as they are in out.
     out: qkv itself (None: in place) or another tensor like it, which gets V too.  -> out."""
     import torch
-    dev = _device_of(qkv)
-    _check_tensor("qkv", qkv, qkv.dtype, 2, dev)
+    i32, dtype, dev = torch.int32, qkv.dtype, _device_of(qkv)
+    _check_tensor("qkv", qkv, dtype, 2, dev)
     cfg, M = _attn_cfg(qkv, n_heads, n_kv_heads), qkv.shape[0]
-    rows = [(name, t) for name, t in (("positions", positions), ("slots", slots)) if t is not None]
-    for name, t in rows:
-        _check_tensor(name, t, torch.int32, 1, dev)
-        if t.shape[0] != M:
-            raise ValueError("%s must have a value per row" % name)
-    for name, t in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
-        if t is not None:
-            _check_tensor(name, t, qkv.dtype, 1, dev)
-            if t.shape[0] != cfg.head_dim:
-                raise ValueError("%s must have a value per feature of a head" % name)
+    at = left = q_norm = k_norm = table = None
     rotary_dim = max_pos = 0
+    if positions is not None:
+        at = _vector("positions", positions, i32, M, dev)
+    if slots is not None:
+        left = _vector("slots", slots, i32, M, dev)
+    if q_gamma is not None:
+        q_norm = _vector("q_gamma", q_gamma, dtype, cfg.head_dim, dev)
+    if k_gamma is not None:
+        k_norm = _vector("k_gamma", k_gamma, dtype, cfg.head_dim, dev)
     if cos_sin is not None:
         _check_tensor("cos_sin", cos_sin, torch.float32, 2, dev)
         max_pos, rotary_dim = cos_sin.shape
+        table = cos_sin.data_ptr()
     if out is None:
         out = qkv
     elif out is not qkv:
-        _check_tensor("out", out, qkv.dtype, 2, dev)
+        _check_tensor("out", out, dtype, 2, dev)
         if out.shape != qkv.shape:
             raise ValueError("out must have qkv's shape")
-    ptr = lambda t: None if t is None else t.data_ptr()
-    r = lpq_rotary(rotary_dim, LPQ_PAIRS_ADJACENT if interleaved else LPQ_PAIRS_HALVES, max_pos, eps, ptr(cos_sin), ptr(q_gamma), ptr(k_gamma))
-    _check(load_library().lpq_qk_norm_rotary(qkv.data_ptr(), cfg, r, ptr(positions), ptr(slots), M, out.data_ptr(), _stream_on(stream, dev)), "lpq_qk_norm_rotary")
+    r = lpq_rotary(rotary_dim, LPQ_PAIRS_ADJACENT if interleaved else LPQ_PAIRS_HALVES, max_pos, eps, table, q_norm, k_norm)
+    _check(load_library().lpq_qk_norm_rotary(qkv.data_ptr(), cfg, r, at, left, M, out.data_ptr(), _stream_on(stream, dev)), "lpq_qk_norm_rotary")
     return out
 
 
 def lpq_paged_append4(qkv, k_pages, v_pages, slots, stream=None):
     """K and V of the rows of qkv ([M][(heads + 2 kv heads) * d], fp16 or bf16), quantised, into their slots of pages of 4-bit cells."""
-    _cells_and_slots("lpq_paged_append4", qkv, k_pages, v_pages, slots, stream)
+    import torch
+    dev, cfg, page_size, n_pages = _cells_cfg(qkv, k_pages, v_pages)
+    M = qkv.shape[0]
+    at, p = _vector("slots", slots, torch.int32, M, dev), lpq_page_pool(page_size, n_pages, 0, None, None, None)
+    _check(load_library().lpq_paged_append4(qkv.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), at, M, _stream_on(stream, dev)), "lpq_paged_append4")
 
 
 def lpq_paged_load4(k_pages, v_pages, slots, out, stream=None):
     """What the slots hold to the K and V parts of the rows of out ([M][(heads + 2 kv heads) * d], fp16 or bf16: the type that was appended).  -> out."""
-    _cells_and_slots("lpq_paged_load4", out, k_pages, v_pages, slots, stream)
-    return out
-
-
-def _cells_and_slots(name, rows, k_pages, v_pages, slots, stream):
     import torch
-    dev, cfg, page_size, n_pages = _cells_cfg(rows, k_pages, v_pages)
-    _check_tensor("slots", slots, torch.int32, 1, dev)
-    M = rows.shape[0]
-    if slots.shape[0] != M:
-        raise ValueError("slots must have a value per row")
-    p, L, on = lpq_page_pool(page_size, n_pages, 0, None, None, None), load_library(), _stream_on(stream, dev)
-    if name == "lpq_paged_append4":
-        _check(L.lpq_paged_append4(rows.data_ptr(), cfg, p, k_pages.data_ptr(), v_pages.data_ptr(), slots.data_ptr(), M, on), name)
-    else:
-        _check(L.lpq_paged_load4(k_pages.data_ptr(), v_pages.data_ptr(), cfg, p, slots.data_ptr(), M, rows.data_ptr(), on), name)
+    dev, cfg, page_size, n_pages = _cells_cfg(out, k_pages, v_pages)
+    M = out.shape[0]
+    at, p = _vector("slots", slots, torch.int32, M, dev), lpq_page_pool(page_size, n_pages, 0, None, None, None)
+    _check(load_library().lpq_paged_load4(k_pages.data_ptr(), v_pages.data_ptr(), cfg, p, at, M, out.data_ptr(), _stream_on(stream, dev)), "lpq_paged_load4")
+    return out
 
 
 def lpq_paged_attention4(qkv, k_pages, v_pages, table, cu_q, kv_lens, max_q=None, max_kv=None, alibi_slopes=None, out=None, stream=None):

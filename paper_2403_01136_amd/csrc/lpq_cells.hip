@@ -38,168 +38,172 @@ template <int DT> __device__ __forceinline__ u32x4 from_floats(const float* v)
     return x;
 }
 
-template <int DT, int D, bool ADJACENT, int HEADS>
+// Bound by the memory: rows in and out, 16 bytes a load.  A wave has 8 heads (D = 128) of a row once: 4168 rows of 120 heads, every byte of them, 47.4 us (5.4 TB/s), with two
+// such turns a wave, sharing the angles, 51.9, with four 50.0; 43 rows of 72 heads 3.3, 3.8, 4.9.
+template <int DT, int D, bool ADJACENT>
 __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(RotaryArgs a)
 {
-    constexpr int LANES = D / 16, SLOTS = 64 / LANES;  // lanes of a head; heads of a wave at a time, HEADS times
+    constexpr int LANES = D / 16, SLOTS = 64 / LANES;  // lanes of a head; heads of a wave
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64));
-    const int row = wave / a.groups, group = wave % a.groups;
+    const int row = wave / a.groups, h = wave % a.groups * SLOTS + lane / LANES;
     if (row >= a.M || (a.slots && a.slots[row] < 0)) return;
     const int p = a.turned ? a.positions[row] : 0;
     if (a.turned && (uint32_t)p >= (uint32_t)a.max_pos) return;
+    if (h >= a.heads) return;                          // all lanes of a head
     const int li = lane % LANES, half = a.turned / 16;                           // chunks of half a turned part
-    const bool turn = li < half;
-    const int c0 = ADJACENT ? 2 * li : turn ? li : 2 * half + 2 * (li - half), c1 = ADJACENT || !turn ? c0 + 1 : li + half;
-    f4 cs[2], sn[2];                                                             // angles 8 li .. 8 li + 7
-    if (turn) {
-        const f4* t = reinterpret_cast<const f4*>(a.table + (size_t)p * a.turned + 8 * li);
-        cs[0] = t[0], cs[1] = t[1];
-        t = reinterpret_cast<const f4*>(a.table + (size_t)p * a.turned + a.turned / 2 + 8 * li);
-        sn[0] = t[0], sn[1] = t[1];
-    }
-    const size_t base = (size_t)row * ((a.H + 2 * a.KV) * D);
-    u32x4 x[HEADS][2];
+    const bool turn = li < half && h < a.H + a.KV;
+    const int c0 = ADJACENT ? 2 * li : li < half ? li : 2 * half + 2 * (li - half), c1 = ADJACENT || li >= half ? c0 + 1 : li + half;
+    const size_t at = ((size_t)row * (a.H + 2 * a.KV) + h) * D;
+    u32x4 x0 = *reinterpret_cast<const u32x4*>(a.in + at + 8 * c0), x1 = *reinterpret_cast<const u32x4*>(a.in + at + 8 * c1);
+    if (h < a.H + a.KV) {
+        float v[16];
+        to_floats<DT>(x0, v);
+        to_floats<DT>(x1, v + 8);
+        const uint16_t* gamma = h < a.H ? a.q_gamma : a.k_gamma;
+        if (gamma) {
+            float ss = 0.0f, g[16];
+            to_floats<DT>(*reinterpret_cast<const u32x4*>(gamma + 8 * c0), g);
+            to_floats<DT>(*reinterpret_cast<const u32x4*>(gamma + 8 * c1), g + 8);
 #pragma unroll
-    for (int n = 0; n < HEADS; ++n) {
-        const int h = (group * HEADS + n) * SLOTS + lane / LANES;
-        if (h >= a.heads) continue;
-        x[n][0] = *reinterpret_cast<const u32x4*>(a.in + base + h * D + 8 * c0);
-        x[n][1] = *reinterpret_cast<const u32x4*>(a.in + base + h * D + 8 * c1);
-    }
+            for (int e = 0; e < 16; ++e) ss = __builtin_fmaf(v[e], v[e], ss);
+            ss = group_reduce<LANES>(ss, OpAdd());
+            const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
 #pragma unroll
-    for (int n = 0; n < HEADS; ++n) {
-        const int h = (group * HEADS + n) * SLOTS + lane / LANES;
-        const uint16_t* gamma = h < a.H ? a.q_gamma : h < a.H + a.KV ? a.k_gamma : nullptr;
-        if (h < a.H + a.KV) {
-            float v[16];
-            to_floats<DT>(x[n][0], v);
-            to_floats<DT>(x[n][1], v + 8);
-            if (gamma) {
-                float ss = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) ss = __builtin_fmaf(v[e], v[e], ss);
-                ss = group_reduce<LANES>(ss, OpAdd());
-                const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-                float g[16];
-                to_floats<DT>(*reinterpret_cast<const u32x4*>(gamma + 8 * c0), g);
-                to_floats<DT>(*reinterpret_cast<const u32x4*>(gamma + 8 * c1), g + 8);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = v[e] * r * g[e];
-            }
-            if (turn)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float c = cs[i / 4][i % 4], s = sn[i / 4][i % 4];
-                    float &va = v[ADJACENT ? 2 * i : i], &vb = v[ADJACENT ? 2 * i + 1 : 8 + i];
-                    const float ra = va * c - vb * s, rb = vb * c + va * s;
-                    va = ra;
-                    vb = rb;
-                }
-            x[n][0] = from_floats<DT>(v);
-            x[n][1] = from_floats<DT>(v + 8);
+            for (int e = 0; e < 16; ++e) v[e] = v[e] * r * g[e];
         }
-        if (h >= a.heads) continue;
-        *reinterpret_cast<u32x4*>(a.out + base + h * D + 8 * c0) = x[n][0];
-        *reinterpret_cast<u32x4*>(a.out + base + h * D + 8 * c1) = x[n][1];
+        if (turn) {
+            const f4 *t = reinterpret_cast<const f4*>(a.table + (size_t)p * a.turned + 8 * li), *u = reinterpret_cast<const f4*>(a.table + (size_t)p * a.turned + a.turned / 2 + 8 * li);
+            const f4 cs[2] = {t[0], t[1]}, sn[2] = {u[0], u[1]};                 // angles 8 li .. 8 li + 7
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float c = cs[i / 4][i % 4], s = sn[i / 4][i % 4];
+                float &va = v[ADJACENT ? 2 * i : i], &vb = v[ADJACENT ? 2 * i + 1 : 8 + i];
+                const float ra = va * c - vb * s, rb = vb * c + va * s;
+                va = ra;
+                vb = rb;
+            }
+        }
+        x0 = from_floats<DT>(v);
+        x1 = from_floats<DT>(v + 8);
     }
+    *reinterpret_cast<u32x4*>(a.out + at + 8 * c0) = x0;
+    *reinterpret_cast<u32x4*>(a.out + at + 8 * c1) = x1;
 }
 
 // ---- cells ------------------------------------------------------------------------------------------
-// A thread has eight features of a row's K head and of the V head, LANES neighbours the whole heads.
+// A thread has eight features of a row's K head and of the V head (the append: 16), neighbours the whole heads.
 struct CellArgs {
     uint16_t* qkv;
     uint8_t *kp, *vp;
     const int32_t* slots;
     int M, H, KV, shift, n_pages;
 };
-struct Cell { bool any; uint16_t* row; size_t group; int at, chunk; };           // K's eight features in the row; the 16-position group and the place in it
-template <int D> __device__ __forceinline__ Cell cell_of(const CellArgs& a)
+struct Cell { uint16_t* row; int head, chunk, slot; };                           // K's features in the row, null behind the last one; slot as the caller gave it
+// TOGETHER rows of one head are neighbours, then come the other heads, then the next rows.
+template <int D, int FEATURES, int TOGETHER> __device__ __forceinline__ Cell cell_of(const CellArgs& a)
 {
-    constexpr int LANES = D / 8;
-    const int per_row = a.KV * LANES;
-    const uint32_t i = blockIdx.x * 256u + threadIdx.x, row = i / (uint32_t)per_row;      // below 2^31: the host's bound on M
-    Cell c{};
-    if (row >= (uint32_t)a.M) return c;
-    const int n = (int)(i - row * (uint32_t)per_row), h = n / LANES, slot = slot_checked(a.slots[row], a.n_pages, a.shift);
-    if (slot < 0) return c;
-    c.any = true;
-    c.chunk = n % LANES;
-    c.row = a.qkv + (size_t)row * ((a.H + 2 * a.KV) * D) + (a.H + h) * D + 8 * c.chunk;
-    c.at = slot & 15;
-    c.group = (size_t)cell_group(slot >> a.shift, h, a.KV, a.shift, (slot & ((1 << a.shift) - 1)) >> 4, D);
-    return c;
+    constexpr int LANES = D / FEATURES;
+    const uint32_t i = (blockIdx.x * 256u + threadIdx.x) / LANES, rows = i / ((uint32_t)a.KV * TOGETHER) * TOGETHER, n = i - rows * (uint32_t)a.KV;      // below 2^31: the host's bound on M
+    const uint32_t h = n / TOGETHER, row = rows + n % TOGETHER, chunk = threadIdx.x % LANES;
+    if (row >= (uint32_t)a.M) return Cell{};
+    return Cell{a.qkv + (size_t)row * ((a.H + 2 * a.KV) * D) + (a.H + h) * D + FEATURES * chunk, (int)h, (int)chunk, a.slots[row]};
+}
+// Where the cell's group of 16 positions begins; its slot is one.
+template <int D> __device__ __forceinline__ size_t group_of(const CellArgs& a, const Cell& c)
+{
+    return (size_t)cell_group(c.slot >> a.shift, c.head, a.KV, a.shift, (c.slot & ((1 << a.shift) - 1)) >> 4, D);
 }
 
-// Codes and parameters of a head of which this lane has eight features:
+// Codes and parameters of a head of which this lane has 16 features:
 //     scale = type((max - min) / 15), a last place less if 15 scales above zero would round to infinity;  zero = min;
 //     code = clamp(rint((x - zero) / scale), 0, 15), 0 where scale is
-// with quotients rounded to fp32.  The division is done where a product with the reciprocal (off by less than 2^-18 below 16) is within 2^-13 of a half.
+// with quotients rounded to fp32.  No division: a product with the reciprocal, refined once, gives f = floor(quotient), or one off next to a whole number, and the sign of
+// d = (x - zero) - (f + 1/2) scale, exact in one FMA as f + 1/2 has five bits and a scale eleven, says which side of the half the quotient is on (one off, d says so as well); d = 0 is
+// the tie, frequent where x has eight bits.  Only a quotient that is not a tie but rounds to one needs more: |d| <= 2^-20 scale, then the wave divides.
 // A head with an infinity or a NaN in it, or a range beyond the type's, is NaN throughout.
 template <int DT, int LANES>
-__device__ __forceinline__ uint32_t quantise_head(const u32x4& x, uint32_t* param)
+__device__ __forceinline__ u32x2 quantise_head(const u32x4 (&x)[2], uint32_t* param)
 {
     typedef typename Elem<DT>::t T;
-    float v[8], lo, hi, probe = 0.0f;
-    to_floats<DT>(x, v);
+    constexpr int N = 16;
+    float v[N], lo, hi, probe = 0.0f;
+    to_floats<DT>(x[0], v);
+    to_floats<DT>(x[1], v + 8);
     lo = hi = v[0];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 1; e < N; ++e) {
         lo = fminf(lo, v[e]);
         hi = fmaxf(hi, v[e]);
-        probe = __builtin_fmaf(v[e], 0.0f, probe);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) probe = Elem<DT>::probe_pair(x[e / 4][e % 4], probe);
     struct OpMin { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
     lo = group_reduce<LANES>(lo, OpMin());
     hi = group_reduce<LANES>(hi, OpMax());
-    probe = group_reduce<LANES>(probe, OpAdd());
     const T scale = (T)__fdiv_rn(__fsub_rn(hi, lo), 15.0f), zero = (T)__fadd_rn(lo, 0.0f);      // lo is a number of the type; -0 becomes 0
     uint16_t sb = __builtin_bit_cast(uint16_t, scale);
     const uint16_t zb = __builtin_bit_cast(uint16_t, zero);
     const float z = (float)zero;
-    const bool odd = probe != probe || !__builtin_isfinite((float)scale);
+    const uint64_t bad_lanes = __ballot(probe != probe);
+    const bool odd = (bad_lanes >> (threadIdx.x & 63 & -LANES) & ((1ull << LANES) - 1)) != 0 || !__builtin_isfinite((float)scale);
     if (!odd && __builtin_isinf((float)(T)__builtin_fmaf(15.0f, (float)scale, z))) --sb;
     const float s = (float)__builtin_bit_cast(T, sb);
-    const bool fast = s >= 0x1p-100f && s <= 0x1p100f;
-    float rcp = __builtin_amdgcn_rcpf(s);
+    float rcp = __builtin_amdgcn_rcpf(s), r[N];
     rcp = __builtin_fmaf(__builtin_fmaf(-s, rcp, 1.0f), rcp, rcp);
-    uint32_t word = 0;
+    const float per_unit = rcp * 0x1p20f;
+    uint32_t least = 0xffffffffu;                      // of |d|, where it is not zero: its bits doubled, less two
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float num = __fsub_rn(v[e], z);
-        float t = __fmul_rn(num, rcp), r = __builtin_rintf(t);
-        if (!fast || __builtin_fabsf(__builtin_fabsf(t - r) - 0.5f) < 0x1p-13f) r = __builtin_rintf(__fdiv_rn(num, s));
-        word |= (uint32_t)fminf(fmaxf(r, 0.0f), 15.0f) << (4 * (e / 2) + 16 * (e % 2));
+    for (int e = 0; e < N; ++e) {
+        const float num = __fsub_rn(v[e], z), b = __builtin_floorf(__fmul_rn(num, rcp)) + 0.5f, d = __builtin_fmaf(-b, s, num);
+        least = min(least, 2u * __builtin_bit_cast(uint32_t, d) - 2u);
+        r[e] = __builtin_rintf(b + __builtin_amdgcn_fmed3f(d * per_unit, -0.25f, 0.25f));
     }
+    if (__any(least <= 2u * __builtin_bit_cast(uint32_t, s * 0x1p-20f) || !(s >= 0x1p-100f && s <= 0x1p100f)))
+#pragma unroll
+        for (int e = 0; e < N; ++e) r[e] = __builtin_rintf(__fdiv_rn(__fsub_rn(v[e], z), s));
+#pragma unroll
+    for (int e = 0; e < N; ++e) r[e] = __builtin_amdgcn_fmed3f(r[e], 0.0f, 15.0f);
+    // code e at bit 4 (e / 2) of its half: sums below 2^16, exact
+    auto half = [&](int e) { return (uint32_t)__builtin_fmaf(r[e + 6], 4096.0f, __builtin_fmaf(r[e + 4], 256.0f, __builtin_fmaf(r[e + 2], 16.0f, r[e]))); };
     constexpr uint32_t NOT_A_NUMBER = DT == LPQ_DT_FP16 ? 0x7e007e00u : 0x7fc07fc0u;
     *param = odd ? NOT_A_NUMBER : (uint32_t)sb | (uint32_t)zb << 16;
-    return odd || sb == 0 ? 0u : word;
+    return odd || sb == 0 ? u32x2{0, 0} : u32x2{half(0) | half(1) << 16, half(8) | half(9) << 16};
 }
 
+// Bound by the memory, of which its reads are most (256 bytes of a row and head at D = 128); what it writes lies in the order of positions, so 16 rows of a head are neighbours here:
+// a group's codes and parameters are whole lines of one XCD's L2.  7246 rows of 8 heads: row by row, eight features a thread and IEEE divisions near halves, 14.4 us; 16 features, no divisions 12.8; so 12.6.
+constexpr int APPEND_TOGETHER = 16;
 template <int DT, int D>
 __global__ __launch_bounds__(256) void paged_append4_kernel(CellArgs a)
 {
-    const Cell c = cell_of<D>(a);
-    if (!c.any) return;                                // all lanes of a head or none
-    const u32x4 k = *reinterpret_cast<const u32x4*>(c.row), v = *reinterpret_cast<const u32x4*>(c.row + a.KV * D);
+    const Cell c = cell_of<D, 16, APPEND_TOGETHER>(a);
+    if (!c.row) return;                                // all lanes of a head or none, here as below
+    const u32x4 *kr = reinterpret_cast<const u32x4*>(c.row), *vr = reinterpret_cast<const u32x4*>(c.row + a.KV * D);
+    const u32x4 k[2] = {kr[0], kr[1]}, v[2] = {vr[0], vr[1]};
+    if (slot_checked(c.slot, a.n_pages, a.shift) < 0) return;
     uint32_t kparam, vparam;
-    const uint32_t kw = quantise_head<DT, D / 8>(k, &kparam), vw = quantise_head<DT, D / 8>(v, &vparam);
-    uint8_t *kg = a.kp + c.group, *vg = a.vp + c.group;
-    *reinterpret_cast<uint32_t*>(kg + c.at * (D / 2) + 4 * c.chunk) = kw;
-    *reinterpret_cast<uint32_t*>(vg + c.at * (D / 2) + 4 * c.chunk) = vw;
+    const u32x2 kw = quantise_head<DT, D / 16>(k, &kparam), vw = quantise_head<DT, D / 16>(v, &vparam);
+    const size_t group = group_of<D>(a, c);
+    uint8_t *kg = a.kp + group, *vg = a.vp + group;
+    const int at = c.slot & 15;
+    *reinterpret_cast<u32x2*>(kg + at * (D / 2) + 8 * c.chunk) = kw;
+    *reinterpret_cast<u32x2*>(vg + at * (D / 2) + 8 * c.chunk) = vw;
     if (c.chunk == 0) {
-        *reinterpret_cast<uint32_t*>(kg + 8 * D + 4 * c.at) = kparam;
-        *reinterpret_cast<uint32_t*>(vg + 8 * D + 4 * c.at) = vparam;
+        *reinterpret_cast<uint32_t*>(kg + 8 * D + 4 * at) = kparam;
+        *reinterpret_cast<uint32_t*>(vg + 8 * D + 4 * at) = vparam;
     }
 }
 
 template <int DT, int D>
 __global__ __launch_bounds__(256) void paged_load4_kernel(CellArgs a)
 {
-    const Cell c = cell_of<D>(a);
-    if (!c.any) return;
-    const uint8_t *kg = a.kp + c.group, *vg = a.vp + c.group;
-    const uint32_t kw = *reinterpret_cast<const uint32_t*>(kg + c.at * (D / 2) + 4 * c.chunk), vw = *reinterpret_cast<const uint32_t*>(vg + c.at * (D / 2) + 4 * c.chunk);
-    const uint32_t kparam = *reinterpret_cast<const uint32_t*>(kg + 8 * D + 4 * c.at), vparam = *reinterpret_cast<const uint32_t*>(vg + 8 * D + 4 * c.at);
+    const Cell c = cell_of<D, 8, 1>(a);
+    if (!c.row || slot_checked(c.slot, a.n_pages, a.shift) < 0) return;
+    const size_t group = group_of<D>(a, c);
+    const uint8_t *kg = a.kp + group, *vg = a.vp + group;
+    const int at = c.slot & 15;
+    const uint32_t kw = *reinterpret_cast<const uint32_t*>(kg + at * (D / 2) + 4 * c.chunk), vw = *reinterpret_cast<const uint32_t*>(vg + at * (D / 2) + 4 * c.chunk);
+    const uint32_t kparam = *reinterpret_cast<const uint32_t*>(kg + 8 * D + 4 * at), vparam = *reinterpret_cast<const uint32_t*>(vg + 8 * D + 4 * at);
     *reinterpret_cast<u32x4*>(c.row) = cell_values<DT>(kw, kparam);
     *reinterpret_cast<u32x4*>(c.row + a.KV * D) = cell_values<DT>(vw, vparam);
 }
@@ -207,18 +211,19 @@ __global__ __launch_bounds__(256) void paged_load4_kernel(CellArgs a)
 template <int DT, int D>
 hipError_t launch_rotary(RotaryArgs a, bool adjacent, hipStream_t s)
 {
-    constexpr int SLOTS = 64 / (D / 16), HEADS = 2;
-    a.groups = (a.heads + SLOTS * HEADS - 1) / (SLOTS * HEADS);
+    constexpr int SLOTS = 64 / (D / 16);
+    a.groups = (a.heads + SLOTS - 1) / SLOTS;
     const unsigned grid = (unsigned)(((int64_t)a.M * a.groups + 3) / 4);
-    if (adjacent) qk_norm_rotary_kernel<DT, D, true, HEADS><<<grid, 256, 0, s>>>(a);
-    else          qk_norm_rotary_kernel<DT, D, false, HEADS><<<grid, 256, 0, s>>>(a);
+    if (adjacent) qk_norm_rotary_kernel<DT, D, true><<<grid, 256, 0, s>>>(a);
+    else          qk_norm_rotary_kernel<DT, D, false><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <bool APPEND, int DT, int D>
 hipError_t launch_cells_of(const CellArgs& a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)(((int64_t)a.M * a.KV * (D / 8) + 255) / 256);
+    const int64_t rows = APPEND ? ((int64_t)a.M + APPEND_TOGETHER - 1) / APPEND_TOGETHER * APPEND_TOGETHER : a.M;
+    const unsigned grid = (unsigned)((rows * a.KV * (D / (APPEND ? 16 : 8)) + 255) / 256);
     if constexpr (APPEND) paged_append4_kernel<DT, D><<<grid, 256, 0, s>>>(a);
     else                  paged_load4_kernel<DT, D><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
