@@ -437,6 +437,8 @@ template <int DT, int D, bool ALIBI, int SRC>
 __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 {
     // Products are of the rows' type; of cells in fp16 for either type, with tiles and queries of bf16 taken by powers of two.
+    // Rounded K puts 2.5e-4 of a result of ordinary scores into it, V 2.0e-4, beside an output's rounding of 2.1e-4 (fp16) and 1.6e-3 (bf16).  (K as codes, with scale and zero behind
+    // the products, was exact and 12 % slower: two chunks of up to 512 tokens beside 9 sequences that decode, 56 heads over 8, biases, 134.6 us for 120.7.)
     constexpr bool SCALED = SRC == SRC_CELLS && DT == LPQ_DT_BF16;
     constexpr int PT = SRC == SRC_CELLS ? (int)LPQ_DT_FP16 : DT;
     typedef typename Elem<PT>::v8 V8;

@@ -44,7 +44,7 @@ template <int DT, int D, bool ADJACENT>
 __global__ __launch_bounds__(256) void qk_norm_rotary_kernel(RotaryArgs a)
 {
     constexpr int LANES = D / 16, SLOTS = 64 / LANES;  // lanes of a head; heads of a wave
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)((blockIdx.y * gridDim.x + blockIdx.x) * 4 + threadIdx.x / 64));
     const int row = wave / a.groups, h = wave % a.groups * SLOTS + lane / LANES;
     if (row >= a.M || (a.slots && a.slots[row] < 0)) return;
     const int p = a.turned ? a.positions[row] : 0;
@@ -213,7 +213,9 @@ hipError_t launch_rotary(RotaryArgs a, bool adjacent, hipStream_t s)
 {
     constexpr int SLOTS = 64 / (D / 16);
     a.groups = (a.heads + SLOTS - 1) / SLOTS;
-    const unsigned grid = (unsigned)(((int64_t)a.M * a.groups + 3) / 4);
+    // M heads are at most 2^27, so waves fit 32 bits; threads need not
+    const unsigned blocks = (unsigned)(((int64_t)a.M * a.groups + 3) / 4), across = std::min(blocks, 1u << 23);
+    const dim3 grid(across, (blocks + across - 1) / across);
     if (adjacent) qk_norm_rotary_kernel<DT, D, true><<<grid, 256, 0, s>>>(a);
     else          qk_norm_rotary_kernel<DT, D, false><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();

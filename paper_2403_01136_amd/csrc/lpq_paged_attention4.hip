@@ -27,7 +27,7 @@ namespace {
 //                    eight; halves of two keys' words are put side by side, and an AND gives a pair of keys of one feature.
 // Weights: P = exp2(score - m), its sum and its sum with the zeros in fp32; t = P s' is taken by a power of two G for each column so that the largest so far is below 2^15.
 // Both m and G are renewed only where t G passes 2^15: one maximum a step decides (P may be up to 2^60).
-constexpr float LARGEST_T = 0x1p15f, NEW_T = 0x1p8f, RENEW_T = 0x1p60f;
+constexpr float LARGEST_T = 0x1p15f, NEW_T = 0x1p12f, RENEW_T = 0x1p60f;
 
 // v <- op(v, v of the lanes that have the same row): the four quarters, and where a tile has 8 or 4 rows the columns that are 8 or 4 apart.
 template <int ROWS, typename Op>

@@ -12,7 +12,7 @@ Up to 32 rows of a sequence and K/V head (codes are multiplied):
   * the matrix units keep a sum of eight products of codes, which are subnormal numbers in steps of 2^-20, to 2^-38 of the largest other factor: to
     2^-18 of a step.  In the score 2^-18 s sum |q_i|, in the result 2^-18 sum w_j s'_j
   * weights times scales are rounded to fp16, the codes' distance from 8 is what they multiply:   u16 sum w_j s'_j |c'_j - 8|, and 8 n 2^-39 max w_j s'_j for those
-    below its normal range beside a largest of 2^8 or more.
+    below its normal range beside a largest of 2^12 or more.
 More rows (values v are v 2^-e in fp16, with the largest of 32 s and 2^-14 |z| of a tile's keys, for V of all so far, between 2^e and 2^(e + 1); steps of at least 2^-24,
 half of which is 2^-24 of the largest of 15 s and |z|, or less):
   * K and V are rounded: the score by u16 sum |q_i k_i| and 2^-24 max (15 s, |z|) sum |q_i|, the result by u16 A + 2^-24 max (15 s', |z'|)
@@ -303,7 +303,7 @@ def attention_ref(q, cells, ok, pos, slopes, tile, dt):
         if tile:
             e = e + U16 * A + 2.0**-24 * torch.maximum(15 * sv, zv.abs()).amax() + U16 * (A + fin(o).abs()) + n * 2.0**-25 * vh.abs().amax()
         else:
-            e = e + (2.0**-18 * (w @ sv) + 8 * n * 2.0**-33 * (w * sv[None, :]).amax(1))[:, None] + U16 * (w @ (sv[:, None] * (cv - 8).abs()))
+            e = e + (2.0**-18 * (w @ sv) + 8 * n * 2.0**-37 * (w * sv[None, :]).amax(1))[:, None] + U16 * (w @ (sv[:, None] * (cv - 8).abs()))
         E[:, h] = e
     return out, E
 
@@ -417,3 +417,434 @@ def test_decode(seqs, H, KV, d, P, pad, alibi, dt):
 def test_chunks_and_mixed(seqs, H, KV, d, P, pad, alibi, dt):
     """Chunks short and long, alone and beside sequences that decode: the streaming kernel's one and two column tiles, the tile kernel, its splits, and both."""
     check_attention(*Cells(seqs, H, KV, d, P, dt, pad).run(alibi, **longest(seqs)), what="chunks")
+
+
+@pytest.mark.parametrize("hints", [(1, 1), (10000, 10**6), (None, None), (5, 100)], ids=str)
+def test_hints_do_not_change_the_result(hints):
+    p = Cells([(300, 1), (400, 70), (0, 1), (90, 5)], 8, 2, 64, 32, "fp16", 3)
+    check_attention(*p.run(max_q=hints[0], max_kv=hints[1], loose=True), what=str(hints))
+
+
+@pytest.mark.parametrize("n", [64, 65, 257, 2048])
+def test_many_sequences(n):
+    r = random.Random(n)
+    seqs = [(r.choice((0, 1, 15, 16, 40, 200 if n < 2000 else 30)), r.choice((0, 1, 1, 1))) for _ in range(n)]
+    check_attention(*Cells(seqs, 4, 2, 64, 16, "fp16", 2).run(max_q=1), what="many")
+
+
+def test_mostly_idle_slots_and_some_long():
+    seqs = [(0, 0)] * 700 + [(3000, 1)] + [(0, 0)] * 600 + [(70, 1), (0, 0), (900, 40)]
+    check_attention(*Cells(seqs, 8, 2, 64, 64, "bf16", 1).run(max_q=40), what="idle")
+
+
+@pytest.mark.parametrize("H,KV,d,dt,alibi", [(8, 1, 128, "fp16", False), (8, 2, 64, "bf16", True), (40, 2, 64, "fp16", False), (3, 1, 128, "bf16", False), (12, 4, 64, "fp16", True)])
+def test_parts_of_both_kernels(H, KV, d, dt, alibi):
+    """Walks that many workers share beside short ones, and row tiles whose keys are split."""
+    check_attention(*Cells([(9000, 1), (3, 1), (5000, 2), (0, 1)], H, KV, d, 32, dt, 1).run(alibi, max_q=2), what="streams")
+    check_attention(*Cells([(6000, 50), (10, 1)], H, KV, d, 16, dt).run(alibi, max_q=50), what="tiles")
+
+
+def test_long_context():
+    """Many parts of one row tile, ids reloaded many times, small pages; long lists of parts."""
+    check_attention(*Cells([(40000, 1)], 4, 1, 128, 16, "fp16").run(max_q=1), what="long")
+    check_attention(*Cells([(90001, 1)], 7, 1, 64, 128, "fp16").run(max_q=1), what="longer")
+    check_attention(*Cells([(20011, 1), (5, 1), (9000, 1)], 6, 2, 64, 64, "bf16").run(True, max_q=1), what="long, ragged")
+    check_attention(*Cells([(9000, 20)], 8, 1, 128, 16, "fp16").run(max_q=20), what="long chunk")
+    check_attention(*Cells([(30000, 1)], 20, 1, 128, 32, "bf16").run(max_q=1), what="two column tiles")
+
+
+@pytest.mark.parametrize("q", [1, 3, 50])
+def test_rows_that_see_nothing(q):
+    """No keys, fewer keys than new tokens, tables without pages: zeros, and the other sequences as ever."""
+    p = Cells([(0, q), (20, q), (100, q), (0, q)], 4, 2, 64, 16, "fp16", 2)
+    p.table[0] = [-1] * len(p.table[0])
+    out, parts = p.run(max_q=q, kv_lens=[0, 20 + q, -3, max(q - 1, 0)])
+    check_attention(out, parts, what="nothing to see")
+    assert bool((out[:q] == 0).all()) and bool((out[2 * q:3 * q] == 0).all())
+
+
+@pytest.mark.parametrize("alibi", [False, True], ids=["plain", "alibi"])
+@pytest.mark.parametrize("q,P", [(1, 16), (1, 64), (3, 32), (60, 16), (150, 64)])
+def test_bad_pages_are_masked(q, P, alibi):
+    """Ids that are no pages of the pool, at the front, in the middle and at the end, and lengths beyond the table."""
+    p = Cells([(400, q), (333, q), (300, q)], 6, 2, 128, P, "fp16", 1, width_extra=0)
+    p.table[0][0] = -1
+    p.table[0][3] = p.n_pages
+    p.table[1][2] = -2**31
+    p.table[1][-2] = 2**31 - 1
+    p.table[2] = [-5] * len(p.table[2])
+    cap = len(p.table[0]) * P
+    check_attention(*p.run(alibi, max_q=q), what="bad pages")
+    check_attention(*p.run(alibi, max_q=q, kv_lens=[cap + 20, cap + 5, 10]), what="beyond the table")
+
+
+@pytest.mark.parametrize("q,H,KV", [(1, 8, 2), (1, 4, 4), (1, 20, 2), (4, 4, 2), (20, 4, 4), (100, 8, 2)])
+@pytest.mark.parametrize("d,dt", [(64, "fp16"), (128, "fp16"), (128, "bf16")])
+def test_stale_cells_do_not_matter(q, H, KV, d, dt):
+    """Scales and zeros that are NaN, infinite or huge in every position that no sequence has: behind the last one in its page, and in pages of nobody."""
+    import torch
+    p = Cells([(37, q), (250, q), (1030, q), (0, q)], H, KV, d, 64, dt)
+    want, _ = p.run(max_q=q)
+    used = torch.zeros((p.n_pages, 64), dtype=torch.bool, device="cuda")
+    for s, (past, n) in enumerate(p.seqs):
+        for j in range(past + n):
+            used[p.table[s][j // 64], j % 64] = True
+    mine = used[None, :, None, :, None]
+    for val in (math.nan, math.inf, -math.inf, 60000.0 if dt == "fp16" else 1e38):
+        p.param = torch.where(mine, p.param, torch.full_like(p.param, val))
+        p.write()
+        got, _ = p.run(max_q=q)
+        assert torch.equal(got, want), val
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("past,q,H,KV,d", [(70, 2, 8, 2, 64), (70, 4, 8, 2, 128), (70, 16, 4, 2, 64), (10, 40, 4, 4, 128), (200, 140, 8, 2, 64), (300, 1, 8, 2, 128)])
+def test_positions_stored_as_nan(past, q, H, KV, d, dt):
+    """What the append makes of a head with a NaN or an infinity: NaN for the rows that see it, K's or V's, and no others."""
+    import torch
+    r = random.Random(past + q)
+    for n, j in enumerate(sorted({past + q - 1, past + q // 2, past, r.randrange(past + q)})):
+        p = Cells([(past, q), (10, q), (33, 1)], H, KV, d, 16, dt, 1)
+        which, head = n % 2, r.randrange(KV)
+        p.param[which, p.table[0][j // 16], head, j % 16] = math.nan
+        p.codes[which, p.table[0][j // 16], head, j % 16] = 0
+        p.write()
+        out, parts = p.run(max_q=q)
+        check_attention(out, parts, what="NaN at %d" % j)
+        seen = torch.isnan(out[:q]).view(q, H, d).all(2)
+        rows, heads = torch.arange(past, past + q, device="cuda")[:, None] >= j, torch.arange(H, device="cuda")[None, :] // (H // KV) == head
+        assert torch.equal(seen, rows & heads)
+
+
+def test_nan_throughout():
+    import torch
+    for where in ("cells", "queries"):
+        p = Cells([(2000, 900), (700, 3), (50, 1)], 8, 2, 128, 64, "bf16")
+        if where == "queries":
+            p.qkv.fill_(math.nan)
+        else:
+            p.param.fill_(math.nan)
+            p.write()
+        out, _ = p.run(max_q=900, out=torch.zeros((p.M, 8 * 128), dtype=torch.bfloat16, device="cuda"))
+        assert bool(torch.isnan(out).all())
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("spread", [4.0, 9.0])
+def test_scales_of_many_sizes(spread, dt):
+    """Neighbouring positions whose scales are powers of two apart, up to 2^18: weights times scales, and tiles, go by the largest."""
+    for seqs, max_q in (([(700, 1), (90, 1)], 1), ([(2000, 3)], 3), ([(500, 60)], 60), ([(300, 200), (1000, 1)], 200)):
+        p = Cells(seqs, 8, 2, 128, 32, dt, spread=spread)
+        p.qkv[:, :8 * 128] *= 2.0**-spread
+        check_attention(*p.run(max_q=max_q), what="spread")
+
+
+@pytest.mark.parametrize("k_size,v_size", [(1e-6, 1e-9), (1e9, 1e12), (1.0, 1e-30), (1e-20, 1e30)])
+def test_cells_of_any_size_in_bf16(k_size, v_size):
+    """Keys and values far from one, with queries that bring the scores back: bf16 has an exponent for them."""
+    for seqs, max_q in (([(700, 1), (90, 1)], 1), ([(500, 6)], 6), ([(500, 60), (100, 1)], 60)):
+        p = Cells(seqs, 8, 2, 64, 32, "bf16")
+        p.qkv[:, :8 * 64] /= k_size
+        p.param[0] *= k_size
+        p.param[1] *= v_size
+        p.write()
+        out, parts = p.run(max_q=max_q)
+        p.check = [((r0, r1), (o / v_size, e / v_size)) for (r0, r1), (o, e) in parts]
+        for (r0, r1), (o, e) in p.check:
+            far = ((out[r0:r1].double().view(o.shape) / v_size - o).abs() / (2.0**-8 * (o.abs() + e) + e + 2.0**-30)).max()
+            assert float(far) <= 1.0, (seqs, float(far))
+
+
+def test_large_scores():
+    """Scores in the thousands: one key takes all; and all scores equal."""
+    p = Cells([(500, 1), (300, 30)], 4, 2, 128, 32, "fp16")
+    p.qkv *= 20
+    check_attention(*p.run(max_q=30), what="large")
+    p.codes[0], p.param[0] = 0, 0.0
+    p.write()
+    check_attention(*p.run(max_q=30), what="equal")
+
+
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_beyond_24_bits(d, dt, biases):
+    """Scores so large that neighbours in 32 bits are tens or hundreds apart, each of them exact: the visible keys with the largest share the weight equally, the
+    others have none.  Off by the output's rounding, values' (u16) or weights' times scales (u16 of 7 steps), and 2^-20 for 32-bit sums and the division."""
+    import torch
+    u, r = {"fp16": 2.0**-11, "bf16": 2.0**-8}[dt], random.Random(d)
+    seqs, H, KV = [(300, 1), (0, 300), (70, 90), (500, 6), (0, 1), (64, 17)], 4, 2
+    for max_q, step in ((300, 2048.0), (300, 4.0), (6, 2048.0)):
+        p = Cells([(a, min(b, max_q)) for a, b in seqs], H, KV, d, 32, dt, 1)
+        p.qkv[:, :H * d] = 16384.0
+        levels = [torch.tensor([r.randint(-7, 7) for _ in range(a + b)], device="cuda") for a, b in p.seqs]
+        p.param[0, ..., 0] = step
+        p.param[0, ..., 1] = -8 * step
+        for s, lv in enumerate(levels):
+            for i in range(0, len(lv), 32):
+                n = min(32, len(lv) - i)
+                p.codes[0, p.table[s][i // 32], :, :n] = (lv[i:i + n] + 8).to(torch.uint8)[None, :, None]
+        p.write()
+        out = torch.full((p.M, H * d), 77.0, dtype=p.qkv.dtype, device="cuda")
+        slopes = torch.zeros(H, device="cuda") if biases else None
+        lpq.lpq_paged_attention4(p.qkv, p.k, p.v, ints(p.table), ints(p.cu), ints([a + b for a, b in p.seqs]), max_q=max_q, alibi_slopes=slopes, out=out)
+        for s, (past, n) in enumerate(p.seqs):
+            L = past + n
+            at, off = torch.tensor([p.table[s][j // 32] for j in range(L)], device="cuda"), torch.arange(L, device="cuda") % 32
+            par = p.param[1, at, :, off].double()
+            v = p.codes[1, at, :, off].double() * par[..., :1] + par[..., 1:]
+            for t in range(n):
+                seen = levels[s][:past + t + 1]
+                rows = v[:past + t + 1][seen == seen.max()].repeat_interleave(H // KV, 1)
+                want, size = rows.mean(0), rows.abs().mean(0) + 7 * float(par[..., 0].max())
+                err = (out[p.cu[s] + t].double().view(H, d) - want).abs()
+                assert bool((err <= u * want.abs() + (U16 + 2.0**-20) * size + 2.0**-25).all()), (max_q, step, s, t, float((err / size).max()))
+
+
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_many_small_weights(dt, biases):
+    """One key that outweighs each of the others by 2^25.5 and has a value of zero, and thousands of others with ones, made of codes 15.  Off by the weights' and the values'
+    rounding (2 u16 of the result, in tiles), the others' weights times scales beside 2^12 or more for the one's (a step of 2^-24 beside 2^12 2^-25.5, halved: 2^-11.5, seven
+    fifteenths of it), exponents of 25.5 from exact 32-bit products (2^-12), 32-bit sums (2 n 2^-24) and the output's rounding.  Short chunks multiply rounded weights times
+    scales by code - 8, and the one's code is 0: its weight is (nearly) 1, its scale 2^-4, so that alone is off by u16 2^-4 8 at most, as in attention_ref's bound."""
+    import torch
+    u, H, KV, d = {"fp16": 2.0**-11, "bf16": 2.0**-8}[dt], 4, 2, 64
+    for past, n in ((60000, 1), (30000, 3), (9000, 64), (3000, 300)):
+        p = Cells([(past, n)], H, KV, d, 64, dt)
+        p.qkv.zero_()
+        p.qkv[:, :H * d:d] = 16.0
+        p.codes[0], p.param[0] = 0, 0.0
+        p.codes[1], p.param[1, ..., 0], p.param[1, ..., 1] = 15, 0.0625, 0.0625
+        at = past // 3
+        p.codes[0, p.table[0][at // 64], :, at % 64, 0] = 1
+        p.param[0, p.table[0][at // 64], :, at % 64, 0] = 8.84375
+        p.codes[1, p.table[0][at // 64], :, at % 64] = 0
+        p.param[1, p.table[0][at // 64], :, at % 64, 1] = 0.0
+        p.write()
+        out = torch.full((p.M, H * d), 77.0, dtype=p.qkv.dtype, device="cuda")
+        lpq.lpq_paged_attention4(p.qkv, p.k, p.v, ints(p.table), ints(p.cu), ints([past + n]), max_q=n, alibi_slopes=torch.zeros(H, device="cuda") if biases else None, out=out)
+        rest = (past + torch.arange(n, device="cuda").double()) * math.exp(-2 * float(p.param[0, p.table[0][at // 64], 0, at % 64, 0]))
+        want = (rest / (1 + rest))[:, None]
+        allowed = (u + 2 * U16 + 2.0**-12.6 + 2.0**-12 + 2 * (past + n) * 2.0**-24) * want + (U16 * 2.0**-4 * 8 if 2 * n <= 32 else 0.0) * (1 + u) + 2.0**-25
+        far = float(((out.double() - want).abs() / allowed).max())
+        assert far <= 1.0, (past, n, far)
+
+
+def test_pool_past_32_bits():
+    """Pages more than 2^32 bytes into the pool."""
+    import torch
+    P, KV, d = 256, 16, 128
+    size = lpq.lpq_cell_page_bytes(P, d)
+    n_pages = 2**32 // (KV * size) + 40
+    k, v = (torch.zeros((n_pages, KV, size), dtype=torch.uint8, device="cuda") for _ in range(2))
+    p = Cells([(700, 1), (100, 40)], 16, KV, d, P, "fp16")
+    off = n_pages - p.n_pages
+    k[off:], v[off:] = p.k, p.v
+    want, _ = p.run(max_q=40)
+    p.table = [[t + off if t >= 0 else t for t in row] for row in p.table]
+    out = torch.full_like(want, 77.0)
+    lpq.lpq_paged_attention4(p.qkv, k, v, ints(p.table), ints(p.cu), ints([701, 140]), max_q=40, out=out)
+    assert torch.equal(out, want)
+    rows, slots = p.qkv[:2].contiguous(), ints([(n_pages - 1) * P + 255, 3])
+    lpq.lpq_paged_append4(rows, k, v, slots)
+    small = [torch.zeros((1, KV, size), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    lpq.lpq_paged_append4(rows, *small, ints([255, 3]))
+    got, ref = (lpq.lpq_paged_load4(a, b, s, torch.zeros_like(rows)) for a, b, s in ((k, v, slots), (*small, ints([255, 3]))))
+    assert torch.equal(got, ref) and bool((got[:, 16 * d:] != 0).any())
+
+
+def test_same_inputs_same_bits():
+    import torch
+    p = Cells([(3000, 1), (700, 60), (10, 1)], 8, 2, 128, 16, "fp16")
+    a, _ = p.run(max_q=60)
+    for _ in range(3):
+        assert torch.equal(p.run(max_q=60)[0], a)
+
+
+def test_binding_checks():
+    import torch
+    p = Cells([(30, 1), (20, 1)], 4, 2, 64, 16, "fp16")
+    t, cu, kv, slots = ints(p.table), ints(p.cu), ints([31, 21]), ints([3, 4])
+    call = lambda **k: lpq.lpq_paged_attention4(**{**dict(qkv=p.qkv, k_pages=p.k, v_pages=p.v, table=t, cu_q=cu, kv_lens=kv), **k})
+    call()
+    for bad in (dict(qkv=p.qkv.float()), dict(qkv=p.qkv[:, :-8].contiguous()), dict(k_pages=p.k[:, :1].contiguous()), dict(v_pages=p.v[1:]), dict(k_pages=p.k[..., :-4].contiguous(), v_pages=p.v[..., :-4].contiguous()),
+                dict(k_pages=p.k.view(torch.int8), v_pages=p.v.view(torch.int8)), dict(table=t.long()), dict(table=t[:1]), dict(cu_q=cu[:2]), dict(kv_lens=kv.cpu()), dict(table=t.t()),
+                dict(out=p.qkv), dict(out=torch.zeros((2, 256), device="cuda")), dict(alibi_slopes=torch.ones(3, device="cuda")), dict(qkv=p.qkv.cpu())):
+        with pytest.raises(ValueError):
+            call(**bad)
+    for bad in (dict(max_q=0), dict(max_kv=0), dict(qkv=p.qkv[:, :-64].contiguous())):      # 3 heads over 2 K/V heads
+        with pytest.raises(lpq.LpqError):
+            call(**bad)
+    for bad in ((p.qkv, p.k, p.v, ints([1])), (p.qkv, p.k, p.v, slots.long()), (p.qkv, p.k[1:], p.v, slots), (p.qkv.t(), p.k, p.v, slots)):
+        with pytest.raises(ValueError):
+            lpq.lpq_paged_append4(*bad)
+        with pytest.raises(ValueError):
+            lpq.lpq_paged_load4(bad[1], bad[2], bad[3], bad[0])
+    table, gamma = rotary_table(10, 64), torch.ones(64, dtype=torch.float16, device="cuda")
+    turn = lambda **k: lpq.lpq_qk_norm_rotary(**{**dict(qkv=p.qkv, positions=slots, n_heads=4, n_kv_heads=2, cos_sin=table, out=torch.empty_like(p.qkv)), **k})
+    turn()
+    for bad in (dict(n_heads=5), dict(n_kv_heads=0), dict(positions=slots[:1]), dict(positions=slots.long()), dict(cos_sin=table.double()), dict(cos_sin=table[:, ::2]), dict(q_gamma=gamma[:32]),
+                dict(k_gamma=gamma.float()), dict(slots=ints([1])), dict(out=torch.empty_like(p.qkv)[:1]), dict(qkv=p.qkv.cpu())):
+        with pytest.raises(ValueError):
+            turn(**bad)
+    both = torch.zeros((3, p.qkv.shape[1]), dtype=torch.float16, device="cuda")
+    for bad in (dict(cos_sin=rotary_table(10, 80)), dict(cos_sin=rotary_table(10, 24)), dict(positions=None), dict(q_gamma=gamma, eps=0.0), dict(qkv=both[:2], out=both[1:])):
+        with pytest.raises(lpq.LpqError):
+            turn(**bad)
+
+
+# ---- a run of them together -------------------------------------------------------------------------------------------
+
+def stored(p_k, p_v, table, L, P, d, dt):
+    """Codes and parameters of a sequence's first L positions, read from the pages' bytes: as attention_ref takes them."""
+    import torch
+    codes, params = [], []
+    at = torch.arange(L, device="cuda")
+    page = torch.tensor([table[j // P] for j in range(L)], dtype=torch.long, device="cuda")
+    for pages in (p_k, p_v):
+        g = pages.view(pages.shape[0], pages.shape[1], P // 16, 16 * (d // 2 + 4))[page, :, at % P // 16]                   # [L][KV][bytes]
+        i = at % 16
+        words = g[..., :8 * d].reshape(L, -1, 16, d // 2)[at, :, i].contiguous().view(torch.int32)                          # [L][KV][d / 8]
+        codes.append(torch.stack([words >> (4 * (e // 2) + 16 * (e % 2)) & 15 for e in range(8)], -1).flatten(2))
+        params.append(g[..., 8 * d:].reshape(L, -1, 16, 4)[at, :, i].contiguous().view(dtype_of(dt)).double())
+    c, p = torch.stack(codes), torch.stack(params)
+    return c, p[..., 0], p[..., 1]
+
+
+@pytest.mark.parametrize("dt,interleaved", [("fp16", False), ("bf16", True)])
+def test_serving_run(dt, interleaved):
+    """Requests come, are prefilled (whole and in chunks) and decode side by side, some finish and their pages go to others: plan, norms and rotation, append, attention.  Every step's
+    attention against 64 bits over what the pages hold, and the pages against the definition's codes of the rows as they were rotated."""
+    import torch
+    H, KV, d, P, n_pages, width, N, M = 8, 2, 64, 16, 40, 12, 6, 96
+    cols, g = (H + 2 * KV) * d, gen(5)
+    size = lpq.lpq_cell_page_bytes(P, d)
+    k, v = (torch.full((n_pages, KV, size), 255, dtype=torch.uint8, device="cuda") for _ in range(2))                       # NaN throughout
+    table, ring, counters = torch.full((N, width), -1, dtype=torch.int32, device="cuda"), torch.arange(n_pages, dtype=torch.int32, device="cuda"), ints([0, n_pages])
+    lens = torch.zeros(N, dtype=torch.int32, device="cuda")
+    angles = rotary_table(width * P, d)
+    gammas = [(1 + 0.2 * torch.randn(d, generator=g, device="cuda")).to(dtype_of(dt)) for _ in range(2)]
+    steps = [[50, 0, 20, 0, 0, 0], [1, 30, 1, 40, 0, 0], [1, 1, 1, 30, 9, 0], [1, 1, -1, 1, 1, 60], [1, -1, 25, 1, 1, 20], [1, 33, 1, -1, 30, 1], [40, 1, 1, 45, 1, 1], [1, 1, 1, 1, 1, 1]]
+    for step, q in enumerate(steps):
+        x = torch.randn((M, cols), generator=g, device="cuda").to(dtype_of(dt))
+        plan = lpq.lpq_paged_plan(lens, ints(q), table, ring, counters, P, M)
+        lens, counters = plan.kv_lens, plan.counters
+        assert plan.info[3].item() == 0, "the pool is large enough for these requests"
+        live = int(plan.info[0])
+        ref, err = rotary_ref(x[:live], H, KV, d, plan.positions[:live], angles, interleaved, *gammas, 1e-6)
+        before = x.clone()
+        assert lpq.lpq_qk_norm_rotary(x, plan.positions, H, KV, cos_sin=angles, interleaved=interleaved, q_gamma=gammas[0], k_gamma=gammas[1], slots=plan.slots) is x
+        u = {"fp16": 2.0**-11, "bf16": 2.0**-8}[dt]
+        assert float(((x[:live].double() - ref).abs() / (u * (ref.abs() + err) + err + 2.0**-25)).max()) <= 1.0
+        assert torch.equal(x[live:], before[live:])
+        lpq.lpq_paged_append4(x, k, v, plan.slots)
+        out = torch.full((M, H * d), 77.0, dtype=x.dtype, device="cuda")
+        lpq.lpq_paged_attention4(x, k, v, table, plan.cu_q, lens, max_q=max(q), out=out)
+        parts, r0, rows_of_table, xs = [], 0, table.tolist(), x.float().cpu().numpy()
+        for s, n in enumerate(q):
+            if n < 0:
+                continue
+            L = int(lens[s])
+            cells = stored(k, v, rows_of_table[s], L, P, d, dt) if L else (torch.zeros((2, 0, KV, d), device="cuda"),) + (torch.zeros((2, 0, KV), dtype=torch.float64, device="cuda"),) * 2
+            for t in range(0, n, 7):                   # some of the new rows' cells
+                for i in range(2):
+                    for h in range(KV):
+                        at = (H + i * KV + h) * d
+                        codes, scale, zero = quantise(xs[r0 + t, at:at + d], dt)
+                        assert np.array_equal(cells[0][i, L - n + t, h].cpu().numpy(), codes)
+                        assert float(cells[1][i, L - n + t, h]) == of_bits(scale, dt) and float(cells[2][i, L - n + t, h]) == of_bits(zero, dt)
+            parts.append(((r0, r0 + n), attention_ref(x[r0:r0 + n, :H * d].reshape(n, H, d), cells, torch.ones(L, dtype=torch.bool, device="cuda"),
+                                                      L - n + torch.arange(n, device="cuda"), None, n * (H // KV) > 32, dt)))
+            r0 += n
+        check_attention(out, parts, what="step %d" % step)
+
+
+def test_prompts_that_see_what_later_steps_see():
+    """A prompt's K and V through the cache and back into its rows, then attention over the packed rows: what attention over the pages gives, within both bounds."""
+    import torch
+    H, KV, d, P, lens = 6, 2, 128, 32, [150, 40, 1]
+    M, cu = sum(lens) + 2, np.concatenate([[0], np.cumsum(lens)])
+    x = torch.randn((M, (H + 2 * KV) * d), generator=gen(3), device="cuda").half()
+    table, ring = torch.full((3, 6), -1, dtype=torch.int32, device="cuda"), torch.arange(20, dtype=torch.int32, device="cuda").flip(0).contiguous()
+    plan = lpq.lpq_paged_plan(ints([0] * 3), ints(lens), table, ring, ints([0, 20]), P, M)
+    k, v = (torch.zeros((20, KV, lpq.lpq_cell_page_bytes(P, d)), dtype=torch.uint8, device="cuda") for _ in range(2))
+    lpq.lpq_paged_append4(x, k, v, plan.slots)
+    q = x[:, :H * d].clone()
+    assert lpq.lpq_paged_load4(k, v, plan.slots, x) is x
+    assert torch.equal(x[:, :H * d], q)
+    paged, packed = lpq.lpq_paged_attention4(x, k, v, table, plan.cu_q, plan.kv_lens, max_q=150), lpq.lpq_packed_attention(x, plan.cu_q, H, KV, max_q=150)
+    # K rounded on either side or one: scores of |q| |k| / sqrt(d) up to some 20, off by 2^-11 of that at most; V and weights rounded; |v| up to 4.5
+    assert float((paged.float() - packed.float()).abs().max()) <= (2 * 20 * 2.0**-11 + 4 * 2.0**-11) * 4.5
+
+
+# ---- streams and graphs -----------------------------------------------------------------------------------------------
+
+def test_on_another_stream():
+    import torch
+    p = Cells([(900, 1), (40, 30)], 8, 2, 64, 16, "fp16", 2)
+    want, _ = p.run(max_q=30)
+    table, pos, slots = rotary_table(200, 64), ints([i % 200 for i in range(p.M)]), ints(list(range(p.M)))
+    turned = lpq.lpq_qk_norm_rotary(p.qkv, pos, 8, 2, cos_sin=table, out=torch.empty_like(p.qkv))
+    k, v, back = torch.zeros_like(p.k), torch.zeros_like(p.v), torch.zeros_like(p.qkv)
+    lpq.lpq_paged_append4(turned, k, v, slots)
+    lpq.lpq_paged_load4(k, v, slots, back)
+    s = torch.cuda.Stream()
+    t, cu, kv = ints(p.table), ints(p.cu), ints([901, 70])
+    outs = [torch.full_like(want, 77.0), torch.empty_like(p.qkv), torch.zeros_like(p.k), torch.zeros_like(p.v), torch.zeros_like(p.qkv)]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)                      # the current stream is busy
+    lpq.lpq_paged_attention4(p.qkv, p.k, p.v, t, cu, kv, max_q=30, out=outs[0], stream=s)
+    lpq.lpq_qk_norm_rotary(p.qkv, pos, 8, 2, cos_sin=table, out=outs[1], stream=s)
+    lpq.lpq_paged_append4(outs[1], outs[2], outs[3], slots, stream=s)
+    lpq.lpq_paged_load4(outs[2], outs[3], slots, outs[4], stream=s)
+    made = lpq.lpq_paged_attention4(p.qkv, p.k, p.v, t, cu, kv, max_q=30, stream=s)
+    s.synchronize()
+    with torch.cuda.stream(s):
+        assert all(torch.equal(a, b) for a, b in zip(outs, (want, turned, k, v, back)))
+        assert torch.equal(made[:31], want[:31]) and bool((made[31:] == 0).all())
+
+
+def test_captured_steps():
+    """A step (plan in place, rotation in place, append, attention) captured once and replayed with lengths that move sequences between the kernels; eager work of other sizes,
+    with its own use of the workspace, between the replays."""
+    import torch
+    H, KV, d, P, N, M, n_pages = 8, 2, 128, 16, 4, 1900, 400
+    rows = torch.randn((M, (H + 2 * KV) * d), generator=gen(1), device="cuda").half()
+    ring, table = torch.randperm(n_pages, generator=gen(4), device="cuda").to(torch.int32), rotary_table(140 * P, 64)
+    size = lpq.lpq_cell_page_bytes(P, d)
+
+    def fresh():
+        return dict(x=torch.zeros_like(rows), k=torch.zeros((n_pages, KV, size), dtype=torch.uint8, device="cuda"), v=torch.zeros((n_pages, KV, size), dtype=torch.uint8, device="cuda"),
+                    table=torch.full((N, 140), -1, dtype=torch.int32, device="cuda"), ring=ring.clone(), counters=ints([0, n_pages]), lens=ints([0] * N), q=ints([0] * N),
+                    plan=[torch.zeros(m, dtype=torch.int32, device="cuda") for m in (N + 1, N, M, M, 2, 4)], out=torch.zeros((M, H * d), dtype=torch.float16, device="cuda"))
+
+    def step(s):
+        plan = (s["plan"][0], s["lens"], s["plan"][2], s["plan"][3], s["counters"], s["plan"][5])
+        s["x"].copy_(rows)
+        lpq.lpq_paged_plan(s["lens"], s["q"], s["table"], s["ring"], s["counters"], P, M, plan=plan)
+        lpq.lpq_qk_norm_rotary(s["x"], s["plan"][3], H, KV, cos_sin=table, slots=s["plan"][2])
+        lpq.lpq_paged_append4(s["x"], s["k"], s["v"], s["plan"][2])
+        lpq.lpq_paged_attention4(s["x"], s["k"], s["v"], s["table"], s["plan"][0], s["lens"], max_q=1500, max_kv=2000, out=s["out"])
+
+    names = ("x", "k", "v", "out", "lens", "counters", "table", "ring")
+    steps = [[1500, 20, 0, 300], [1, 1, 900, 1], [1, 200, 40, 1], [-1, 1, 1, 500], [600, 1, -1, 1], [1, 1, 5, 1]]
+    eager, want = fresh(), []
+    for q in steps:
+        eager["q"].copy_(ints(q))
+        step(eager)
+        want.append([eager[n].clone() for n in names])
+        assert eager["plan"][5][3].item() == 0
+    s = fresh()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(s)
+    other = Cells([(3000, 1), (100, 40)], 8, 2, 128, 32, "fp16")
+    other_want, _ = other.run(max_q=40)
+    for q, w in zip(steps, want):
+        s["q"].copy_(ints(q))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(s[n], t) for n, t in zip(names, w)), q
+        assert torch.equal(other.run(max_q=40)[0], other_want)
