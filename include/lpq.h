@@ -400,10 +400,11 @@ lpq_status lpq_paged_append4(const void* qkv, const lpq_attn_cfg* cfg, const lpq
 lpq_status lpq_paged_load4(const void* k_pages, const void* v_pages, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const int32_t* slots, int32_t M,
                            void* qkv, void* hip_stream);
 
-/* lpq_paged_attention over pages of cells, with the same arguments, masks and limits.  Where a sequence and K/V head have more than 32 rows, values of cells are rounded to
- * the type (as lpq_paged_load4 gives them) before they are multiplied; with fewer they are not rounded.  A position that is stored as NaN makes the rows that see it NaN.
- * Partial results are kept in the library's workspace, up to 290 MiB of them, split less under a smaller reservation as there: tiles of chunks and prompts first, then, below
- * 34 MiB, decoding sequences too.
+/* lpq_paged_attention over pages of cells, with the same arguments, masks and limits.  A position that is stored as NaN makes the rows that see it NaN.  Products are of
+ * 16-bit floats with 11 bits, sums of 32 bits.  Where a sequence and K/V head have up to 32 rows, codes are multiplied as they are: rounded are the query's elements
+ * 2^-24 of the largest and smaller, and weights times V's scales.  With more rows, values of cells and weights are rounded (bf16: tiles of values without their power of two).
+ * Partial results are kept in the library's workspace, up to 290 MiB of them.  A smaller reservation splits less: tiles of chunks and prompts first, then, below 34 MiB,
+ * decoding sequences too.
  * Errors: as lpq_paged_attention. */
 lpq_status lpq_paged_attention4(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const void* k_pages, const void* v_pages,
                                 const float* alibi_slopes, const int32_t* cu_q, const int32_t* kv_lens, int32_t n_seqs, int32_t M,

@@ -11,7 +11,7 @@ k_j = s_j c_j + z_j and v_j = s'_j c'_j + z'_j.  Of all kernels:
 Up to 32 rows of a sequence and K/V head (codes are multiplied):
   * the matrix units keep a sum of eight products of codes, which are subnormal numbers in steps of 2^-20, to 2^-38 of the largest other factor: to
     2^-18 of a step.  In the score 2^-18 s sum |q_i|, in the result 2^-18 sum w_j s'_j
-  * weights times scales are rounded to fp16, the codes' distance from 8 is what they multiply:   u16 sum w_j s'_j |c'_j - 8|, and 8 n 2^-39 max w_j s'_j for those
+  * weights times scales are rounded to fp16, the codes' distance from 8 is what they multiply:   u16 sum w_j s'_j |c'_j - 8|, and 8 n 2^-37 max w_j s'_j for those
     below its normal range beside a largest of 2^12 or more.
 More rows (values v are v 2^-e in fp16, with the largest of 32 s and 2^-14 |z| of a tile's keys, for V of all so far, between 2^e and 2^(e + 1); steps of at least 2^-24,
 half of which is 2^-24 of the largest of 15 s and |z|, or less):
