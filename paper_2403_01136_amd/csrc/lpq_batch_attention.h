@@ -437,9 +437,11 @@ template <int DT, int D, bool ALIBI, int SRC>
 __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 {
     // Products are of the rows' type; of cells in fp16 for either type, with tiles and queries of bf16 taken by powers of two.
-    // Rounded K puts 2.5e-4 of a result of ordinary scores into it, V 2.0e-4, beside an output's rounding of 2.1e-4 (fp16) and 1.6e-3 (bf16).  (K as codes, with scale and zero behind
-    // the products, was exact and 12 % slower: two chunks of up to 512 tokens beside 9 sequences that decode, 56 heads over 8, biases, 134.6 us for 120.7.)
     constexpr bool SCALED = SRC == SRC_CELLS && DT == LPQ_DT_BF16;
+    // K of fp16 cells stays codes, whose products with a row get scale and zero behind them, as in the streaming kernel: rounded K puts 2.5e-4 of a result of ordinary scores into it,
+    // V 2.0e-4, beside an output's rounding of 2.1e-4 (fp16) and 1.6e-3 (bf16).  It takes 6 % (two chunks of up to 512 tokens beside 9 sequences that decode, 56 heads over 8, biases:
+    // 128.3 us; K rounded 120.8; parameters in LDS as fp32 products with c, twice the reads, 132.6); V so would take as much again and leave weights times scales rounded instead.
+    constexpr bool K_CODES = SRC == SRC_CELLS && DT == LPQ_DT_FP16;
     constexpr int PT = SRC == SRC_CELLS ? (int)LPQ_DT_FP16 : DT;
     typedef typename Elem<PT>::v8 V8;
     constexpr int CH = D / 8, KS = D / 16, DTL = D / 32, ROWS = 512 / D, FILLS = 16 / ROWS;       // chunks of a row; feature steps; feature tiles; keys per load; loads of a wave's 16 keys
@@ -535,6 +537,7 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
     };
 
     V8 qf[KS];                                         // Q^T operands: lane (row col, features 16 k + 8 half ..)
+    float qsum = 0.0f;                                 // K_CODES: the sum of the row, in steps of the codes
     {
         const uint16_t* qp = a.qkv + (size_t)(q.first + tok) * cols + head * D + 8 * half;
 #pragma unroll
@@ -556,6 +559,13 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
                 qf[k] = __builtin_bit_cast(V8, x);
             }
             c = __builtin_ldexpf(c, ex);
+        }
+        if constexpr (K_CODES) {
+#pragma unroll
+            for (int k = 0; k < 4 * KS; ++k) qsum = Elem<PT>::add_pair(__builtin_bit_cast(u32x4, qf[k / 4])[k % 4], qsum);
+            const f2 z = both_halves(qsum);
+            qsum = (z[0] + z[1]) * 0x1p-20f;
+            c *= 0x1p20f;
         }
     }
     f16x o[DTL];
@@ -581,10 +591,12 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
     uint32_t* const odd_values = reinterpret_cast<uint32_t*>(smem_raw + 4 * TILE_BYTES);
     if (lane == 0) odd_values[wave] = 0;
 
-    float near[ALIBI ? 16 : 1];                        // bias of a register's key within its 32
-    if constexpr (ALIBI)
+    float near[ALIBI ? 16 : 1];                        // bias of a register's key within its 32; K_CODES: over c
+    if constexpr (ALIBI) {
+        const float per_key = K_CODES ? slope / c : slope;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) near[i] = slope * (float)(8 * (i / 4) + i % 4);
+        for (int i = 0; i < 16; ++i) near[i] = per_key * (float)(8 * (i / 4) + i % 4);
+    }
 
     // Cells: tile j's parameters have landed.  Keys that no row sees get none (values of zero, like their weights; K's scores are replaced); and, in
     // bf16, the largest of K's and of V's among the wave's keys for all waves.
@@ -606,6 +618,7 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
             tops[8 * buf + 4 + wave] = vt;
         }
     };
+    uint32_t* const kparams = reinterpret_cast<uint32_t*>(smem_raw + 4 * TILE_BYTES + 80);       // K_CODES: [n % 2][key]
     int k_ex = 0, v_ex = -200, k_ex_next = 0, v_ex_next = -200;                 // the tile's K is taken by 2^-k_ex, its V and the sums by 2^-v_ex
     // the values of the cells into LDS
     auto place = [&](int j, int buf) {
@@ -623,11 +636,12 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
             kp = scaled_pair<DT>(kparam, 20 - k_ex_next, -k_ex_next);
             vp = scaled_pair<DT>(vparam, 20 - v_ex_next, -v_ex_next);
         }
+        if (K_CODES && lane < 16) kparams[TILE_KEYS * buf + row] = kp;
         uint8_t *kr = smem_raw + buf * TILE_BYTES + row * D * 2, *vr = kr + 2 * TILE_BYTES;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
             const int chunk = (D / 32) * (lane >> 4) + i;
-            *reinterpret_cast<u32x4*>(kr + 16 * (chunk ^ k_swizzle<D>(row))) = tile_values<SCALED>(kcodes[i], kp);
+            *reinterpret_cast<u32x4*>(kr + 16 * (chunk ^ k_swizzle<D>(row))) = K_CODES ? code_pairs(kcodes[i]) : tile_values<SCALED>(kcodes[i], kp);
             *reinterpret_cast<u32x4*>(vr + 16 * (chunk ^ v_swizzle_cells<D>(row))) = tile_values<SCALED>(vcodes[i], vp);
         }
     };
@@ -724,13 +738,23 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         for (int k = 0; k < KS; ++k) s[1] = Elem<PT>::mfma32(rb[k], qf[k], k == 0 ? zero : s[1]);
         __builtin_amdgcn_sched_barrier(0);
         const float ct = SCALED ? __builtin_ldexpf(c, k_ex) : c;
+        if constexpr (K_CODES)                         // by instructions that take the parameters as they are
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const u32x4 par = *reinterpret_cast<const u32x4*>(kparams + TILE_KEYS * buf + 32 * kt + 2 * i + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s[kt][i + e] = __builtin_fmaf(param_scale<DT>(par[e]), s[kt][i + e], __builtin_fmaf(param_zero<DT>(par[e]), qsum, ALIBI ? near[ALIBI ? i + e : 0] : 0.0f));
+                }
         float base[2] = {0.0f, 0.0f};                  // bias of a 32-key tile's first key; the others' are in near[]
         if constexpr (ALIBI)                           // to base 2, with the bias within the 32 keys
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
                 base[kt] = slope * (float)(j0 + 32 * kt + 4 * half - p);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[kt][i] = __builtin_fmaf(s[kt][i], ct, near[i]);
+                for (int i = 0; i < 16 && !K_CODES; ++i) s[kt][i] = __builtin_fmaf(s[kt][i], ct, near[i]);
             }
         if (bad != 0 || j0 + TILE_KEYS > all_see) {    // some key of the tile is not for some row of the wave
             const int rel = min(p, tl.key_end - 1) - j0 - 4 * half;
@@ -745,7 +769,8 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mk[kt] = fmaxf(mk[kt], s[kt][i]);
-        float mx = ALIBI ? fmaxf(mk[0] + base[0], mk[1] + base[1]) : fmaxf(mk[0], mk[1]) * ct;
+        constexpr bool BASE_2 = ALIBI && !K_CODES;     // s is, with the bias
+        float mx = BASE_2 ? fmaxf(mk[0] + base[0], mk[1] + base[1]) : ALIBI ? fmaxf(__builtin_fmaf(mk[0], ct, base[0]), __builtin_fmaf(mk[1], ct, base[1])) : fmaxf(mk[0], mk[1]) * ct;
         const f2 m2 = both_halves(mx);
         mx = fmaxf(m2[0], m2[1]);
         // An exponent is c s - m by one FMA, m the rounded product of a largest s (or s + base - m, likewise): up to half of m's last place off.  Where that is much,
@@ -764,7 +789,7 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[kt][i] = (ALIBI ? s[kt][i] + base[kt] : s[kt][i] * ct) - (m == -INFINITY ? 0.0f : m);
+                    for (int i = 0; i < 16; ++i) s[kt][i] = ((BASE_2 ? s[kt][i] : s[kt][i] * ct) + base[kt]) - (m == -INFINITY ? 0.0f : m);
         }
         const float ms = m == -INFINITY ? 0.0f : m, by = large ? 1.0f : ct;
         const float from[2] = {large ? 0.0f : ms - base[0], large ? 0.0f : ms - base[1]};
@@ -776,8 +801,8 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
                 u32x4 x;
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e] - from[kt] : __builtin_fmaf(s[kt][i + e], by, -from[kt]));
-                    const float e1 = __builtin_amdgcn_exp2f(ALIBI ? s[kt][i + e + 1] - from[kt] : __builtin_fmaf(s[kt][i + e + 1], by, -from[kt]));
+                    const float e0 = __builtin_amdgcn_exp2f(BASE_2 ? s[kt][i + e] - from[kt] : __builtin_fmaf(s[kt][i + e], by, -from[kt]));
+                    const float e1 = __builtin_amdgcn_exp2f(BASE_2 ? s[kt][i + e + 1] - from[kt] : __builtin_fmaf(s[kt][i + e + 1], by, -from[kt]));
                     x[e / 2] = Elem<PT>::pack(e0, e1);
                     l = Elem<PT>::add_pair(x[e / 2], l);
                 }
@@ -866,8 +891,8 @@ __global__ __launch_bounds__(256) void tile_combine_kernel(AttnArgs a)
     *reinterpret_cast<u32x2*>(a.out + (size_t)(tl.q.first + tok) * a.heads * D + head * D + f) = x;
 }
 
-// LDS of a workgroup of the tile kernel: its tiles, a word per wave, and for cells the largest values of two tiles.  Allowed once per kernel and device where it is more than 64 KB.
-constexpr size_t tile_lds(int d, bool cells) { return (size_t)4 * TILE_KEYS * d * 2 + (cells ? 20 : 4) * sizeof(uint32_t); }
+// LDS of a workgroup of the tile kernel: its tiles, a word per wave, and for cells the largest values and K's parameters of two tiles.  Allowed once per kernel and device where it is more than 64 KB.
+constexpr size_t tile_lds(int d, bool cells) { return (size_t)4 * TILE_KEYS * d * 2 + (cells ? 20 + 2 * TILE_KEYS : 4) * sizeof(uint32_t); }
 template <auto KERNEL>
 static hipError_t allow_lds(size_t bytes)
 {

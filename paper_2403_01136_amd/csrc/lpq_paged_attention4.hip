@@ -1,15 +1,16 @@
 // Causal attention of new tokens over pages of 4-bit cells:
 //     out[row] = sum_j w_j v_j / sum_j w_j,   w_j = exp(q . k_j / sqrt(D) + slope (j - p)),   j <= p,   k_j = s_j c_j + z_j, v_j = s'_j c'_j + z'_j
 // with codes c of 0 to 15 for each feature and a scale and a zero for each key and head.  Rows, work lists, splits and the joining of parts are those of the
-// 16-bit caches' kernels.  The tile kernel (prompts and chunks) is theirs too, with values made from the cells on their way into LDS, rounded to the type.
+// 16-bit caches' kernels.  The tile kernel (prompts and chunks) is theirs too, with codes or values made from the cells on their way into LDS.
 //
 // The streaming kernel multiplies the codes themselves: scale and zero are one number each for a key, so
 //     q . k_j        = s_j (q . c_j) + z_j sum(q)
-//     sum_j w_j v_jf = sum_j (w_j s'_j) (c'_jf - 8) + sum_j w_j (z'_j + 8 s'_j)
-// where the first sum of each is the matrix units' and the others cost two operations a score.  A code in the last bits of an fp16 number with no exponent is
-// that number, code * 2^-24 (or 2^-20 four bits higher): unpacking is one AND per pair and half a shift, for queries of either type: those in bf16 are taken by a power of two
-// for each row, which changes none of their eight bits that count.  Codes are exact; what is rounded are the weights w s', to fp16 beside a
-// largest of 2^15, and only the codes' distance from 8 sees it.
+//     sum_j w_j v_jf = sum_j (w_j s'_j) c'_jf + sum_j w_j z'_j
+// where the first sum of each is the matrix units' and the others cost two operations a score.  A code in bits 4 to 7 of an fp16 number without exponent is that number,
+// code * 2^-20: unpacking a word of eight takes three shifts and four ANDs, for queries of either type: those in bf16 are taken by a power of two for each row, which changes
+// none of their eight bits that count.  Codes are exact; what is rounded are the weights w s', to fp16 beside a largest of 2^12 or more.  What that takes from them is added up in
+// 32 bits and counts as for a code of 8, so that only the codes' distance from it sees the rounding; in fp16, where tiles of up to 8 rows leave columns of the products idle, it
+// has those (an error of 2.1e-4 of a result, all of it the output's rounding, where it was 3.0e-4 to 3.2e-4 without; 16 sequences of 40 heads 18.6 us for 18.4).
 #include <algorithm>
 
 #include "lpq_batch_attention.h"
@@ -88,6 +89,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
     constexpr int W = D / 32, F = D / 16;                                        // words of a lane's codes of a key; its features of V
     constexpr int NT = ROWS == 32 ? 2 : 1, PARTS = ROWS < 16 ? 16 / ROWS : 1, N = 8 / PARTS;     // column tiles; parts of the keys; a lane's keys of a step
     constexpr int SLOT = ROWS * (D + 2);
+    constexpr bool FINE = DT == LPQ_DT_FP16 && PARTS > 1;                        // what rounding takes from weights goes to idle columns
     typedef uint32_t kcodes_t __attribute__((ext_vector_type(W)));
     typedef uint32_t params_t __attribute__((ext_vector_type(N < 4 ? N : 4)));
     typedef std::conditional_t<D == 128, uint32_t, uint16_t> vcodes_t;
@@ -196,6 +198,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
             for (int e = 0; e < F; ++e) o[t][e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 
+        const int rest_of = FINE ? __builtin_amdgcn_update_dpp(0, part, 0x120 + ROWS, 0xf, 0xf, false) : 0;
         // the lane's keys of a step, in order of the quarters' eight {4 quarter + 0..3, 16 + 4 quarter + 0..3}: N from the part's N-th on
         const int my_group = N < 8 ? part * N / 4 : 0, my_key = 16 * my_group + 4 * quarter + part * N % 4;
         const uint32_t koff = (uint32_t)(col * (D / 2) + quarter * (D / 8)), voff = (uint32_t)(4 * quarter * (D / 2) + col * (D / 32)), poff = (uint32_t)(8 * D + 4 * (my_key % 16));
@@ -356,7 +359,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     for (int f = 0; f < F; ++f) o[t][f] *= by;
                     G[t] = g;
                 }
-                uint32_t pk[N / 2];
+                uint32_t pk[N / 2], rk[N / 2];
 #pragma unroll
                 for (int k = 0; k < N; k += 2) {
                     const float t0 = ts[k] * G[t], t1 = ts[k + 1] * G[t];
@@ -364,11 +367,15 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     zs[t] = __builtin_fmaf(pw[k], param_zero<DT>(par[k]), zs[t]);
                     zs[t] = __builtin_fmaf(pw[k + 1], param_zero<DT>(par[k + 1]), zs[t]);
                     pk[k / 2] = Elem<LPQ_DT_FP16>::pack(t0, t1);
-                    ws[t] = __builtin_amdgcn_fdot2(as_h2(pk[k / 2]), h2{-1, -1}, ws[t] + (t0 + t1), false);
+                    if constexpr (FINE) {
+                        const h2 p16 = as_h2(pk[k / 2]);
+                        rk[k / 2] = __builtin_amdgcn_update_dpp(0, Elem<LPQ_DT_FP16>::pack(t0 - (float)p16[0], t1 - (float)p16[1]), 0x120 + ROWS, 0xf, 0xf, false);     // row_ror
+                    } else ws[t] = __builtin_amdgcn_fdot2(as_h2(pk[k / 2]), h2{-1, -1}, ws[t] + (t0 + t1), false);
                 }
-                u32x4 operand;                         // zero for the keys of other parts
+                u32x4 operand;                         // this part's keys; FINE: what the next part's lost; zero for the others
 #pragma unroll
-                for (int k = 0; k < 4; ++k) operand[k] = PARTS == 1 || part == k / (N / 2) ? pk[k % (N / 2)] : 0u;
+                for (int k = 0; k < 4; ++k)
+                    operand[k] = PARTS == 1 || part == k / (N / 2) ? pk[k % (N / 2)] : FINE && (PARTS == 2 || rest_of == k / (N / 2)) ? rk[k % (N / 2)] : 0u;
                 pf[t] = __builtin_bit_cast(h8, operand);
             }
             // V^T operands: halves of two keys' words side by side, then pairs by AND

@@ -13,9 +13,10 @@ Up to 32 rows of a sequence and K/V head (codes are multiplied):
     2^-18 of a step.  In the score 2^-18 s sum |q_i|, in the result 2^-18 sum w_j s'_j
   * weights times scales are rounded to fp16, the codes' distance from 8 is what they multiply:   u16 sum w_j s'_j |c'_j - 8|, and 8 n 2^-37 max w_j s'_j for those
     below its normal range beside a largest of 2^12 or more.
-More rows (values v are v 2^-e in fp16, with the largest of 32 s and 2^-14 |z| of a tile's keys, for V of all so far, between 2^e and 2^(e + 1); steps of at least 2^-24,
-half of which is 2^-24 of the largest of 15 s and |z|, or less):
-  * K and V are rounded: the score by u16 sum |q_i k_i| and 2^-24 max (15 s, |z|) sum |q_i|, the result by u16 A + 2^-24 max (15 s', |z'|)
+More rows:
+  * K in fp16 as above; in bf16, and V, values v are v 2^-e in fp16, with the largest of 32 s and 2^-14 |z| of a tile's keys, for V of all so far, between 2^e and
+    2^(e + 1), and steps of at least 2^-24, half of which is 2^-24 of the largest of 15 s and |z|, or less (fp16: as they are, half a smallest step 2^-25): the score is off by
+    u16 sum |q_i k_i| and 2^-24 max (15 s, |z|) sum |q_i|, the result by u16 A + 2^-24 max (15 s', |z'|) + 2^-25 (fp16)
   * weights are rounded, in the products and in the sum that divides them:                u16 (A + |out|), and n 2^-25 max |v|."""
 import math
 import random
@@ -281,7 +282,7 @@ def attention_ref(q, cells, ok, pos, slopes, tile, dt):
         s = (qh @ kh.t().contiguous()) / math.sqrt(d)
         size = qh.abs().sum(1, keepdim=True) / math.sqrt(d)                      # sum |q_i|
         err = (d + 8) * 2.0**-24 * size * (15 * sk + zk.abs())[None, :]
-        if tile:
+        if tile and dt == "bf16":
             err = err + U16 * (qh.abs() @ kh.abs().t().contiguous()) / math.sqrt(d) + 2.0**-24 * size * torch.maximum(15 * sk, zk.abs()).amax()
         else:
             err = err + 2.0**-18 * size * sk[None, :]
