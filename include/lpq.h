@@ -403,68 +403,6 @@ lpq_status lpq_paged_load4(const void* k_pages, const void* v_pages, const lpq_a
 /* lpq_paged_attention over pages of cells, with the same arguments, masks and limits.  A position that is stored as NaN makes the rows that see it NaN.  Products are of
  * numbers with 11 bits, sums of 32 bits.  Where a sequence and K/V head have up to 32 rows, codes are multiplied as they are, and weights times V's scales are what is rounded.
  * With more, weights and values of V are, and in bf16 values of K (tiles of them without a power of two).
- * Partial results are kept in the library's workspace, up to 290 MiB of them; where a reservation has room for less the work is split less: first the tiles of
- * chunks and prompts, then, below 17 MiB (34 with 17 to 32 rows of a sequence and K/V head), decoding sequences too.  out must not overlap qkv.
- * Errors: NULL, SHAPE (as above, n_seqs in 1 .. 2048, n_seqs * n_kv_heads <= 2^23, max_q, max_kv < 1), UNSUPPORTED (dtype), ALIGN, DEVICE. */
-lpq_status lpq_paged_attention(const void *qkv, const lpq_attn_cfg *cfg, const lpq_page_pool *pool, const void *k_pages, const void *v_pages,
-                               const float *alibi_slopes, const int32_t *cu_q, const int32_t *kv_lens, int32_t n_seqs, int32_t M,
-                               int32_t max_q, int32_t max_kv, void *out, void *hip_stream);
-
-/* Causal attention of whole prompts over themselves: the same with keys and values read from the packed rows, no cache.
- * Errors: as lpq_paged_attention. */
-lpq_status lpq_packed_attention(const void *qkv, const lpq_attn_cfg *cfg, const float *alibi_slopes, const int32_t *cu_q, int32_t n_seqs,
-                                int32_t M, int32_t max_q, void *out, void *hip_stream);
-
-/* ---- 4-bit paged caches: norms and rotation of q and k, quantising append, its inverse, attention ----------------
- * The same pools, tables, plans and slots as above, with pages of cells: K and V of a position and K/V head are quantised by themselves, d codes of 4 bits, a scale
- * and a zero, 68 bytes where 16-bit elements of a 128-wide head take 256.  k_pages, v_pages are [n_pages][n_kv_heads][page_size / 16] groups of 16 positions:
- *   16 * head_dim / 2 bytes   codes of the positions in order, eight features to a little-endian u32: code e at bit 4 * (e / 2) + 16 * (e % 2)
- *   16 * 4 bytes              scale and zero of the positions, 16-bit numbers of the rows' type
- * and a code c stands for scale * c + zero.  Of x, the head_dim values of a head (the quantiser of lpq_quantize_pack, fp32 IEEE arithmetic, round-half-even):
- *   scale = type((max - min) / 15), a last place less if 15 * scale + zero would round to infinity;   zero = min (+0 for -0);
- *   code = clamp(rint((x - zero) / scale), 0, 15), 0 where scale is 0
- * A head with an infinity or NaN in it, or with max - min beyond the type's range, is stored as NaN throughout.
- * A layer's step is lpq_qk_norm_rotary (where the model has it), lpq_paged_append4, lpq_paged_attention4. */
-
-/* Bytes of one K/V head's part of a page: page_size / 16 * 16 * (head_dim / 2 + 4); 0 if either is not supported.  Host-only. */
-size_t lpq_cell_page_bytes(int32_t page_size, int32_t head_dim);
-
-typedef enum { LPQ_PAIRS_HALVES = 0,     /* features i and i + rotary_dim / 2 are a pair */
-               LPQ_PAIRS_ADJACENT = 1    /* features 2 i and 2 i + 1                     */
-} lpq_pairs;
-
-/* Norms and rotation of q and k.  With gammas: x <- x / sqrt(mean(x^2) + eps) * gamma for each head of q (k); then the first rotary_dim features of
- * each head, pair i of a row at position p: (a, b) <- (a cos - b sin, b cos + a sin), cosines and sines of angle i from row p of the table. */
-typedef struct {
-    int32_t rotary_dim;              /* % 16 == 0, 0 (no rotation) .. head_dim                             */
-    int32_t pairs;                   /* lpq_pairs                                                          */
-    int32_t max_pos;                 /* rows of the table                                                  */
-    float eps;                       /* > 0 where a gamma is given                                         */
-    const float *cos_sin;            /* device fp32 [max_pos][rotary_dim]: rotary_dim / 2 cosines, then as many sines */
-    const void *q_gamma, *k_gamma;   /* device [head_dim] of the rows' type, or NULL: no norm of q (k)     */
-} lpq_rotary;
-
-/* q and k parts of the rows of qkv ([M][(n_heads + 2 * n_kv_heads) * head_dim]) to out: qkv itself (V parts are not touched) or another buffer of that shape that does not
- * overlap it (V parts are copied).  positions: int32 [M] (a plan's; may be NULL without rotation).  Rows with a negative entry in slots (a plan's; NULL: no such rows), or at
- * a position that the table has no row for, are left as they were in out.  Computed in fp32, rounded once.
- * Errors: NULL, SHAPE (heads, rotary_dim, max_pos, eps, buffers that overlap; M * n_heads <= 2^27), UNSUPPORTED (dtype, pairs), ALIGN (table and gammas 16 bytes), DEVICE. */
-lpq_status lpq_qk_norm_rotary(const void* qkv, const lpq_attn_cfg* cfg, const lpq_rotary* rotary, const int32_t* positions, const int32_t* slots, int32_t M,
-                              void* out, void* hip_stream);
-
-/* K and V parts of each row of qkv quantised into its slot.  Slots as in lpq_paged_append: rows whose slot is negative or behind the pool are skipped; where two rows
- * name the same one it ends up with words of either.  Errors: as lpq_paged_append. */
-lpq_status lpq_paged_append4(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, void* k_pages, void* v_pages, const int32_t* slots,
-                             int32_t M, void* hip_stream);
-
-/* The inverse: what the slots hold, rounded once to the type, to the K and V parts of the rows of qkv; q parts, and rows without a slot in the pool, are left as they
- * were.  Slots may repeat.  For contexts that move to another pool, and for prompts whose lpq_packed_attention shall see what later steps will.
- * Errors: as lpq_paged_append. */
-lpq_status lpq_paged_load4(const void* k_pages, const void* v_pages, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const int32_t* slots, int32_t M,
-                           void* qkv, void* hip_stream);
-
-/* lpq_paged_attention over pages of cells, with the same arguments, masks and limits.  A position that is stored as NaN makes the rows that see it NaN.  Products are of
- * 16-bit floats with 11 bits, sums of 32 bits.  Where a sequence and K/V head have up to 32 rows, codes are multiplied as they are: rounded are the query's elements
- * 2^-24 of the largest and smaller, and weights times V's scales.  With more rows, values of cells and weights are rounded (bf16: tiles of values without their power of two).
  * Partial results are kept in the library's workspace, up to 290 MiB of them.  A smaller reservation splits less: tiles of chunks and prompts first, then, below 34 MiB,
  * decoding sequences too.
  * Errors: as lpq_paged_attention. */
