@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void mixed_attention_kernel(AttnArgs stream
 
 // Room that the tile kernel's parts may take: its list has a place for each sequence, also for those that the streaming kernel does.
 constexpr size_t MAX_PART_BYTES = (size_t)256 << 20;
-constexpr int FEW_STEPS = 8, SHORT_WALK = 4096;        // steps of a worker, positions: see below
+constexpr int FEW_STEPS = 8, SHORT_WALK = 2048;        // steps of a worker, positions: see below
 
 // What a call launches: the streaming kernel, the tile kernel or, where a batch may have sequences of both kinds, both, in one launch if column tiles are single.
 AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int n_seqs, int M, int max_q, int max_kv, int cus)
@@ -351,16 +351,16 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int 
     const int64_t most = (int64_t)std::min(max_q, M) * group;
     // Rows of the streaming kernel's tiles: those to expect where it is alone, else those of a decoding sequence; from 4 on for cells.  Two tiles of 8 rows for 9 to 16 where walks are
     // short and a worker has few steps of them: cells read twice cost less there than a softmax that idle columns share saves.  One tile of 16 / two of 8, us: 16 sequences of 400 to 700
-    // positions, 80 heads (5 K/V heads) 20.4 / 17.0; 24, 64 (8), two tokens, up to 700 20.5 / 18.4; 24, 40 (8), three tokens, up to 2600 26.6 / 24.8, up to 9000 36.7 / 39.6; 8 such up
+    // positions, 80 heads (5 K/V heads) 20.4 / 17.0; 24, 64 (8), two tokens, up to 700 20.5 / 18.4; 24, 40 (8), three tokens, up to 2600 26.4 / 24.3, up to 4000 28.5 / 29.0, up to 9000 36.7 / 39.6; 8 such up to 4000 26.8 / 27.7, up
     // to 8000 31.2 / 34.7; one of 90001, 112 (8) 37.8 / 43.9.
     auto tile_of_rows = [&](int64_t rows, int smallest) { return rows <= 4 && smallest <= 4 ? 4 : rows <= 8 && smallest <= 8 ? 8 : rows <= STREAM_ROWS ? STREAM_ROWS : 2 * STREAM_ROWS; };
     const int smallest = source == SRC_CELLS ? 4 : STREAM_ROWS;
     p.stream_tile = 0;
     if (paged && most <= 2 * STREAM_ROWS) p.stream_tile = tile_of_rows(most, smallest);
-    const int64_t steps = (int64_t)n_seqs * c.n_kv_heads * (((int64_t)max_kv + STREAM_KEYS - 1) / STREAM_KEYS);
-    if (source == SRC_CELLS && p.stream_tile == STREAM_ROWS && max_kv <= SHORT_WALK && steps < (int64_t)FEW_STEPS * 4 * cus * CELL_WAVES) p.stream_tile = 8;
     else if (paged && n_seqs > 1 && group <= 2 * STREAM_ROWS) p.stream_tile = tile_of_rows(group, std::max(smallest, 8));
     p.tile = !(paged && most <= 2 * STREAM_ROWS);
+    const int64_t steps = (int64_t)n_seqs * c.n_kv_heads * (((int64_t)max_kv + STREAM_KEYS - 1) / STREAM_KEYS);
+    if (source == SRC_CELLS && !p.tile && p.stream_tile == STREAM_ROWS && max_kv <= SHORT_WALK && steps < (int64_t)FEW_STEPS * 4 * cus * CELL_WAVES) p.stream_tile = 8;
     p.workers = 4 * cus * (source == SRC_CELLS && p.stream_tile <= STREAM_ROWS && !p.tile ? CELL_WAVES : STREAM_WAVES);
     p.tiles = (int)tile_bound(M, group, n_seqs, TILE_ROWS_Q);
     p.splits = 1;
