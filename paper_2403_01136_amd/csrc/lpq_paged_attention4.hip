@@ -334,7 +334,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     for (int k = 0; k < N; ++k) {
                         pw[k] = __builtin_amdgcn_exp2f(sc[t][k] - ms);
                         ts[k] = pw[k] * param_scale<DT>(par[k]);
-                        tm = fmaxf(tm, ts[k]);
+                        tm = fmaxf(tm, __builtin_fabsf(ts[k]));
                     }
                 };
                 weights();

@@ -281,11 +281,11 @@ def attention_ref(q, cells, ok, pos, slopes, tile, dt):
         qh = q[:, h].double()
         s = (qh @ kh.t().contiguous()) / math.sqrt(d)
         size = qh.abs().sum(1, keepdim=True) / math.sqrt(d)                      # sum |q_i|
-        err = (d + 8) * 2.0**-24 * size * (15 * sk + zk.abs())[None, :]
+        err = (d + 8) * 2.0**-24 * size * (15 * sk.abs() + zk.abs())[None, :]
         if tile and dt == "bf16":
-            err = err + U16 * (qh.abs() @ kh.abs().t().contiguous()) / math.sqrt(d) + 2.0**-24 * size * torch.maximum(15 * sk, zk.abs()).amax()
+            err = err + U16 * (qh.abs() @ kh.abs().t().contiguous()) / math.sqrt(d) + 2.0**-24 * size * torch.maximum(15 * sk.abs(), zk.abs()).amax()
         else:
-            err = err + 2.0**-18 * size * sk[None, :]
+            err = err + 2.0**-18 * size * sk.abs()[None, :]
         if slopes is not None:
             s = s + float(slopes[h]) * dist
             err = err + 2.0**-24 * (float(slopes[h]) * dist).abs()
@@ -300,11 +300,11 @@ def attention_ref(q, cells, ok, pos, slopes, tile, dt):
         out[:, h] = o
         A, n = w @ vh.abs(), L
         arg = err * lg + 3 * 2.0**-24 * (fin(s).abs() + fin(top).abs()) * lg
-        e = 2 * (math.log(2) * torch.where(vis, arg, none).amax(1, keepdim=True) + 2.0**-22) * A + 2 * n * 2.0**-24 * (w @ (15 * sv + zv.abs()))[:, None]
+        e = 2 * (math.log(2) * torch.where(vis, arg, none).amax(1, keepdim=True) + 2.0**-22) * A + 2 * n * 2.0**-24 * (w @ (15 * sv.abs() + zv.abs()))[:, None]
         if tile:
-            e = e + U16 * A + 2.0**-24 * torch.maximum(15 * sv, zv.abs()).amax() + U16 * (A + fin(o).abs()) + n * 2.0**-25 * vh.abs().amax()
+            e = e + U16 * A + 2.0**-24 * torch.maximum(15 * sv.abs(), zv.abs()).amax() + U16 * (A + fin(o).abs()) + n * 2.0**-25 * vh.abs().amax()
         else:
-            e = e + (2.0**-18 * (w @ sv) + 8 * n * 2.0**-37 * (w * sv[None, :]).amax(1))[:, None] + U16 * (w @ (sv[:, None] * (cv - 8).abs()))
+            e = e + (2.0**-18 * (w @ sv.abs()) + 8 * n * 2.0**-37 * (w * sv.abs()[None, :]).amax(1))[:, None] + U16 * (w @ (sv[:, None] * (cv - 8)).abs())
         E[:, h] = e
     return out, E
 
@@ -538,6 +538,18 @@ def test_scales_of_many_sizes(spread, dt):
         p = Cells(seqs, 8, 2, 128, 32, dt, spread=spread)
         p.qkv[:, :8 * 128] *= 2.0**-spread
         check_attention(*p.run(max_q=max_q), what="spread")
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_negative_scales(dt):
+    """The append makes none, but cells from elsewhere may have them: c -> -|s| c + z is a number like any other.  The bounds go by |s|."""
+    for seqs, max_q in (([(700, 1), (90, 1)], 1), ([(2000, 3)], 3), ([(500, 60)], 60), ([(300, 200), (1000, 1)], 200)):
+        p = Cells(seqs, 8, 2, 128, 32, dt)
+        p.param *= 2000.0 if dt == "fp16" else 1e6
+        p.param[..., ::2, :] *= -1
+        p.qkv[:, :8 * 128] /= 2000.0 if dt == "fp16" else 1e6
+        p.write()
+        check_attention(*p.run(max_q=max_q), what="negative")
 
 
 @pytest.mark.parametrize("k_size,v_size", [(1e-6, 1e-9), (1e9, 1e12), (1.0, 1e-30), (1e-20, 1e30)])
