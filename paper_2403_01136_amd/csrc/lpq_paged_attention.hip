@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void mixed_attention_kernel(AttnArgs stream
 
 // Room that the tile kernel's parts may take: its list has a place for each sequence, also for those that the streaming kernel does.
 constexpr size_t MAX_PART_BYTES = (size_t)256 << 20;
-constexpr int FEW_STEPS = 8, SHORT_WALK = 2048;        // steps of a worker, positions: see below
+constexpr int FEW_STEPS = 8, SHORT_WALK = 2048, WHOLE_WALK = 192;        // steps of a worker, positions: see below
 
 // What a call launches: the streaming kernel, the tile kernel or, where a batch may have sequences of both kinds, both, in one launch if column tiles are single.
 AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int n_seqs, int M, int max_q, int max_kv, int cus)
@@ -377,7 +377,10 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int 
         p.key_tiles = (int)key_tiles;
     }
     const size_t d2 = (size_t)c.head_dim + 2;
-    if (p.stream_tile) p.stream_floats = (size_t)p.workers * (2 * p.stream_tile * d2 + sizeof(Cut) / sizeof(float));
+    // Cells of short walks are left whole, without a second launch.  Split / whole, us on the device, for 3 sequences of 64-wide heads, 16 of 40 heads, 61 of 64 (8 K/V heads), 24 drafts: up to
+    // 128 positions 8.4 / 6.5, 11.9 / 9.9, 14.7 / 10.8, 15.5 / 13.8, 160 to 190 8.6 / 8.2, 13.6 / 12.9, 16.7 / 11.3, 17.9 / 15.6, up to 256 8.7 / 9.3, 13.3 / 13.7, 17.0 / 14.8, 17.9 / 19.1.
+    const bool whole = source == SRC_CELLS && !p.tile && max_kv <= WHOLE_WALK;
+    if (p.stream_tile && !whole) p.stream_floats = (size_t)p.workers * (2 * p.stream_tile * d2 + sizeof(Cut) / sizeof(float));
     // lists of 32 parts and more, where the walks are long enough to be cut that often (4 sequences of up to 800 positions: long lists' form 7.2 us, the other's 4.0)
     p.long_lists = (int64_t)n_seqs * c.n_kv_heads * 32 <= p.workers && max_kv >= 64 * STREAM_KEYS;
     p.stream_rows = (int)std::min<int64_t>(p.stream_tile, p.tile ? 2 * STREAM_ROWS : most);

@@ -426,6 +426,16 @@ def test_hints_do_not_change_the_result(hints):
     check_attention(*p.run(max_q=hints[0], max_kv=hints[1], loose=True), what=str(hints))
 
 
+@pytest.mark.parametrize("alibi", [False, True], ids=["plain", "alibi"])
+@pytest.mark.parametrize("q,H,KV,d,dt", [(1, 12, 12, 64, "fp16"), (1, 40, 40, 128, "bf16"), (1, 64, 8, 128, "fp16"), (3, 8, 2, 64, "bf16"), (5, 10, 2, 128, "bf16"), (16, 2, 1, 128, "fp16")])
+def test_whole_walks(q, H, KV, d, dt, alibi):
+    """Contexts that the caller says are short are not split, also where one is longer than that."""
+    r = random.Random(q + H)
+    seqs = [(r.randrange(192 - q), q) for _ in range(7)] + [(0, q), (192 - q, q)]
+    check_attention(*Cells(seqs, H, KV, d, 32, dt, 2).run(alibi, max_q=q, max_kv=192), what="whole")
+    check_attention(*Cells(seqs + [(1500, q)], H, KV, d, 32, dt, 2).run(alibi, max_q=q, max_kv=192), what="one longer")
+
+
 @pytest.mark.parametrize("n", [64, 65, 257, 2048])
 def test_many_sequences(n):
     r = random.Random(n)
