@@ -117,9 +117,10 @@ template <int D> __device__ __forceinline__ size_t group_of(const CellArgs& a, c
 // Codes and parameters of a head of which this lane has 16 features:
 //     scale = type((max - min) / 15), a last place less if 15 scales above zero would round to infinity;  zero = min;
 //     code = clamp(rint((x - zero) / scale), 0, 15), 0 where scale is
-// with quotients rounded to fp32.  No division: a product with the reciprocal, refined once, gives f = floor(quotient), or one off next to a whole number, and the sign of
-// d = (x - zero) - (f + 1/2) scale, exact in one FMA as f + 1/2 has five bits and a scale eleven, says which side of the half the quotient is on (one off, d says so as well); d = 0 is
-// the tie, frequent where x has eight bits.  Only a quotient that is not a tie but rounds to one needs more: |d| <= 2^-20 scale, then the wave divides.
+// with quotients rounded to fp32, made without a division: of q = a / s, q0 = a rcp(s) is off by 1.5 2^-23 of it at most, the remainder a - q0 s is exact in one FMA (s has eleven bits),
+// and q0 + remainder * rcp(s) before its rounding by 2^-45 of q.  That rounds as the quotient does: where a rounds differently above than below, a / s is half way between two fp32
+// numbers, a number m of 25 bits; a - m s, of numbers of 24 and 36 bits, is zero or 2^-37 of a at least, and zero it is not, as m s has more than 24 bits.  Scales below 2^-100, where
+// the remainder may be too small for an exponent, divide.
 // A head with an infinity or a NaN in it, or a range beyond the type's, is NaN throughout.
 template <int DT, int LANES>
 __device__ __forceinline__ u32x2 quantise_head(const u32x4 (&x)[2], uint32_t* param)
@@ -148,21 +149,18 @@ __device__ __forceinline__ u32x2 quantise_head(const u32x4 (&x)[2], uint32_t* pa
     const bool odd = (bad_lanes >> (threadIdx.x & 63 & -LANES) & ((1ull << LANES) - 1)) != 0 || !__builtin_isfinite((float)scale);
     if (!odd && __builtin_isinf((float)(T)__builtin_fmaf(15.0f, (float)scale, z))) --sb;
     const float s = (float)__builtin_bit_cast(T, sb);
-    float rcp = __builtin_amdgcn_rcpf(s), r[N];
-    rcp = __builtin_fmaf(__builtin_fmaf(-s, rcp, 1.0f), rcp, rcp);
-    const float per_unit = rcp * 0x1p20f;
-    uint32_t least = 0xffffffffu;                      // of |d|, where it is not zero: its bits doubled, less two
+    const float rcp = __builtin_amdgcn_rcpf(s);
+    float r[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        const float num = __fsub_rn(v[e], z), b = __builtin_floorf(__fmul_rn(num, rcp)) + 0.5f, d = __builtin_fmaf(-b, s, num);
-        least = min(least, 2u * __builtin_bit_cast(uint32_t, d) - 2u);
-        r[e] = __builtin_rintf(b + __builtin_amdgcn_fmed3f(d * per_unit, -0.25f, 0.25f));
+        const float a = __fsub_rn(v[e], z), q0 = __fmul_rn(a, rcp);
+        r[e] = __builtin_fmaf(__builtin_fmaf(-q0, s, a), rcp, q0);
     }
-    if (__any(least <= 2u * __builtin_bit_cast(uint32_t, s * 0x1p-20f) || !(s >= 0x1p-100f && s <= 0x1p100f)))
+    if (__any(s > 0.0f && s < 0x1p-100f))
 #pragma unroll
-        for (int e = 0; e < N; ++e) r[e] = __builtin_rintf(__fdiv_rn(__fsub_rn(v[e], z), s));
+        for (int e = 0; e < N; ++e) r[e] = __fdiv_rn(__fsub_rn(v[e], z), s);
 #pragma unroll
-    for (int e = 0; e < N; ++e) r[e] = __builtin_amdgcn_fmed3f(r[e], 0.0f, 15.0f);
+    for (int e = 0; e < N; ++e) r[e] = __builtin_rintf(__builtin_amdgcn_fmed3f(r[e], 0.0f, 15.0f));
     // code e at bit 4 (e / 2) of its half: sums below 2^16, exact
     auto half = [&](int e) { return (uint32_t)__builtin_fmaf(r[e + 6], 4096.0f, __builtin_fmaf(r[e + 4], 256.0f, __builtin_fmaf(r[e + 2], 16.0f, r[e]))); };
     constexpr uint32_t NOT_A_NUMBER = DT == LPQ_DT_FP16 ? 0x7e007e00u : 0x7fc07fc0u;
@@ -171,7 +169,8 @@ __device__ __forceinline__ u32x2 quantise_head(const u32x4 (&x)[2], uint32_t* pa
 }
 
 // Bound by the memory, of which its reads are most (256 bytes of a row and head at D = 128); what it writes lies in the order of positions, so 16 rows of a head are neighbours here:
-// a group's codes and parameters are whole lines of one XCD's L2.  7246 rows of 8 heads: row by row, eight features a thread and IEEE divisions near halves, 14.4 us; 16 features, no divisions 12.8; so 12.6.
+// a group's codes and parameters are whole lines of one XCD's L2.  7246 rows of 8 heads: row by row, eight features a thread and IEEE divisions near halves, 14.4 us; 16 features, no divisions 12.8; so 12.6; quotients by a remainder instead of
+// whole numbers and a test of doubt 10.6 (3.5 TB/s read and written).
 constexpr int APPEND_TOGETHER = 16;
 template <int DT, int D>
 __global__ __launch_bounds__(256) void paged_append4_kernel(CellArgs a)

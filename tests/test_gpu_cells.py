@@ -159,6 +159,32 @@ def test_append_and_load_bit_exact(H, KV, d, P, M, dt):
         assert torch.equal(again[:, H * d:].contiguous().view(torch.int16), out[1:2, H * d:].expand(M, -1).contiguous().view(torch.int16))
 
 
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("size", [1.0, 2.0**-9, 2.0**9])
+def test_append_next_to_halves(dt, size):
+    """Elements half way between two codes, and the numbers of the type next to that, over every kind of scale and over zeros on either side."""
+    M, KV, d, P = 96, 8, 64, 16
+    rng = np.random.default_rng(3)
+    scale = of_bits(to_bits((1 + rng.random((M * 2 * KV, 1))) * size, dt), dt).astype(np.float64)
+    zero = np.where(rng.random(scale.shape) < 0.5, 0.0, of_bits(to_bits(scale * rng.integers(-16, 3, scale.shape), dt), dt))
+    x = of_bits(to_bits(zero + scale * (rng.integers(0, 15, (len(scale), d)) + 0.5), dt), dt).copy()
+    bits = to_bits(x, dt).astype(np.int32) + rng.integers(-1, 2, x.shape)
+    x = np.where(x != 0, of_bits(bits.astype(np.uint16), dt), x)
+    x[:, 3:4], x[:, 40:41] = zero, of_bits(to_bits(zero + 15 * scale, dt), dt)
+    x = x.reshape(M, 2 * KV * d)
+    row = np.concatenate([np.zeros((M, KV * d), np.float32), x.astype(np.float32)], 1)
+    import torch
+    k, v = (torch.zeros((M // P, KV, lpq.lpq_cell_page_bytes(P, d)), dtype=torch.uint8, device="cuda") for _ in range(2))
+    lpq.lpq_paged_append4(from_bits(to_bits(row, dt), dt).view(M, -1), k, v, ints(list(range(M))))
+    for i, pages in enumerate((k.cpu().numpy(), v.cpu().numpy())):
+        for r in range(M):
+            for h in range(KV):
+                codes, sb, zb = quantise(x[r, (i * KV + h) * d:(i * KV + h + 1) * d].astype(np.float32), dt)
+                cells, param = head_of(pages, r // P, h, d)[r % P]
+                want = cell_bytes(codes, sb, zb)
+                assert np.array_equal(cells, want[0]) and np.array_equal(param, want[1]), (r, h)
+
+
 # ---- norms and rotation ------------------------------------------------------------------------------------------------
 
 def rotary_table(max_pos, rd, seed=0):
