@@ -377,7 +377,7 @@ def _check_tensor(name, t, dtype, dims, dev):
 
 def _vector(name, t, dtype, size, dev):
     """Address of a contiguous vector of `size` elements."""
-    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != size or t.get_device() != dev or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != size or t.dim() != 1 or t.get_device() != dev or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of %d elements on CUDA device %d" % (name, dtype, size, dev))
     return t.data_ptr()
 
@@ -404,18 +404,18 @@ def _new_tensors(make, stream, dev):
 
 
 def _attn_cfg(qkv, n_heads, n_kv_heads):
-    import torch
-    if qkv.dtype is not torch.float16 and qkv.dtype is not torch.bfloat16:
-        raise ValueError("qkv must be fp16 or bf16")
-    return _attn_cfg_of(qkv.shape[1], n_heads, n_kv_heads, LPQ_DT_FP16 if qkv.dtype is torch.float16 else LPQ_DT_BF16)
+    return _attn_cfg_of(qkv.shape[1], n_heads, n_kv_heads, qkv.dtype)
 
 
 @functools.lru_cache(maxsize=256)
 def _attn_cfg_of(cols, n_heads, n_kv_heads, dtype):
+    import torch
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise ValueError("qkv must be fp16 or bf16")
     heads = n_heads + 2 * n_kv_heads
     if n_heads < 1 or n_kv_heads < 1 or cols % heads:
         raise ValueError("qkv has %d columns, not a multiple of %d heads" % (cols, heads))
-    return lpq_attn_cfg(n_heads, n_kv_heads, cols // heads, dtype)
+    return lpq_attn_cfg(n_heads, n_kv_heads, cols // heads, LPQ_DT_FP16 if dtype is torch.float16 else LPQ_DT_BF16)
 
 
 def _paged_cfg(qkv, k_pages, v_pages):
@@ -565,7 +565,8 @@ def lpq_qk_norm_rotary(qkv, positions, n_heads, n_kv_heads, cos_sin=None, interl
     import torch
     i32, dtype, dev = torch.int32, qkv.dtype, _device_of(qkv)
     _check_tensor("qkv", qkv, dtype, 2, dev)
-    cfg, M = _attn_cfg(qkv, n_heads, n_kv_heads), qkv.shape[0]
+    M, cols = shape = qkv.shape
+    cfg = _attn_cfg_of(cols, n_heads, n_kv_heads, dtype)
     at = left = q_norm = k_norm = table = None
     rotary_dim = max_pos = 0
     if positions is not None:
@@ -584,7 +585,7 @@ def lpq_qk_norm_rotary(qkv, positions, n_heads, n_kv_heads, cos_sin=None, interl
         out = qkv
     elif out is not qkv:
         _check_tensor("out", out, dtype, 2, dev)
-        if out.shape != qkv.shape:
+        if out.shape != shape:
             raise ValueError("out must have qkv's shape")
     r = lpq_rotary(rotary_dim, LPQ_PAIRS_ADJACENT if interleaved else LPQ_PAIRS_HALVES, max_pos, eps, table, q_norm, k_norm)
     _check(load_library().lpq_qk_norm_rotary(qkv.data_ptr(), cfg, r, at, left, M, out.data_ptr(), _stream_on(stream, dev)), "lpq_qk_norm_rotary")
