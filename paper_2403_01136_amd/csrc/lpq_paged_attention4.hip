@@ -20,14 +20,19 @@ namespace lpq {
 namespace {
 
 // ---- streaming kernel -----------------------------------------------------------------------------
-// Bound by the memory: D + 8 bytes per key and K/V head.  Workers are single waves with equal shares of the list of 32-key units.
+// Bound by the memory while it streams, D + 8 bytes per key and K/V head; by starts and ends of walks where they are short.  Workers are single waves, two a SIMD (the 32-row tile, with
+// its registers, one), with equal shares of the list of 32-key steps; the loads of one step are under way while the step before is computed.  61 sequences of 100 to 7000 positions, 64 heads (8 K/V heads),
+// bf16, 29.6 us and 4.9 for the parts (112 MB; 3.8 TB/s, with some 8 us of start and end in it); one of 90001, 56 heads (8), fp16 25.0 and 5.0; 16 of 400 to 700, 40 heads 14.2 and 3.9; one wave
+// a SIMD 62 for the first, three 41.
 // Products on 16x16x32, columns = rows of the problem:
-//   S^T = C_k . Q^T  lane (i = lane % 16, q = lane / 16) holds codes D / 4 q .. of key i as they lie; a word has pairs 0 and 2 at 2^-24, 1 and 3 at 2^-20, which go to a
-//                    product each, with the query's pairs in that order.  Register r of the result: key 4 q + r, column i.
+//   S^T = C_k . Q^T  lane (i = lane % 16, q = lane / 16) holds codes D / 4 q .. of key i as they lie; a word makes an operand of four pairs, of neighbours, as the query's row has them.
+//                    Register r of the result: key 4 q + r, column i.
 //   O^T = C_v^T . P^T over 32 keys: quarter q contracts over its own keys {4 q + 0..3, 16 + 4 q + 0..3}.  A lane has a word (D = 128; half a word, D = 64) of each of the
-//                    eight; halves of two keys' words are put side by side, and an AND gives a pair of keys of one feature.
+//                    eight; halves of two keys' words are put side by side, and what makes pairs of a word's neighbours makes a pair of keys of one feature.
+// A tile of 4 or 8 rows has its columns four times or twice: each copy scores all keys and does the softmax of its part of them (16 columns doing all of it: 50.9 us for the first case where this
+// took 47.1, both before other steps).
 // Weights: P = exp2(score - m), its sum and its sum with the zeros in fp32; t = P s' is taken by a power of two G for each column so that the largest so far is below 2^15.
-// Both m and G are renewed only where t G passes 2^15: one maximum a step decides (P may be up to 2^60).
+// Both m and G are renewed only where t G passes 2^15: one maximum a step decides (P may be up to 2^60).  Renewed, the largest is 2^12 to 2^13 (2^8, 2^10, 2^14: 24 drafts 29.7, 29.6, 31.2 us for 30.4).
 constexpr float LARGEST_T = 0x1p15f, NEW_T = 0x1p12f, RENEW_T = 0x1p60f;
 
 // v <- op(v, v of the lanes that have the same row): the four quarters, and where a tile has 8 or 4 rows the columns that are 8 or 4 apart.
@@ -42,7 +47,7 @@ __device__ __forceinline__ float over_row(float v, Op op)
 }
 
 // ---- the list: walks (sequence, K/V head, row tile) of 32-key steps, with WALK_COST units ahead of each for what its start and end take; a share's worker needs no
-// other wave to find it.  Lanes have 64 sequences side by side.
+// other wave to find it (0, 3, 6 units: 61 sequences 42.8, 36.8, 37.1 us, 24 drafts 35.2, 30.7, 29.8).  Lanes have 64 sequences side by side.
 constexpr int WALK_COST = 3;
 __device__ __forceinline__ int64_t read_lane64(int64_t v, int lane)
 {
@@ -378,7 +383,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     operand[k] = PARTS == 1 || part == k / (N / 2) ? pk[k % (N / 2)] : FINE && (PARTS == 2 || rest_of == k / (N / 2)) ? rk[k % (N / 2)] : 0u;
                 pf[t] = __builtin_bit_cast(h8, operand);
             }
-            // V^T operands: halves of two keys' words side by side, then pairs by AND
+            // V^T operands: halves of two keys' words side by side, then pairs
 #pragma unroll
             for (int half = 0; half < W / 2; ++half) { // D = 128: even, odd features; D = 64: the lane has a half of a word only
                 u32x4 pair[4];                         // [keys][e]: feature 2 e + half of the word
