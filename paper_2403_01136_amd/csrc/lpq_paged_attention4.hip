@@ -32,8 +32,10 @@ namespace {
 // A tile of 4 or 8 rows has its columns four times or twice: each copy scores all keys and does the softmax of its part of them (16 columns doing all of it: 50.9 us for the first case where this
 // took 47.1, both before other steps).
 // Weights: P = exp2(score - m), its sum and its sum with the zeros in fp32; t = P s' is taken by a power of two G for each column so that the largest so far is below 2^15.
-// Both m and G are renewed only where t G passes 2^15: one maximum a step decides (P may be up to 2^60).  Renewed, the largest is 2^12 to 2^13 (2^8, 2^10, 2^14: 24 drafts 29.7, 29.6, 31.2 us for 30.4).
-constexpr float LARGEST_T = 0x1p15f, NEW_T = 0x1p12f, RENEW_T = 0x1p60f;
+// G is renewed where t G passes 2^15, to a largest of 2^12 to 2^13 (2^8, 2^10, 2^14: 24 drafts 29.7, 29.6, 31.2 us for 30.4).  m is renewed where t passes 2^60, or the sum of a lane's P of a step
+// 2^40: t alone says nothing of P where s' is zero (a flat head) or tiny.  That sum is made for l anyway.  Sums of P and of P z' are then in range for z' up to 2^64 and 2^23 keys.
+// (2^24, 2^40, 2^60 and nothing asked: 24 drafts with biases 34.4, 33.8, 33.5, 33.3 us; without biases 30.3 to 30.5, 30.1.)
+constexpr float LARGEST_T = 0x1p15f, NEW_T = 0x1p12f, RENEW_T = 0x1p60f, RENEW_P = 0x1p40f;
 
 // v <- op(v, v of the lanes that have the same row): the four quarters, and where a tile has 8 or 4 rows the columns that are 8 or 4 apart.
 template <int ROWS, typename Op>
@@ -331,21 +333,23 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                         sc[t][k] = hidden ? -INFINITY : sc[t][k];
                         par[k] = hidden ? 0u : par[k];
                     }
-                float pw[N], ts[N], tm = 0.0f;
+                float pw[N], ts[N], tm = 0.0f, sum = 0.0f;
                 auto weights = [&] {
                     const float ms = m[t] == -INFINITY ? 0.0f : m[t];
-                    tm = 0.0f;
+                    tm = sum = 0.0f;
 #pragma unroll
                     for (int k = 0; k < N; ++k) {
                         pw[k] = __builtin_amdgcn_exp2f(sc[t][k] - ms);
                         ts[k] = pw[k] * param_scale<DT>(par[k]);
                         tm = fmaxf(tm, __builtin_fabsf(ts[k]));
                     }
+#pragma unroll
+                    for (int k = 0; k < N; k += 2) sum += pw[k] + pw[k + 1];
                 };
                 weights();
-                if (__any(m[t] == -INFINITY || !(tm * G[t] < LARGEST_T))) {
+                if (__any(m[t] == -INFINITY || !(tm * G[t] < LARGEST_T) || !(sum < RENEW_P))) {
                     float alpha = 1.0f;
-                    if (__any(m[t] == -INFINITY || !(tm < RENEW_T))) {
+                    if (__any(m[t] == -INFINITY || !(tm < RENEW_T) || !(sum < RENEW_P))) {
                         float mx = -INFINITY;
 #pragma unroll
                         for (int k = 0; k < N; ++k) mx = fmaxf(mx, sc[t][k]);
@@ -364,11 +368,11 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     for (int f = 0; f < F; ++f) o[t][f] *= by;
                     G[t] = g;
                 }
+                l[t] += sum;
                 uint32_t pk[N / 2], rk[N / 2];
 #pragma unroll
                 for (int k = 0; k < N; k += 2) {
                     const float t0 = ts[k] * G[t], t1 = ts[k + 1] * G[t];
-                    l[t] += pw[k] + pw[k + 1];
                     zs[t] = __builtin_fmaf(pw[k], param_zero<DT>(par[k]), zs[t]);
                     zs[t] = __builtin_fmaf(pw[k + 1], param_zero<DT>(par[k + 1]), zs[t]);
                     pk[k / 2] = Elem<LPQ_DT_FP16>::pack(t0, t1);

@@ -1,0 +1,126 @@
+"""Attention over 4-bit cells where its running quantities can leave their range: values that are flat in a position (a scale of 0), scores that rise far beyond the first
+keys', queries and keys of zero.  Everything against the 64-bit implementation and the bounds of test_gpu_cells.py, whose derivation covers these inputs."""
+import pytest
+
+import paper_2403_01136_amd as lpq
+from test_gpu_cells import Cells, check_attention
+from test_gpu_paged import ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU (no fallback path)"
+    lpq.load_library()
+
+
+# sequences, heads, K/V heads, features, what the caller says of them, and a bias that makes scores rise by more than 128 (base 2) within a share of the work: rows of 4, 8, 16 and 32 to a
+# tile, whole walks, parts of several steps, long lists of parts, both kernels in one launch, the tile kernel
+KINDS = {
+    "whole4": ([(159, 1), (190, 1), (900, 1)], 8, 2, 64, dict(max_q=1, max_kv=192), 0.9),
+    "whole8": ([(150, 2), (500, 2), (20, 1)], 8, 2, 128, dict(max_q=2, max_kv=192), 0.9),
+    "whole16": ([(170, 1), (400, 1)], 16, 1, 64, dict(max_q=1, max_kv=192), 0.9),
+    "whole32": ([(170, 5), (400, 4)], 12, 2, 128, dict(max_q=5, max_kv=192), 0.9),
+    "slow": ([(3000, 1)], 4, 1, 64, dict(max_q=1, max_kv=192), 0.0625),
+    "parts4": ([(1500 + 60 * i, 1) for i in range(24)], 4, 4, 128, dict(max_q=1), 4.0),
+    "parts8": ([(1500 + 61 * i, 2) for i in range(24)], 16, 4, 64, dict(max_q=2), 4.0),
+    "parts16": ([(9000 + i, 1) for i in range(6)], 36, 4, 64, dict(max_q=1), 4.0),
+    "two8": ([(1500 + 10 * i, 1) for i in range(18)], 20, 2, 128, dict(max_q=1, max_kv=1700), 4.0),
+    "parts32": ([(1500 + 50 * i, 5) for i in range(12)], 16, 4, 128, dict(max_q=5), 4.0),
+    "long": ([(40000, 1)] * 2, 8, 4, 64, dict(max_q=1), 1.5),
+    "mixed": ([(2000 + 31 * i, 1) for i in range(12)] + [(300, 40)], 8, 4, 128, dict(max_q=40), 4.0),
+    "mixed16": ([(2000 + 31 * i, 1) for i in range(12)] + [(300, 20)], 40, 4, 64, dict(max_q=20), 4.0),
+    "chunks": ([(500, 150)], 8, 2, 64, dict(max_q=150), 0.9),
+}
+
+
+def kind_of(name, dt):
+    seqs, H, KV, d, hints, slope = KINDS[name]
+    return Cells(seqs, H, KV, d, 32, dt, 1), hints, slope
+
+
+def run(p, slope, hints):
+    """(out, parts) as Cells.run gives them, with the same bias for every head, or none."""
+    import torch
+    out, kv = torch.full((p.M, p.H * p.d), 77.0, dtype=p.qkv.dtype, device="cuda"), [past + n for past, n in p.seqs]
+    slopes = torch.full((p.H,), slope, device="cuda") if slope else None
+    lpq.lpq_paged_attention4(p.qkv, p.k, p.v, ints(p.table), ints(p.cu), ints(kv), alibi_slopes=slopes, out=out, **hints)
+    return out, p.parts(kv, slopes)
+
+
+def positions(p):
+    """[(sequence, position, page, place in the page)] of all that the sequences have."""
+    return [(s, j, p.table[s][j // p.P], j % p.P) for s, (past, n) in enumerate(p.seqs) for j in range(past + n)]
+
+
+def flatten_values(p, which):
+    """Values of the positions that `which` names, of every head: scale 0, as the append stores a flat head."""
+    import torch
+    at = torch.tensor([(page, off) for s, j, page, off in positions(p) if which(s, j)], device="cuda")
+    flat = torch.zeros((p.n_pages, p.P), dtype=torch.bool, device="cuda")
+    flat[at[:, 0], at[:, 1]] = True
+    p.param[1, ..., 0] = torch.where(flat[:, None, :], torch.zeros_like(p.param[1, ..., 0]), p.param[1, ..., 0])
+    p.codes[1] = torch.where(flat[:, None, :, None], torch.zeros_like(p.codes[1]), p.codes[1])
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("value", [0.0, 3.25, None], ids=["zero", "constant", "any"])
+def test_flat_values_under_rising_biases(kind, value, dt):
+    """Every position's values are flat while biases let scores rise by far more than 128 (base 2) over a walk; also one value for all, whose mean it is."""
+    p, hints, slope = kind_of(kind, dt)
+    flatten_values(p, lambda s, j: True)
+    if value is not None:
+        p.param[1, ..., 1] = value
+    p.write()
+    check_attention(*run(p, slope, hints), what="flat")
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("length", [1, 32, 150])
+def test_runs_of_flat_values_between_others(kind, length, dt):
+    p, hints, slope = kind_of(kind, dt)
+    flatten_values(p, lambda s, j: j // length % 2 == (s + j // 1000) % 2)
+    p.write()
+    check_attention(*run(p, slope, hints), what="runs")
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("flat", ["one", "all"])
+def test_one_key_far_above_the_others(kind, flat, dt):
+    """Without biases: a key in the middle whose score is more than 300 (base 2) above all before it, flat or among flat ones, and a higher one later."""
+    import torch
+    p, hints, slope = kind_of(kind, dt)
+    p.qkv[:, :p.H * p.d] = 1.0
+    top = {}
+    for s, (past, n) in enumerate(p.seqs):
+        for i, j in enumerate((2 * past // 3, past - past // 8)):
+            top[s, j] = (page, off) = p.table[s][j // 32], j % 32
+            p.codes[0, page, :, off], p.param[0, page, :, off, 0] = 0, 0.0
+            p.param[0, page, :, off, 1] = 40.0 + 30.0 * i
+    flatten_values(p, lambda s, j: flat == "all" or (s, j) in top)
+    p.write()
+    check_attention(*run(p, 0.0, hints), what="one key")
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("size", [2.0**-70, 2.0**-100])
+def test_tiny_scales_under_rising_biases_in_bf16(kind, size):
+    """Scales so small that weights would pass 32 bits ahead of weights times scales; zeros are ordinary."""
+    p, hints, slope = kind_of(kind, "bf16")
+    p.param[1, ..., 0] *= size
+    p.write()
+    check_attention(*run(p, slope, hints), what="tiny")
+
+
+@pytest.mark.parametrize("q", [1, 5])
+def test_tiny_scales_under_a_slow_rise_in_bf16(q):
+    """A bias so small that many keys have nearly the largest weight: their sum passes 32 bits well ahead of any of them."""
+    p = Cells([(13000, q)], 6, 1, 64, 64, "bf16")
+    p.param[1, ..., 0] *= 2.0**-70
+    p.write()
+    check_attention(*run(p, 0.011, dict(max_q=q, max_kv=192)), what="slow")
