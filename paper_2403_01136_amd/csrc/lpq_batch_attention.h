@@ -737,7 +737,8 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
 #pragma unroll
         for (int k = 0; k < KS; ++k) s[1] = Elem<PT>::mfma32(rb[k], qf[k], k == 0 ? zero : s[1]);
         __builtin_amdgcn_sched_barrier(0);
-        const float ct = SCALED ? __builtin_ldexpf(c, k_ex) : c;
+        // Finite and not zero, whatever the powers of two (a row of zeros over keys of zeros): scores that are masked are -inf times it.  Sums of products are below 2^38.
+        const float ct = SCALED ? __builtin_amdgcn_fmed3f(__builtin_ldexpf(c, k_ex), 0x1p-126f, 0x1.fffffep127f) : c;
         if constexpr (K_CODES)                         // by instructions that take the parameters as they are
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)

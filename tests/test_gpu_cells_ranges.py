@@ -124,3 +124,48 @@ def test_tiny_scales_under_a_slow_rise_in_bf16(q):
     p.param[1, ..., 0] *= 2.0**-70
     p.write()
     check_attention(*run(p, 0.011, dict(max_q=q, max_kv=192)), what="slow")
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("seqs,H,KV,d", [([(0, 100)], 4, 4, 64), ([(0, 64), (70, 130), (128, 1)], 8, 2, 128), ([(700, 50), (9, 3)], 8, 2, 64), ([(4000, 90)], 4, 1, 128), ([(300, 5), (60, 1)], 4, 2, 64)],
+                         ids=lambda v: "_".join("%d+%d" % x for x in v) if isinstance(v, list) else str(v))
+@pytest.mark.parametrize("what", ["both", "queries", "keys", "a head", "a row and its keys", "tiny", "large and tiny"])
+def test_queries_and_keys_of_zero(what, seqs, H, KV, d, biases, dt):
+    """Scores of zero, or next to it, under the causal mask and behind the last key: a row is the mean of what it sees.  All of it, one head of it or one row beside ordinary ones."""
+    p = Cells(seqs, H, KV, d, 64, dt, 2)
+    q, k = p.qkv[:, :H * d], p.param[0]
+    if what in ("both", "queries"):
+        q.zero_()
+    if what in ("both", "keys"):
+        p.codes[0], p.param[0] = 0, 0.0
+    if what == "a head":
+        q[:, :d] = 0
+        p.codes[0, :, 0], p.param[0, :, 0] = 0, 0.0
+    if what == "a row and its keys":
+        q[int(p.cu[1]) - 1] = 0
+        for j in range(min(64, sum(seqs[0]))):
+            p.codes[0, p.table[0][0], :, j], p.param[0, p.table[0][0], :, j] = 0, 0.0
+    if what == "tiny":
+        q *= 2.0**-76 if dt == "bf16" else 2.0**-9
+        k *= 2.0**-76 if dt == "bf16" else 2.0**-9
+    if what == "large and tiny":
+        q *= 2.0**-96 if dt == "bf16" else 2.0**-9
+        k *= 2.0**94 if dt == "bf16" else 2.0**9
+    p.write()
+    check_attention(*p.run(biases, max_q=max(n for _, n in seqs)), what=what)
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("q", [1, 5, 90, 200])
+@pytest.mark.parametrize("zero", ["queries", "a row", "none"])
+def test_whole_tiles_without_pages(zero, q, biases, dt):
+    """Sixty-four keys and more that have no page, at the front, in the middle and at the end, for rows of zero and ordinary ones."""
+    p = Cells([(450, q), (256, q), (0, q)], 8, 2, 128 if q % 2 else 64, 64, dt, 1)
+    p.table[0][1] = p.table[0][2] = p.table[0][5] = -1
+    p.table[1][0] = p.n_pages
+    p.table[1][-2] = p.table[2][0] = -7
+    if zero != "none":
+        p.qkv[slice(None) if zero == "queries" else slice(1, 2), :8 * p.d] = 0
+    check_attention(*p.run(biases, max_q=q), what="holes")
