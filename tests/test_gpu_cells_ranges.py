@@ -1,9 +1,11 @@
 """Attention over 4-bit cells where its running quantities can leave their range: values that are flat in a position (a scale of 0), scores that rise far beyond the first
 keys', queries and keys of zero.  Everything against the 64-bit implementation and the bounds of test_gpu_cells.py, whose derivation covers these inputs."""
+import random
+
 import pytest
 
 import paper_2403_01136_amd as lpq
-from test_gpu_cells import Cells, check_attention
+from test_gpu_cells import U16, Cells, check_attention
 from test_gpu_paged import ints
 
 pytestmark = pytest.mark.gpu
@@ -169,3 +171,55 @@ def test_whole_tiles_without_pages(zero, q, biases, dt):
     if zero != "none":
         p.qkv[slice(None) if zero == "queries" else slice(1, 2), :8 * p.d] = 0
     check_attention(*p.run(biases, max_q=q), what="holes")
+
+
+# ---- the ends of the range that the header gives for bf16 ---------------------------------------------------------------
+
+def check_scaled(out, parts, size, what):
+    """check_attention for values of about `size`, a power of two."""
+    check_attention((out.double() / size).to(out.dtype), [((r0, r1), (o / size, e / size)) for (r0, r1), (o, e) in parts], what=what)
+
+
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("kind", [k for k in KINDS if k != "long"])
+@pytest.mark.parametrize("k_exp,v_exp", [(95, 60), (-77, 60), (95, -77), (-77, -77)])
+def test_ends_of_the_range_in_bf16(k_exp, v_exp, kind, biases):
+    """Keys, queries and values next to 2^100, 2^64 and 2^-80, scores ordinary or rising."""
+    p, hints, slope = kind_of(kind, "bf16")
+    p.qkv[:, :p.H * p.d] *= 2.0**-k_exp
+    p.param[0] *= 2.0**k_exp
+    p.param[1] *= 2.0**v_exp
+    p.write()
+    out, parts = run(p, slope if biases else 0.0, hints)
+    assert bool((out[int(p.cu[-1]):] == 77).all())
+    out[int(p.cu[-1]):] *= 2.0**v_exp
+    check_scaled(out, parts, 2.0**v_exp, "ends")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q_exp,step_exp", [(50, 55), (98, 10), (20, 90), (94, -60)])
+def test_scores_next_to_the_end_in_bf16(q_exp, step_exp, d):
+    """Scores up to 2^116, each of them exact: visible keys with the largest share the weight equally.  Off by the output's rounding, values' or weights' times scales (U16 of 7 steps), and
+    2^-20 for 32-bit sums and the division."""
+    import torch
+    r, H, KV = random.Random(d), 4, 2
+    for seqs, max_q in (([(300, 1), (70, 6), (0, 1)], 6), ([(300, 1), (0, 300), (70, 90)], 300)):
+        p = Cells(seqs, H, KV, d, 32, "bf16", 1)
+        p.qkv[:, :H * d] = 2.0**q_exp
+        levels = [torch.tensor([r.randint(-7, 7) for _ in range(a + b)], device="cuda") for a, b in seqs]
+        p.param[0, ..., 0], p.param[0, ..., 1] = 2.0**step_exp, -8 * 2.0**step_exp
+        for s, lv in enumerate(levels):
+            for j in range(len(lv)):
+                p.codes[0, p.table[s][j // 32], :, j % 32] = int(lv[j]) + 8
+        p.write()
+        out, _ = run(p, 0.0, dict(max_q=max_q))
+        for s, (past, n) in enumerate(seqs):
+            at, off = torch.tensor([p.table[s][j // 32] for j in range(past + n)], device="cuda"), torch.arange(past + n, device="cuda") % 32
+            par = p.param[1, at, :, off].double()
+            v = p.codes[1, at, :, off].double() * par[..., :1] + par[..., 1:]
+            for t in range(n):
+                seen = levels[s][:past + t + 1]
+                rows = v[:past + t + 1][seen == seen.max()].repeat_interleave(H // KV, 1)
+                want, size = rows.mean(0), rows.abs().mean(0) + 7 * float(par[..., 0].max())
+                err = (out[p.cu[s] + t].double().view(H, d) - want).abs()
+                assert bool((err <= 2.0**-8 * want.abs() + (U16 + 2.0**-20) * size + 2.0**-25).all()), (s, t, float((err / size).max()))
