@@ -361,7 +361,7 @@ lpq_status lpq_packed_attention(const void *qkv, const lpq_attn_cfg *cfg, const 
  * and a code c stands for scale * c + zero.  Of x, the head_dim values of a head (the quantiser of lpq_quantize_pack, fp32 IEEE arithmetic, round-half-even):
  *   scale = type((max - min) / 15), a last place less if 15 * scale + zero would round to infinity;   zero = min (+0 for -0);
  *   code = clamp(rint((x - zero) / scale), 0, 15), 0 where scale is 0
- * A head with an infinity or NaN in it, or with max - min beyond the type's range, is stored as NaN throughout.
+ * A head with an infinity or NaN in it, or with max - min beyond fp32 (in bf16; fp16 heads of finite elements are numbers), is stored as NaN throughout.
  * A layer's step is lpq_qk_norm_rotary (where the model has it), lpq_paged_append4, lpq_paged_attention4. */
 
 /* Bytes of one K/V head's part of a page: page_size / 16 * 16 * (head_dim / 2 + 4); 0 if either is not supported.  Host-only. */

@@ -121,7 +121,7 @@ template <int D> __device__ __forceinline__ size_t group_of(const CellArgs& a, c
 // and q0 + remainder * rcp(s) before its rounding by 2^-45 of q.  That rounds as the quotient does: where a rounds differently above than below, a / s is half way between two fp32
 // numbers, a number m of 25 bits; a - m s, of numbers of 24 and 36 bits, is zero or 2^-37 of a at least, and zero it is not, as m s has more than 24 bits.  Scales below 2^-100, where
 // the remainder may be too small for an exponent, divide.
-// A head with an infinity or a NaN in it, or a range beyond the type's, is NaN throughout.
+// A head with an infinity or a NaN in it, or (in bf16) a range beyond fp32, is NaN throughout.
 template <int DT, int LANES>
 __device__ __forceinline__ u32x2 quantise_head(const u32x4 (&x)[2], uint32_t* param)
 {

@@ -6,7 +6,7 @@ import pytest
 
 import paper_2403_01136_amd as lpq
 from test_gpu_cells import U16, Cells, check_attention
-from test_gpu_paged import ints
+from test_gpu_paged import dtype_of, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -171,6 +171,25 @@ def test_whole_tiles_without_pages(zero, q, biases, dt):
     if zero != "none":
         p.qkv[slice(None) if zero == "queries" else slice(1, 2), :8 * p.d] = 0
     check_attention(*p.run(biases, max_q=q), what="holes")
+
+
+@pytest.mark.parametrize("dt,big,odd", [("fp16", 65504.0, False), ("bf16", 2.0**127, True), ("bf16", 2.0**126, False)])
+def test_widest_heads(dt, big, odd):
+    """The largest number of the type beside its negative: a range that fp32 holds is quantised, one that it does not is NaN throughout."""
+    import torch
+    d, KV = 64, 2
+    x = torch.zeros((1, 3 * KV * d), device="cuda")
+    x[0, KV * d::2], x[0, KV * d + 1::2] = big, -big
+    x = x.to(dtype_of(dt))
+    k, v = (torch.zeros((1, KV, lpq.lpq_cell_page_bytes(16, d)), dtype=torch.uint8, device="cuda") for _ in range(2))
+    lpq.lpq_paged_append4(x, k, v, ints([3]))
+    out = lpq.lpq_paged_load4(k, v, ints([3]), torch.zeros_like(x))[0, KV * d:].double()
+    if odd:
+        assert bool(torch.isnan(out).all())
+        return
+    # min is exact; of max the scale's rounding, and in fp16 a last place where 15 scales would be infinite: at most eps of fifteen scales, twice; then the output's
+    assert bool((out[1::2] == -big).all())
+    assert bool(((out[::2] - big).abs() <= 5 * big * torch.finfo(x.dtype).eps).all()), float(out[0])
 
 
 # ---- the ends of the range that the header gives for bf16 ---------------------------------------------------------------
