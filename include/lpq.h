@@ -394,8 +394,8 @@ lpq_status lpq_qk_norm_rotary(const void* qkv, const lpq_attn_cfg* cfg, const lp
 lpq_status lpq_paged_append4(const void* qkv, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, void* k_pages, void* v_pages, const int32_t* slots,
                              int32_t M, void* hip_stream);
 
-/* The inverse: what the slots hold, rounded once to the type, to the K and V parts of the rows of qkv; q parts, and rows without a slot in the pool, are left as they
- * were.  Slots may repeat.  For contexts that move to another pool, and for prompts whose lpq_packed_attention shall see what later steps will.
+/* The inverse: what the slots hold, rounded to the type (once in fp16; in bf16 from scale * c + zero rounded to fp32), to the K and V parts of the rows of qkv; q parts, and rows
+ * without a slot in the pool, are left as they were.  Slots may repeat.  For contexts that move to another pool, and for prompts whose lpq_packed_attention shall see what later steps will.
  * Errors: as lpq_paged_append. */
 lpq_status lpq_paged_load4(const void* k_pages, const void* v_pages, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const int32_t* slots, int32_t M,
                            void* qkv, void* hip_stream);

@@ -121,7 +121,7 @@ __device__ __forceinline__ uint32_t and_or(uint32_t v, uint32_t mask, uint32_t b
     asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v), "s"(mask), "v"(bits));
     return r;
 }
-// What a word of codes stands for, rounded once to the type.
+// What a word of codes stands for, rounded once to the type; in bf16, which has no such instruction, to fp32 first.
 template <int DT> __device__ __forceinline__ u32x4 cell_values(uint32_t w, uint32_t param)
 {
     u32x4 x;

@@ -192,6 +192,23 @@ def test_widest_heads(dt, big, odd):
     assert bool(((out[::2] - big).abs() <= 5 * big * torch.finfo(x.dtype).eps).all()), float(out[0])
 
 
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_loads_next_to_halves_between_two_numbers(dt):
+    """Scale times code half way between two numbers of the type, and a zero of -tiny, 0 or tiny: fp16 rounds their sum once; bf16 rounds it to 32 bits first, where the tiny ones are gone."""
+    import torch
+    d, t, last, tiny = 64, dtype_of(dt), {"fp16": 2.0**-10, "bf16": 2.0**-7}[dt], 2.0**-24 if dt == "fp16" else 2.0**-60
+    size = lpq.lpq_cell_page_bytes(16, d)
+    k = torch.zeros((1, 1, size), dtype=torch.uint8, device="cuda")
+    k[0, 0, :8 * d] = 0x33                             # codes 3 of scales of 1 + last: 3 + 3 last, between 3 + 2 last and 3 + 4 last, of which the last is even
+    param = torch.zeros((16, 2), device="cuda")
+    param[:, 0] = 1 + last
+    param[0:3, 1] = torch.tensor([-tiny, 0.0, tiny], device="cuda")
+    k[0, 0, 8 * d:] = param.to(t).view(torch.uint8).flatten()
+    out = lpq.lpq_paged_load4(k, k, ints([0, 1, 2]), torch.zeros((3, 3 * d), dtype=t, device="cuda"))[:, d:].double()
+    want = [3 + (2 if dt == "fp16" else 4) * last, 3 + 4 * last, 3 + 4 * last]
+    assert bool((out == torch.tensor(want, dtype=torch.float64, device="cuda")[:, None]).all()), out[:, 0].tolist()
+
+
 # ---- the ends of the range that the header gives for bf16 ---------------------------------------------------------------
 
 def check_scaled(out, parts, size, what):
