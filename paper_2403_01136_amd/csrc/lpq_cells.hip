@@ -156,9 +156,10 @@ __device__ __forceinline__ u32x2 quantise_head(const u32x4 (&x)[2], uint32_t* pa
         const float a = __fsub_rn(v[e], z), q0 = __fmul_rn(a, rcp);
         r[e] = __builtin_fmaf(__builtin_fmaf(-q0, s, a), rcp, q0);
     }
-    if (__any(s > 0.0f && s < 0x1p-100f))
+    if constexpr (DT == LPQ_DT_BF16)                   // fp16 has no such scales
+        if (__any(s > 0.0f && s < 0x1p-100f))
 #pragma unroll
-        for (int e = 0; e < N; ++e) r[e] = __fdiv_rn(__fsub_rn(v[e], z), s);
+            for (int e = 0; e < N; ++e) r[e] = __fdiv_rn(__fsub_rn(v[e], z), s);
 #pragma unroll
     for (int e = 0; e < N; ++e) r[e] = __builtin_rintf(__builtin_amdgcn_fmed3f(r[e], 0.0f, 15.0f));
     // code e at bit 4 (e / 2) of its half: sums below 2^16, exact
