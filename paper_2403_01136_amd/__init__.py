@@ -365,7 +365,7 @@ def _device_of(t):
     """Index of the current CUDA device, where the kernels run and t has to be."""
     import torch
     dev = t.get_device()
-    if dev < 0 or dev != torch._C._cuda_getDevice():   # a CUDA tensor: the runtime is up
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError("tensors must be on the current CUDA device")
     return dev
 
