@@ -407,6 +407,13 @@ def _attn_cfg(qkv, n_heads, n_kv_heads):
     return _attn_cfg_of(qkv.shape[1], n_heads, n_kv_heads, qkv.dtype)
 
 
+class _kept_attn_cfg(lpq_attn_cfg):
+    """One that all calls with the same heads are handed: it cannot be written to."""
+
+    def __setattr__(self, name, value):
+        raise AttributeError("an attention cfg that calls share")
+
+
 @functools.lru_cache(maxsize=256)
 def _attn_cfg_of(cols, n_heads, n_kv_heads, dtype):
     import torch
@@ -415,7 +422,7 @@ def _attn_cfg_of(cols, n_heads, n_kv_heads, dtype):
     heads = n_heads + 2 * n_kv_heads
     if n_heads < 1 or n_kv_heads < 1 or cols % heads:
         raise ValueError("qkv has %d columns, not a multiple of %d heads" % (cols, heads))
-    return lpq_attn_cfg(n_heads, n_kv_heads, cols // heads, LPQ_DT_FP16 if dtype is torch.float16 else LPQ_DT_BF16)
+    return _kept_attn_cfg.from_buffer_copy(lpq_attn_cfg(n_heads, n_kv_heads, cols // heads, LPQ_DT_FP16 if dtype is torch.float16 else LPQ_DT_BF16))
 
 
 def _paged_cfg(qkv, k_pages, v_pages):
