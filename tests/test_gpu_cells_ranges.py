@@ -173,6 +173,55 @@ def test_whole_tiles_without_pages(zero, q, biases, dt):
     check_attention(*p.run(biases, max_q=q), what="holes")
 
 
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q", [1, 3, 20, 50, 150])
+def test_rows_that_see_nothing_of_either_type(q, d, biases, dt):
+    """No keys, fewer keys than new tokens, negative lengths, tables without pages: zeros, and the other sequences as ever."""
+    p = Cells([(0, q), (20, q), (100, q), (0, q), (300, q)], 4, 2, d, 64, dt, 2)
+    p.table[0] = [-1] * len(p.table[0])
+    p.table[4] = [p.n_pages + i for i in range(len(p.table[4]))]
+    out, parts = p.run(biases, max_q=q, kv_lens=[0, 20 + q, -3, max(q - 1, 0), 300 + q])
+    check_attention(out, parts, what="nothing to see")
+    for s in (0, 2, 4):
+        assert bool((out[s * q:(s + 1) * q] == 0).all())
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("P", [16, 64])
+def test_ids_that_are_no_pages_of_either_type(P, d, biases, dt):
+    for q in (1, 3, 60, 150):
+        p = Cells([(400, q), (333, q), (300, q)], 6, 2, d, P, dt, 1, width_extra=0)
+        p.table[0][0], p.table[0][3], p.table[1][2], p.table[1][-2] = -1, p.n_pages, -2**31, 2**31 - 1
+        for i in range(64 // P, 3 * 64 // P):          # a whole tile of 64 keys and more
+            p.table[1][i] = -1
+        p.table[2] = [-5] * len(p.table[2])
+        cap = len(p.table[0]) * P
+        check_attention(*p.run(biases, max_q=q), what="bad pages")
+        check_attention(*p.run(biases, max_q=q, kv_lens=[cap + 20, cap + 5, 10]), what="beyond the table")
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("biases", [False, True], ids=["plain", "biases"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_and_equal_scores_of_either_type(d, biases, dt):
+    """Scores in the hundreds and thousands: one key takes all; and all of them equal, of keys of zero and of the same key everywhere."""
+    for seqs in ([(500, 1), (300, 30)], [(300, 6), (40, 2)]):
+        p = Cells(seqs, 4, 2, d, 32, dt, 1)
+        p.qkv[:, :4 * d] *= 20
+        check_attention(*p.run(biases, max_q=seqs[1][1]), what="large")
+        p.codes[0] = p.codes[0, :1, :1, :1]
+        p.param[0] = p.param[0, :1, :1, :1]
+        p.write()
+        check_attention(*p.run(biases, max_q=max(n for _, n in seqs)), what="equal")
+        p.codes[0], p.param[0] = 0, 0.0
+        p.write()
+        check_attention(*p.run(biases, max_q=max(n for _, n in seqs)), what="zero")
+
+
 @pytest.mark.parametrize("dt,big,odd", [("fp16", 65504.0, False), ("bf16", 2.0**127, True), ("bf16", 2.0**126, False)])
 def test_widest_heads(dt, big, odd):
     """The largest number of the type beside its negative: a range that fp32 holds is quantised, one that it does not is NaN throughout."""
