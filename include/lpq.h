@@ -400,9 +400,9 @@ lpq_status lpq_paged_append4(const void* qkv, const lpq_attn_cfg* cfg, const lpq
 lpq_status lpq_paged_load4(const void* k_pages, const void* v_pages, const lpq_attn_cfg* cfg, const lpq_page_pool* pool, const int32_t* slots, int32_t M,
                            void* qkv, void* hip_stream);
 
-/* lpq_paged_attention over pages of cells, with the same arguments, masks and limits.  A position that is stored as NaN makes the rows that see it NaN.  Products are of
- * numbers with 11 bits, sums of 32 bits.  Where a sequence and K/V head have up to 32 rows, codes are multiplied as they are, and weights times V's scales are what is rounded.
- * With more, weights and values of V are, and in bf16 values of K (tiles of them without a power of two).
+/* lpq_paged_attention over pages of cells, with the same arguments, masks and limits.  A position that is stored as NaN makes the rows that see it NaN.  Sums are of
+ * 32 bits.  Where a sequence and K/V head have up to 32 rows, codes are multiplied as they are, weights times V's scales with 22 bits (11 in bf16 with more than 8 rows).  With more rows
+ * weights and values of V are multiplied with 11 bits, and in bf16 values of K (tiles of them without a power of two).
  * In bf16 elements of q and K are to be below 2^100 and of V below 2^64, sums of |q_i k_i| below 2^120: what the rows see beyond that may make them infinite, NaN or wrong.  Heads whose
  * elements are all below 2^-80 keep fewer bits.
  * Partial results are kept in the library's workspace, up to 290 MiB of them.  A smaller reservation splits less: tiles of chunks and prompts first, then, below 34 MiB,

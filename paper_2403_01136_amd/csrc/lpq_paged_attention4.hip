@@ -8,9 +8,10 @@
 //     sum_j w_j v_jf = sum_j (w_j s'_j) c'_jf + sum_j w_j z'_j
 // where the first sum of each is the matrix units' and the others cost two operations a score.  A code in bits 4 to 7 of an fp16 number without exponent is that number,
 // code * 2^-20: unpacking a word of eight takes three shifts and four ANDs, for queries of either type: those in bf16 are taken by a power of two for each row, which changes
-// none of their eight bits that count.  Codes are exact; what is rounded are the weights w s', to fp16 beside a largest of 2^12 or more.  What that takes from them is added up in
-// 32 bits and counts as for a code of 8, so that only the codes' distance from it sees the rounding; in fp16, where tiles of up to 8 rows leave columns of the products idle, it
-// has those (an error of 2.1e-4 of a result, all of it the output's rounding, where it was 3.0e-4 to 3.2e-4 without; 16 sequences of 40 heads 18.6 us for 18.4).
+// none of their eight bits that count.  Codes are exact; what is rounded are the weights w s', to fp16 beside a largest of 2^12 or more.  What that takes from them is multiplied as well, in columns
+// that tiles of up to 8 rows leave idle (16 sequences of 40 heads 18.6 us for 18.4 without, 61 of 64 heads over 8 35.8 for 35.4), in fp16 also by second products of larger tiles (24 drafts 31.6 us for
+// 29.7): an error of 2.1e-4 of a result in fp16, all of it the output's rounding, for 2.7e-4 to 3.2e-4 without.  Larger tiles in bf16, whose outputs are rounded at 1.66e-3, would take as much for 1.67e-3:
+// there it is added up in 32 bits and counts as for a code of 8, so that only the codes' distance from it sees the rounding.
 #include <algorithm>
 
 #include "lpq_batch_attention.h"
@@ -96,7 +97,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
     constexpr int W = D / 32, F = D / 16;                                        // words of a lane's codes of a key; its features of V
     constexpr int NT = ROWS == 32 ? 2 : 1, PARTS = ROWS < 16 ? 16 / ROWS : 1, N = 8 / PARTS;     // column tiles; parts of the keys; a lane's keys of a step
     constexpr int SLOT = ROWS * (D + 2);
-    constexpr bool FINE = DT == LPQ_DT_FP16 && PARTS > 1;                        // what rounding takes from weights goes to idle columns
+    constexpr bool FINE = DT == LPQ_DT_FP16 || PARTS > 1, SECOND = FINE && PARTS == 1;           // what rounding takes from weights is multiplied: in idle columns, or by products of its own
     typedef uint32_t kcodes_t __attribute__((ext_vector_type(W)));
     typedef uint32_t params_t __attribute__((ext_vector_type(N < 4 ? N : 4)));
     typedef std::conditional_t<D == 128, uint32_t, uint16_t> vcodes_t;
@@ -205,7 +206,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
             for (int e = 0; e < F; ++e) o[t][e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 
-        const int rest_of = FINE ? __builtin_amdgcn_update_dpp(0, part, 0x120 + ROWS, 0xf, 0xf, false) : 0;
+        const int rest_of = PARTS > 1 ? __builtin_amdgcn_update_dpp(0, part, 0x120 + ROWS, 0xf, 0xf, false) : 0;
         // the lane's keys of a step, in order of the quarters' eight {4 quarter + 0..3, 16 + 4 quarter + 0..3}: N from the part's N-th on
         const int my_group = N < 8 ? part * N / 4 : 0, my_key = 16 * my_group + 4 * quarter + part * N % 4;
         const uint32_t koff = (uint32_t)(col * (D / 2) + quarter * (D / 8)), voff = (uint32_t)(4 * quarter * (D / 2) + col * (D / 32)), poff = (uint32_t)(8 * D + 4 * (my_key % 16));
@@ -319,7 +320,7 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
             __builtin_amdgcn_sched_barrier(0);
             load_k(min(n + 1, n_last - 1));
             __builtin_amdgcn_sched_barrier(0);
-            h8 pf[NT];
+            h8 pf[NT], rf[SECOND ? NT : 1];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 uint32_t par[N];
@@ -378,14 +379,16 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     pk[k / 2] = Elem<LPQ_DT_FP16>::pack(t0, t1);
                     if constexpr (FINE) {
                         const h2 p16 = as_h2(pk[k / 2]);
-                        rk[k / 2] = __builtin_amdgcn_update_dpp(0, Elem<LPQ_DT_FP16>::pack(t0 - (float)p16[0], t1 - (float)p16[1]), 0x120 + ROWS, 0xf, 0xf, false);     // row_ror
+                        rk[k / 2] = Elem<LPQ_DT_FP16>::pack(t0 - (float)p16[0], t1 - (float)p16[1]);
+                        if constexpr (!SECOND) rk[k / 2] = __builtin_amdgcn_update_dpp(0, rk[k / 2], 0x120 + ROWS, 0xf, 0xf, false);      // row_ror
                     } else ws[t] = __builtin_amdgcn_fdot2(as_h2(pk[k / 2]), h2{-1, -1}, ws[t] + (t0 + t1), false);
                 }
-                u32x4 operand;                         // this part's keys; FINE: what the next part's lost; zero for the others
+                u32x4 operand;                         // this part's keys; what the next part's lost; zero for the others
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    operand[k] = PARTS == 1 || part == k / (N / 2) ? pk[k % (N / 2)] : FINE && (PARTS == 2 || rest_of == k / (N / 2)) ? rk[k % (N / 2)] : 0u;
+                    operand[k] = PARTS == 1 || part == k / (N / 2) ? pk[k % (N / 2)] : PARTS == 2 || rest_of == k / (N / 2) ? rk[k % (N / 2)] : 0u;
                 pf[t] = __builtin_bit_cast(h8, operand);
+                if constexpr (SECOND) rf[t] = __builtin_bit_cast(h8, u32x4{rk[0], rk[1], rk[2], rk[3]});
             }
             // V^T operands: halves of two keys' words side by side, then pairs
 #pragma unroll
@@ -400,6 +403,9 @@ __device__ __forceinline__ void stream4_block(const AttnArgs& a, int block)
                     const int f = D == 128 ? 2 * e + half : e;
 #pragma unroll
                     for (int t = 0; t < NT; ++t) o[t][f] = Elem<LPQ_DT_FP16>::mfma16(__builtin_bit_cast(h8, vt), pf[t], o[t][f]);
+                    if constexpr (SECOND)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) o[t][f] = Elem<LPQ_DT_FP16>::mfma16(__builtin_bit_cast(h8, vt), rf[t], o[t][f]);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);

@@ -1,12 +1,13 @@
 """Attention over 4-bit cells where its running quantities can leave their range: values that are flat in a position (a scale of 0), scores that rise far beyond the first
 keys', queries and keys of zero.  Everything against the 64-bit implementation and the bounds of test_gpu_cells.py, whose derivation covers these inputs."""
+import math
 import random
 
 import pytest
 
 import paper_2403_01136_amd as lpq
 from test_gpu_cells import U16, Cells, check_attention
-from test_gpu_paged import dtype_of, ints
+from test_gpu_paged import dtype_of, gen, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -220,6 +221,30 @@ def test_large_and_equal_scores_of_either_type(d, biases, dt):
         p.codes[0], p.param[0] = 0, 0.0
         p.write()
         check_attention(*p.run(biases, max_q=max(n for _, n in seqs)), what="zero")
+
+
+@pytest.mark.parametrize("whole", [True, False], ids=["whole", "parts"])
+@pytest.mark.parametrize("dt,q,H,KV,d", [("fp16", 1, 8, 2, 64), ("bf16", 1, 4, 1, 128), ("fp16", 2, 8, 2, 128), ("bf16", 4, 4, 2, 64), ("fp16", 1, 32, 2, 64), ("fp16", 1, 12, 1, 128), ("fp16", 5, 12, 2, 128),
+                                         ("fp16", 3, 40, 4, 64), ("bf16", 1, 8, 1, 128)])
+def test_weights_beyond_their_eleven_bits(dt, q, H, KV, d, whole):
+    """Up to 32 rows of a sequence and K/V head in fp16, up to 8 in bf16: what rounding takes from weights times scales is multiplied too.  All values are 2^-4, of a scale of 1, codes of 15 and zeros
+    of -14.9375, so that is every row's result whatever its weights; a row's keys but the first have one weight between a sixteenth and one of the first's, so that roundings of it, up to u16 of it,
+    are of one sign and would show sevenfold or more.  Off by the output's rounding, 32-bit sums of n keys and a few operations on numbers of up to 15 and their difference, the units' 2^-18 and the
+    remainders' rounding (u16 of u16 / 2, codes of 15)."""
+    import torch
+    u, n = {"fp16": 2.0**-11, "bf16": 2.0**-8}[dt], 100
+    p = Cells([(n - q, q)] * 12, H, KV, d, 16, dt, 1)
+    p.qkv[:, :H * d] = 0
+    p.qkv[:, :H * d:d] = 2.7 * math.sqrt(d) * torch.rand((p.M, H), generator=gen(7), device="cuda").to(p.qkv.dtype)
+    p.codes[0], p.param[0] = 0, 0.0
+    for row in p.table:
+        p.param[0, row[0], :, 0, 1] = 1.0
+    p.codes[1], p.param[1, ..., 0], p.param[1, ..., 1] = 15, 1.0, -14.9375
+    p.write()
+    out, _ = run(p, 0.0, dict(max_q=q, max_kv=192 if whole else 3000))
+    got = out[:int(p.cu[-1])].double()
+    allowed = u * 2.0**-4 + (2 * n + 8) * 2.0**-24 * 29.9375 + 2.0**-18 + 15 * U16 * U16 / 2
+    assert float((got - 2.0**-4).abs().max()) <= allowed * (1 + u), (float((got - 2.0**-4).abs().max()), allowed)
 
 
 @pytest.mark.parametrize("dt,big,odd", [("fp16", 65504.0, False), ("bf16", 2.0**127, True), ("bf16", 2.0**126, False)])
