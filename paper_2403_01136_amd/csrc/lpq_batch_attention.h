@@ -440,7 +440,8 @@ __device__ __forceinline__ void tile_block(const AttnArgs& a, int block)
     constexpr bool SCALED = SRC == SRC_CELLS && DT == LPQ_DT_BF16;
     // K of fp16 cells stays codes, whose products with a row get scale and zero behind them, as in the streaming kernel: rounded K puts 2.5e-4 of a result of ordinary scores into it,
     // V 2.0e-4, beside an output's rounding of 2.1e-4 (fp16) and 1.6e-3 (bf16).  It takes 6 % (two chunks of up to 512 tokens beside 9 sequences that decode, 56 heads over 8, biases:
-    // 128.3 us; K rounded 120.8; parameters in LDS as fp32 products with c, twice the reads, 132.6); V so would take as much again and leave weights times scales rounded instead.
+    // 128.3 us; K rounded 120.8; parameters in LDS as fp32 products with c, twice the reads, 132.6).  V's values and the weights are rounded: 1.3 to 1.63 times an output's rounding over 60 batches.  V as codes
+    // too, with weights times scales and what rounding takes from them as two operands, leaves the output's rounding alone, but takes 179 us there, and 738 for 523 of a chunk behind 6000 positions.
     constexpr bool K_CODES = SRC == SRC_CELLS && DT == LPQ_DT_FP16;
     constexpr int PT = SRC == SRC_CELLS ? (int)LPQ_DT_FP16 : DT;
     typedef typename Elem<PT>::v8 V8;

@@ -351,7 +351,7 @@ AttentionPlan attention_plan(const lpq_attn_cfg& c, AttentionSource source, int 
     const int64_t most = (int64_t)std::min(max_q, M) * group;
     // Rows of the streaming kernel's tiles: those to expect where it is alone, else those of a decoding sequence; from 4 on for cells.  Two tiles of 8 rows for 9 to 16 where walks are
     // short and a worker has few steps of them: cells read twice cost less there than a softmax that idle columns share saves.  One tile of 16 / two of 8, us: 16 sequences of 400 to 700
-    // positions, 80 heads (5 K/V heads) 20.4 / 17.0; 24, 64 (8), two tokens, up to 700 20.5 / 18.4; 24, 40 (8), three tokens, up to 2600 26.4 / 24.3, up to 4000 28.5 / 29.0, up to 9000 36.7 / 39.6; 8 such up to 4000 26.8 / 27.7, up
+    // positions, 80 heads (5 K/V heads) 20.2 / 16.6; 24, 64 (8), two tokens, up to 700 20.5 / 18.4; 24, 40 (8), three tokens, up to 2600 26.4 / 24.3, up to 4000 28.5 / 29.0, up to 9000 36.7 / 39.6; 8 such up to 4000 26.8 / 27.7, up
     // to 8000 31.2 / 34.7; one of 90001, 112 (8) 37.8 / 43.9.
     auto tile_of_rows = [&](int64_t rows, int smallest) { return rows <= 4 && smallest <= 4 ? 4 : rows <= 8 && smallest <= 8 ? 8 : rows <= STREAM_ROWS ? STREAM_ROWS : 2 * STREAM_ROWS; };
     const int smallest = source == SRC_CELLS ? 4 : STREAM_ROWS;

@@ -23,7 +23,7 @@ namespace {
 // ---- streaming kernel -----------------------------------------------------------------------------
 // Bound by the memory while it streams, D + 8 bytes per key and K/V head; by starts and ends of walks where they are short.  Workers are single waves, two a SIMD (the 32-row tile, with
 // its registers, one), with equal shares of the list of 32-key steps; the loads of one step are under way while the step before is computed.  61 sequences of 100 to 7000 positions, 64 heads (8 K/V heads),
-// bf16, 29.6 us and 4.9 for the parts (112 MB; 3.8 TB/s, with some 8 us of start and end in it); one of 90001, 56 heads (8), fp16 25.0 and 5.0; 16 of 400 to 700, 40 heads 14.2 and 3.9; one wave
+// bf16, 30.0 us and 4.7 for the parts (112 MB; 3.7 TB/s, with some 8 us of start and end in it); one of 90001, 56 heads (8), fp16 25.7 and 4.8; 16 of 400 to 700, 40 heads 14.8 and 3.9; one wave
 // a SIMD 62 for the first, three 41.
 // Products on 16x16x32, columns = rows of the problem:
 //   S^T = C_k . Q^T  lane (i = lane % 16, q = lane / 16) holds codes D / 4 q .. of key i as they lie; a word makes an operand of four pairs, of neighbours, as the query's row has them.
